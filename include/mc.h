@@ -26,14 +26,14 @@
  *     the first of two kernels) stay enqueued, so the outputs are undefined.
  *   - The calls that take host lengths or offsets hand them to a kernel as an
  *     argument where they are few: mc_prefill_attn_paged and mc_prefill_attn_auto up
- *     to 63 requests with new tokens, mc_kv_append_paged up to 64 requests,
+ *     to 63 requests with new tokens, mc_kv_append_paged and mc_kv_rope_append_paged up to 64 requests,
  *     mc_prefix_hash and mc_prefix_match up to 64 requests and 64 instances.
  *     Longer tables, and the lists of _paged_split and _prepare, are uploaded
  *     from a small ring of pinned HOST slots the library owns.  A call that uploads
  *     may allocate a slot with hipHostMalloc (the first calls, or a list larger than
  *     any before), and with 256 uploads in flight it waits for the oldest: such
  *     calls are not for stream capture.  The run calls (mc_prefill_attn_run,
- *     _run_split, mc_kv_append_run), pack / unpack and the merge upload nothing,
+ *     _run_split, mc_kv_append_run, mc_kv_rope_append_run), pack / unpack and the merge upload nothing,
  *     allocate nothing and never wait.  Calls may come from several host threads.
  *   - Page ids that live in device memory cannot be range-checked without a
  *     sync: an id outside [0, num_pages) is undefined behaviour.
@@ -338,6 +338,79 @@ mc_status mc_kv_append_paged(const mc_attn_params* p, const void* k_new, const v
                              void* v_pool, const int32_t* block_tables, int32_t max_pages_per_req,
                              const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch,
                              void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * mc_kv_append_paged with what stands before it in a layer: the new tokens' Q and K head rows are normalised (where a weight is
+ * given), rotated by their positions, and Q is written out while K and V go into their page slots - one pass over the projections.
+ *
+ *   x         a head row of Q or K (D elements), t its token's position: P_r + i for token i of request r
+ *   norm      y = x * rsqrt(mean(x^2) + norm_eps) * weight, if the weight is not NULL; else y = x
+ *   rotation  of the first R = rotary_dim elements, pair (u, v) number i by the angle a = t * inv_freq[i]:
+ *             (u, v) -> gain * (u cos a - v sin a, v cos a + u sin a);  the pairs are (y[i], y[i + R/2]) (MC_ROPE_HALF) or
+ *             (y[2i], y[2i + 1]) (MC_ROPE_PAIRS); elements R .. D-1 stay as they are
+ *   V         verbatim
+ *
+ * fp32 between the load and the one rounding to p->dtype (to nearest even); angles in 64 bits, so that far positions lose nothing.
+ */
+typedef enum { MC_ROPE_HALF = 0, MC_ROPE_PAIRS = 1 } mc_rope_layout;
+/* How mc_rope_init stretches the frequencies f_i = base^(-2i/R) for contexts `factor` times as long:
+ *   PLAIN     f_i
+ *   LINEAR    f_i / factor
+ *   BASE      with the base multiplied by factor^(R / (R - 2))
+ *   BY_PARTS  f_i (g_i + (1 - g_i) / factor), g_i = clamp((n_i - low) / (high - low), 0, 1), n_i = original_len f_i / 2 pi the
+ *             turns of pair i over the original context */
+typedef enum { MC_ROPE_PLAIN = 0, MC_ROPE_LINEAR = 1, MC_ROPE_BASE = 2, MC_ROPE_BY_PARTS = 3 } mc_rope_scaling;
+#define MC_ROPE_MAX_PAIRS 64
+typedef struct {
+  int32_t rotary_dim;  /* R: a multiple of 16 from 0 to head_dim */
+  int32_t layout;      /* mc_rope_layout */
+  float norm_eps;      /* >= 0 */
+  float gain;          /* > 0: factor on the rotated elements (1 leaves their length) */
+  double inv_freq[MC_ROPE_MAX_PAIRS];   /* radians a position, pairs 0 .. R/2 - 1 */
+} mc_rope_params;
+
+/*
+ * Fills inv_freq (entries past R/2 with zeros) and rotary_dim; the other fields are the caller's.  Host arithmetic only.
+ * MC_ERR_NULL: rope; MC_ERR_UNSUPPORTED: rotary_dim not a multiple of 16 in [0, 128], unknown scaling; MC_ERR_SHAPE: base or factor
+ * not a finite positive number, BY_PARTS without 0 <= low < high (finite) and a finite original_len > 0.
+ */
+mc_status mc_rope_init(mc_rope_params* rope, int32_t rotary_dim, double base, int32_t scaling, double factor, double low,
+                       double high, double original_len);
+
+/*
+ *   q        dev   [total_new_tokens, Hq, D], requests back to back
+ *   k, v     dev   [total_new_tokens, Hkv, D]
+ *   strides  host  int64 [3]: elements from token to token of q, k and v, such as the width of a fused projection whose
+ *                  columns they are; NULL: Hq D, Hkv D, Hkv D.  A token's heads are always dense.  At least those, and a multiple
+ *                  of 16 bytes
+ *   q_norm, k_norm  dev  [D] weights of p->dtype, or NULL
+ *   q_out    dev   [total_new_tokens, Hq, D] dense; may be q itself where q is dense, may not overlap the inputs otherwise
+ *   the rest as in mc_kv_append_paged (workspace: mc_kv_append_workspace_bytes(batch)), same status codes; also MC_ERR_NULL for
+ *   rope, MC_ERR_UNSUPPORTED for rotary_dim, layout, MC_ERR_SHAPE for norm_eps, gain, a frequency that is not finite, strides.
+ *
+ * mc_kv_rope_append_run takes the batch from a plan of mc_prefill_attn_prepare, as mc_kv_append_run does.
+ */
+mc_status mc_kv_rope_append_paged(const mc_attn_params* p, const mc_rope_params* rope, const void* q, const void* k, const void* v,
+                                  const int64_t* strides, const void* q_norm, const void* k_norm, void* q_out, void* k_pool,
+                                  void* v_pool, const int32_t* block_tables, int32_t max_pages_per_req, const int32_t* prefix_lens,
+                                  const int32_t* new_lens, int32_t batch, void* workspace, size_t workspace_bytes, void* hip_stream);
+mc_status mc_kv_rope_append_run(const mc_attn_params* p, const mc_attn_plan* plan, const mc_rope_params* rope, const void* q,
+                                const void* k, const void* v, const int64_t* strides, const void* q_norm, const void* k_norm,
+                                void* q_out, void* k_pool, void* v_pool, const int32_t* block_tables, int32_t max_pages_per_req,
+                                const void* workspace, void* hip_stream);
+/*
+ * The form of a decode step: one new token a row, whose length stands in DEVICE memory, so that a captured step can be replayed
+ * while the lengths grow.
+ *
+ *   q, k, v   dev  one token a row: [batch, Hq, D], [batch, Hkv, D] twice
+ *   seq_lens  dev  int32 [batch]: the row's length with its new token, which stands at position seq_lens[r] - 1.  A row whose length
+ *                  is not in [1, max_pages_per_req * 16] (a padding row: 0) is left out: its q_out and the pools stay as they are
+ * Nothing is allocated, uploaded or waited for; the call can be captured.
+ */
+mc_status mc_kv_rope_append_decode(const mc_attn_params* p, const mc_rope_params* rope, const void* q, const void* k, const void* v,
+                                   const int64_t* strides, const void* q_norm, const void* k_norm, void* q_out, void* k_pool,
+                                   void* v_pool, const int32_t* block_tables, int32_t max_pages_per_req, const int32_t* seq_lens,
+                                   int32_t batch, void* hip_stream);
 
 /*
  * Store path of layer-wise prefill (Section 5.2): gather pages of one layer's

@@ -27,7 +27,10 @@ EXPORTS = ("mc_status_string", "mc_prefill_attn_workspace_bytes", "mc_prefill_at
            "mc_kv_unpack_layer_ordered", "mc_prefill_attn_suggest_kv_splits", "mc_kv_check_page_ids",
            "mc_prefill_attn_plan", "mc_prefill_attn_prepare", "mc_prefill_attn_run", "mc_prefill_attn_run_split",
            "mc_kv_append_run", "mc_prefill_attn_auto_workspace_bytes", "mc_prefill_attn_auto",
-           "mc_prefill_attn_paged_noalloc")
+           "mc_prefill_attn_paged_noalloc", "mc_rope_init", "mc_kv_rope_append_paged", "mc_kv_rope_append_run",
+           "mc_kv_rope_append_decode")
+MC_ROPE_HALF, MC_ROPE_PAIRS = 0, 1
+MC_ROPE_PLAIN, MC_ROPE_LINEAR, MC_ROPE_BASE, MC_ROPE_BY_PARTS = 0, 1, 2, 3
 MC_MAX_KV_SPLITS = 256
 
 
@@ -43,6 +46,11 @@ class McAttnPlan(ctypes.Structure):
                 ("need_pages", ctypes.c_int32), ("total_new_tokens", ctypes.c_int64), ("reqs_offset", ctypes.c_int64),
                 ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("reserved", ctypes.c_int32)]
+
+
+class McRopeParams(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("norm_eps", ctypes.c_float), ("gain", ctypes.c_float),
+                ("inv_freq", ctypes.c_double * 64)]
 
 
 class McError(RuntimeError):
@@ -126,6 +134,15 @@ def lib():
         l.mc_prefix_match.argtypes = [vp, vp, i32, vp, vp, i32, vp, vp, vp, vp, ctypes.c_size_t, vp]
         l.mc_attn_merge_lse.restype = ctypes.c_int
         l.mc_attn_merge_lse.argtypes = [vp, vp, i32, i64, i32, i32, vp, vp, vp]
+        f64, rp = ctypes.c_double, ctypes.POINTER(McRopeParams)
+        l.mc_rope_init.restype = ctypes.c_int
+        l.mc_rope_init.argtypes = [rp, i32, f64, i32, f64, f64, f64, f64]
+        l.mc_kv_rope_append_paged.restype = ctypes.c_int
+        l.mc_kv_rope_append_paged.argtypes = [pp, rp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, i32, vp, ctypes.c_size_t, vp]
+        l.mc_kv_rope_append_run.restype = ctypes.c_int
+        l.mc_kv_rope_append_run.argtypes = [pp, pl_, rp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp]
+        l.mc_kv_rope_append_decode.restype = ctypes.c_int
+        l.mc_kv_rope_append_decode.argtypes = [pp, rp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, vp]
         try:
             from . import _mccall
         except ModuleNotFoundError:                        # none was built for this Python
@@ -173,13 +190,20 @@ _KINDS = {
     "mc_prefix_match": "pQipQippppii",
     "mc_kv_append_paged": "spppppiIIipii",
 }
+# ... and of those that keep the cache beside the prefill's attention (strides: three integers in a ctypes array).
+_CACHE_KINDS = {
+    "mc_kv_rope_append_paged": "sspppsppppppiIIipii",
+    "mc_kv_rope_append_run": "ssspppsppppppipi",
+    "mc_kv_rope_append_decode": "sspppsppppppipii",
+}
+_ALL_KINDS = {**_KINDS, **_CACHE_KINDS}
 
 
 def _enqueue(name: str, *args) -> None:
-    """The library's function ``name`` with arguments as _KINDS has them."""
+    """The library's function ``name`` with arguments as _KINDS and _CACHE_KINDS have them."""
     if _call is None:
         lib()
-    st = _call(_function[name], _KINDS[name], *args)
+    st = _call(_function[name], _ALL_KINDS[name], *args)
     if st != MC_OK:
         raise McError(st, name)
 
@@ -566,3 +590,111 @@ def attn_params(num_q_heads: int, num_kv_heads: int, head_dim: int, page_size: i
                 dtype: str, softmax_scale: float = 0.0) -> McAttnParams:
     return McAttnParams(num_q_heads, num_kv_heads, head_dim, page_size, num_pages,
                         MC_DTYPE_BF16 if dtype == "bf16" else MC_DTYPE_F32, softmax_scale)
+
+
+def rope_params(rotary_dim: int, layout: int, base: float = 10000.0, scaling: int = MC_ROPE_PLAIN, factor: float = 1.0, low: float = 1.0,
+                high: float = 4.0, original_len: float = 8192.0, gain: float = 1.0, norm_eps: float = 1e-6) -> McRopeParams:
+    """The rotation of mc_kv_rope_append_*; frequencies by mc_rope_init (or set ``inv_freq`` afterwards)."""
+    r = McRopeParams(0, layout, norm_eps, gain)
+    st = int(lib().mc_rope_init(ctypes.byref(r), rotary_dim, base, scaling, factor, low, high, original_len))
+    if st != MC_OK:
+        raise McError(st, "mc_rope_init")
+    return r
+
+
+_torch = None
+_DTYPES: dict = {}             # mc_dtype -> torch dtype
+
+
+def _dtypes() -> dict:
+    global _torch
+    if _torch is None:
+        import torch
+        _DTYPES.update({MC_DTYPE_BF16: torch.bfloat16, MC_DTYPE_F32: torch.float32})
+        _torch = torch
+    return _DTYPES
+
+
+def _dense(name: str, device: int, t, dtype, least: int) -> None:
+    """A dense tensor of a call: its type, its device, and that it has the elements the call will use."""
+    if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or t.numel() < least:
+        raise ValueError(f"{name}: dense {dtype} of at least {least} elements on device {device} wanted, "
+                         f"not {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+
+
+def _row_stride(name: str, device: int, t, dtype, tokens: int, heads: int, dim: int) -> int:
+    """Elements from token to token of [tokens, heads, dim] or [tokens, heads * dim], a token's heads dense."""
+    shape, stride = t.shape, t.stride()
+    fits = (len(shape) == 2 and shape[1] == heads * dim and stride[1] == 1) or (
+        len(shape) == 3 and shape[1] == heads and shape[2] == dim and stride[2] == 1 and (stride[1] == dim or heads == 1))
+    if not fits or shape[0] != tokens or t.dtype is not dtype or t.get_device() != device:
+        raise ValueError(f"{name}: {dtype} [{tokens}, {heads}, {dim}] with dense heads on device {device} wanted, "
+                         f"not {t.dtype} {tuple(shape)} strides {stride} on {t.device}")
+    return stride[0] if tokens > 1 else heads * dim
+
+
+def _pools(params, device: int, dtype, k_pool, v_pool) -> None:
+    least = params.num_pages * params.num_kv_heads * params.page_size * params.head_dim
+    _dense("k_pool", device, k_pool, dtype, least)
+    _dense("v_pool", device, v_pool, dtype, least)
+
+
+def _table(device: int, block_tables, rows: int) -> int:
+    """Columns of a block table that has ``rows`` rows."""
+    if block_tables.dim() != 2 or block_tables.shape[0] < rows:
+        raise ValueError(f"block_tables: [{rows}, pages] wanted, not {tuple(block_tables.shape)}")
+    _dense("block_tables", device, block_tables, _torch.int32, 0)
+    return block_tables.shape[1]
+
+
+def _rope_tensors(params, q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, tokens: int):
+    """Looks the tensors of a rotation call over: (device, strides or None where all of them are dense)."""
+    dtype = _dtypes()[params.dtype]
+    device, Hq, Hkv, D = q.get_device(), params.num_q_heads, params.num_kv_heads, params.head_dim
+    strides = (_row_stride("q", device, q, dtype, tokens, Hq, D), _row_stride("k", device, k, dtype, tokens, Hkv, D),
+               _row_stride("v", device, v, dtype, tokens, Hkv, D))
+    if q_norm is not None:
+        _dense("q_norm", device, q_norm, dtype, D)
+    if k_norm is not None:
+        _dense("k_norm", device, k_norm, dtype, D)
+    _dense("q_out", device, q_out, dtype, tokens * Hq * D)
+    _pools(params, device, dtype, k_pool, v_pool)
+    return device, None if strides == (Hq * D, Hkv * D, Hkv * D) else (ctypes.c_int64 * 3)(*strides)
+
+
+def _rope(rope):
+    if not isinstance(rope, McRopeParams):
+        raise TypeError(f"McRopeParams wanted, not {type(rope).__name__}")
+    return rope
+
+
+def mc_kv_rope_append_paged(params: McAttnParams, rope: McRopeParams, q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, block_tables,
+                            prefix_lens, new_lens, workspace, stream=None) -> None:
+    """Enqueue head norms (``q_norm`` / ``k_norm``: weights or None), rotation and append of the new tokens' rows.
+
+    q, k, v: [tokens, heads, head_dim] or [tokens, heads * head_dim], dense or columns of a wider projection; q_out: dense."""
+    n = len(prefix_lens)
+    if len(new_lens) != n:
+        raise ValueError(f"{n} prefix lengths and {len(new_lens)} new lengths")
+    device, strides = _rope_tensors(_params(params), q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, sum(new_lens))
+    _enqueue("mc_kv_rope_append_paged", params, _rope(rope), q, k, v, strides, q_norm, k_norm, q_out, k_pool, v_pool, block_tables,
+             _table(device, block_tables, n), _ints("i", prefix_lens, n), _ints("i", new_lens, n), n, workspace, _nbytes(workspace),
+             _on(stream))
+
+
+def mc_kv_rope_append_run(params: McAttnParams, plan: McAttnPlan, rope: McRopeParams, q, k, v, q_norm, k_norm, q_out, k_pool, v_pool,
+                          block_tables, workspace, stream=None) -> None:
+    """mc_kv_rope_append_paged for a prepared batch."""
+    device, strides = _rope_tensors(_params(params), q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, _plan(plan).total_new_tokens)
+    _enqueue("mc_kv_rope_append_run", params, plan, _rope(rope), q, k, v, strides, q_norm, k_norm, q_out, k_pool, v_pool, block_tables,
+             _table(device, block_tables, plan.batch), workspace, _on(stream))
+
+
+def mc_kv_rope_append_decode(params: McAttnParams, rope: McRopeParams, q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, block_tables,
+                             seq_lens, stream=None) -> None:
+    """The same for one new token a row, at position ``seq_lens[r] - 1``; ``seq_lens``: int32 device tensor."""
+    n = seq_lens.shape[0]
+    device, strides = _rope_tensors(_params(params), q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, n)
+    _dense("seq_lens", device, seq_lens, _torch.int32, n)
+    _enqueue("mc_kv_rope_append_decode", params, _rope(rope), q, k, v, strides, q_norm, k_norm, q_out, k_pool, v_pool, block_tables,
+             _table(device, block_tables, n), seq_lens, n, _on(stream))

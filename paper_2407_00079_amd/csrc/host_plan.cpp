@@ -1020,6 +1020,50 @@ bool kernel_may_reach(uint32_t flags, uintptr_t at, uintptr_t start, size_t size
   return (flags & ~kPlainHostFlags) == 0 && at >= start && at - start <= size && bytes <= size - (at - start);
 }
 
+mc_status check_rope(const mc_attn_params* p, const mc_rope_params* rope, const int64_t* strides) {
+  if (rope == nullptr) return MC_ERR_NULL;
+  if (rope->rotary_dim < 0 || rope->rotary_dim > p->head_dim || rope->rotary_dim % 16 != 0) return MC_ERR_UNSUPPORTED;
+  if (rope->layout != MC_ROPE_HALF && rope->layout != MC_ROPE_PAIRS) return MC_ERR_UNSUPPORTED;
+  if (!(rope->norm_eps >= 0.f) || std::isinf(rope->norm_eps) || !(rope->gain > 0.f) || std::isinf(rope->gain)) return MC_ERR_SHAPE;
+  for (int32_t i = 0; i < rope->rotary_dim / 2; ++i)
+    if (!std::isfinite(rope->inv_freq[i])) return MC_ERR_SHAPE;
+  const int64_t most = INT64_MAX / 4 / INT32_MAX;          // (bytes from token to token times tokens have to fit 64 bits)
+  const int64_t per = p->dtype == MC_DTYPE_BF16 ? 8 : 4;   // elements in 16 bytes
+  for (int i = 0; strides != nullptr && i < 3; ++i) {
+    const int64_t dense = (int64_t)(i == 0 ? p->num_q_heads : p->num_kv_heads) * p->head_dim;
+    if (strides[i] < dense || strides[i] > most) return MC_ERR_SHAPE;
+    if (strides[i] % per != 0) return MC_ERR_ALIGN;
+  }
+  return MC_OK;
+}
+
+mc_status rope_init(mc_rope_params* rope, int32_t rotary_dim, double base, int32_t scaling, double factor, double low, double high,
+                    double original_len) {
+  if (rope == nullptr) return MC_ERR_NULL;
+  if (rotary_dim < 0 || rotary_dim > 2 * MC_ROPE_MAX_PAIRS || rotary_dim % 16 != 0) return MC_ERR_UNSUPPORTED;
+  if (scaling < MC_ROPE_PLAIN || scaling > MC_ROPE_BY_PARTS) return MC_ERR_UNSUPPORTED;
+  auto positive = [](double x) { return std::isfinite(x) && x > 0; };
+  if (!positive(base) || !positive(factor)) return MC_ERR_SHAPE;
+  if (scaling == MC_ROPE_BY_PARTS && (!(low >= 0) || !std::isfinite(high) || !(low < high) || !positive(original_len))) return MC_ERR_SHAPE;
+  const double R = rotary_dim, two_pi = 6.283185307179586476925;
+  if (scaling == MC_ROPE_BASE && rotary_dim > 0) base *= std::pow(factor, R / (R - 2));
+  rope->rotary_dim = rotary_dim;
+  for (int32_t i = 0; i < MC_ROPE_MAX_PAIRS; ++i) {
+    if (i >= rotary_dim / 2) {
+      rope->inv_freq[i] = 0;
+      continue;
+    }
+    double f = std::pow(base, -2.0 * i / R);
+    if (scaling == MC_ROPE_LINEAR) f /= factor;
+    if (scaling == MC_ROPE_BY_PARTS) {
+      const double share = std::min(1.0, std::max(0.0, (original_len * f / two_pi - low) / (high - low)));
+      f *= share + (1 - share) / factor;
+    }
+    rope->inv_freq[i] = f;
+  }
+  return MC_OK;
+}
+
 mc_status check_copy(const void* a, const void* b, int64_t num_pages, int64_t page_bytes, const int32_t* ids,
                      int64_t n, const void* c, const void* d) {
   if (num_pages < 0 || page_bytes < 0 || n < 0) return MC_ERR_SHAPE;

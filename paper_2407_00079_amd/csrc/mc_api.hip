@@ -92,17 +92,22 @@ class StagingRing {
 
 StagingRing g_staging;
 
+// enqueue the upload of `bytes` that lie in a slot acquired for them
+mc_status upload_slot(void* dst, const void* host, int slot, size_t bytes, hipStream_t stream) {
+  if (hipMemcpyAsync(dst, host, bytes, hipMemcpyHostToDevice, stream) != hipSuccess) {
+    g_staging.abandon(slot);
+    return MC_ERR_HIP;
+  }
+  return g_staging.release_after(slot, stream) ? MC_OK : MC_ERR_HIP;
+}
+
 // enqueue the upload of `bytes` of host data to `dst` through a pinned slot
 mc_status upload(void* dst, const void* src, size_t bytes, hipStream_t stream) {
   int slot = -1;
   void* host = g_staging.acquire(bytes, &slot);
   if (host == nullptr) return MC_ERR_HIP;
   std::memcpy(host, src, bytes);
-  if (hipMemcpyAsync(dst, host, bytes, hipMemcpyHostToDevice, stream) != hipSuccess) {
-    g_staging.abandon(slot);
-    return MC_ERR_HIP;
-  }
-  return g_staging.release_after(slot, stream) ? MC_OK : MC_ERR_HIP;
+  return upload_slot(dst, host, slot, bytes, stream);
 }
 
 // Where the device sees `bytes` of host memory that a kernel may reach, or null.
@@ -136,6 +141,57 @@ mc_status host_copy(bool load, const void* k_host, const void* v_host, void* k_s
   *done = true;
   return mc::launch_kv_host(load, k, v, k_stage, v_stage, k_pool, v_pool, page_ids, n, page_bytes, stream) == hipSuccess ? MC_OK
                                                                                                                        : MC_ERR_HIP;
+}
+
+// The request table of an append call: in `arg` if it fits, else uploaded to the workspace (written where the upload takes it from).
+mc_status place_requests(const mc_attn_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, void* workspace,
+                         hipStream_t stream, mc::AttnReqTable* arg) {
+  const bool in_arg = batch <= mc::kMaxArgEntries;
+  const size_t bytes = sizeof(mc::AttnReq) * (size_t)batch;
+  int slot = -1;
+  mc::AttnReq* reqs = in_arg ? arg->r : reinterpret_cast<mc::AttnReq*>(g_staging.acquire(bytes, &slot));
+  if (reqs == nullptr) return MC_ERR_HIP;
+  int64_t q_off = 0;
+  for (int32_t r = 0; r < batch; ++r) {
+    reqs[r] = {(int32_t)q_off, prefix_lens[r], new_lens[r],
+               (int32_t)(((int64_t)prefix_lens[r] + new_lens[r] + p->page_size - 1) / p->page_size)};
+    q_off += new_lens[r];
+  }
+  return in_arg ? MC_OK : upload_slot(workspace, reqs, slot, bytes, stream);
+}
+
+mc_status check_rope_buffers(const mc_attn_params* p, const void* q, const void* k, const void* v, const void* q_norm, const void* k_norm,
+                             const void* q_out, const void* k_pool, const void* v_pool, const int32_t* block_tables,
+                             const int64_t* strides, int64_t tokens) {
+  for (const void* at : {q, k, v, q_out, k_pool, v_pool})
+    if (at == nullptr) return MC_ERR_NULL;
+  if (block_tables == nullptr) return MC_ERR_NULL;
+  for (const void* at : {q, k, v, q_out, k_pool, v_pool, q_norm, k_norm})
+    if (!aligned16(at)) return MC_ERR_ALIGN;
+  if (!aligned4(block_tables)) return MC_ERR_ALIGN;
+  // in place only where a token's rows are read and written at one place
+  if (q == q_out && strides != nullptr && strides[0] != (int64_t)p->num_q_heads * p->head_dim) return MC_ERR_SHAPE;
+  const int64_t rows = p->num_q_heads + 2 * (int64_t)p->num_kv_heads;
+  return rows > INT32_MAX / 2 || tokens * rows / 16 + 1 > INT32_MAX ? MC_ERR_RANGE : MC_OK;     // (a workgroup takes 16 rows at least)
+}
+
+mc::RopeArgs rope_args(const mc_attn_params* p, const mc_rope_params* rope, const void* q, const void* k, const void* v,
+                       const int64_t* strides, const void* q_norm, const void* k_norm, void* q_out, void* k_pool, void* v_pool,
+                       const int32_t* block_tables, int32_t max_pages, int64_t tokens) {
+  mc::RopeArgs a = {};
+  for (int32_t i = 0; i < rope->rotary_dim / 2; ++i) a.turns[i] = rope->inv_freq[i] / 6.283185307179586476925;
+  a.q = q, a.k = k, a.v = v, a.q_norm = q_norm, a.k_norm = k_norm;
+  a.q_out = q_out, a.k_pool = k_pool, a.v_pool = v_pool;
+  a.block_tables = block_tables;
+  const int64_t row = row_bytes_of(p), elem = row / p->head_dim;
+  a.q_stride = strides != nullptr ? strides[0] * elem : p->num_q_heads * row;
+  a.k_stride = strides != nullptr ? strides[1] * elem : p->num_kv_heads * row;
+  a.v_stride = strides != nullptr ? strides[2] * elem : p->num_kv_heads * row;
+  a.total_rows = tokens * ((int64_t)p->num_q_heads + 2 * (int64_t)p->num_kv_heads);
+  a.Hq = p->num_q_heads, a.Hkv = p->num_kv_heads, a.max_pages = max_pages;
+  a.rotary = rope->rotary_dim, a.layout = rope->layout;
+  a.eps = rope->norm_eps, a.gain = rope->gain;
+  return a;
 }
 
 // Two offset tables for a prefix call: in `arg` if they fit, else uploaded to the workspace back to back.
@@ -584,25 +640,106 @@ mc_status mc_kv_append_paged(const mc_attn_params* p, const void* k_new, const v
 
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   mc::AttnReqTable arg = {};
-  std::vector<mc::AttnReq> list;
   const bool in_arg = batch <= mc::kMaxArgEntries;
-  if (!in_arg) list.resize((size_t)batch);
-  mc::AttnReq* reqs = in_arg ? arg.r : list.data();
-  int64_t q_off = 0;
-  for (int32_t r = 0; r < batch; ++r) {
-    reqs[r] = {(int32_t)q_off, prefix_lens[r], new_lens[r],
-               (int32_t)(((int64_t)prefix_lens[r] + new_lens[r] + p->page_size - 1) / p->page_size)};
-    q_off += new_lens[r];
-  }
-  if (!in_arg) {
-    st = upload(workspace, list.data(), sizeof(mc::AttnReq) * list.size(), stream);
-    if (st != MC_OK) return st;
-  }
+  st = place_requests(p, prefix_lens, new_lens, batch, workspace, stream, &arg);
+  if (st != MC_OK) return st;
   if (mc::launch_kv_append(k_new, v_new, k_pool, v_pool, block_tables, max_pages_per_req,
                            reinterpret_cast<const mc::AttnReq*>(workspace), in_arg ? &arg : nullptr, batch, total_new,
                            p->num_kv_heads, row_bytes_of(p), stream) != hipSuccess)
     return MC_ERR_HIP;
   return MC_OK;
+}
+
+mc_status mc_rope_init(mc_rope_params* rope, int32_t rotary_dim, double base, int32_t scaling, double factor, double low,
+                       double high, double original_len) {
+  return rope_init(rope, rotary_dim, base, scaling, factor, low, high, original_len);
+}
+
+mc_status mc_kv_rope_append_paged(const mc_attn_params* p, const mc_rope_params* rope, const void* q, const void* k, const void* v,
+                                  const int64_t* strides, const void* q_norm, const void* k_norm, void* q_out, void* k_pool,
+                                  void* v_pool, const int32_t* block_tables, int32_t max_pages_per_req, const int32_t* prefix_lens,
+                                  const int32_t* new_lens, int32_t batch, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  mc_status st = check_params(p);
+  if (st != MC_OK) return st;
+  st = check_rope(p, rope, strides);
+  if (st != MC_OK) return st;
+  if (batch < 0 || max_pages_per_req < 0) return MC_ERR_SHAPE;
+  if (batch == 0) return MC_OK;
+  if (prefix_lens == nullptr || new_lens == nullptr) return MC_ERR_NULL;
+  int64_t total_new = 0;
+  int32_t need_pages = 0;
+  st = check_lens(p, prefix_lens, new_lens, batch, &total_new, &need_pages);
+  if (st != MC_OK) return st;
+  if (total_new == 0) return MC_OK;
+  if (max_pages_per_req < need_pages) return MC_ERR_SHAPE;
+  st = check_rope_buffers(p, q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, block_tables, strides, total_new);
+  if (st != MC_OK) return st;
+  if (!aligned16(workspace)) return MC_ERR_ALIGN;
+  if (total_new > INT32_MAX || (int64_t)batch * max_pages_per_req > INT32_MAX) return MC_ERR_RANGE;
+  if (workspace == nullptr || workspace_bytes < mc_kv_append_workspace_bytes(batch)) return MC_ERR_WORKSPACE;
+
+  hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+  mc::AttnReqTable arg = {};
+  const bool in_arg = batch <= mc::kMaxArgEntries;
+  st = place_requests(p, prefix_lens, new_lens, batch, workspace, stream, &arg);
+  if (st != MC_OK) return st;
+  const mc::RopeArgs args = rope_args(p, rope, q, k, v, strides, q_norm, k_norm, q_out, k_pool, v_pool, block_tables, max_pages_per_req,
+                                      total_new);
+  return mc::launch_rope_append(p->dtype, p->head_dim, args, reinterpret_cast<const mc::AttnReq*>(workspace), in_arg ? &arg : nullptr,
+                                batch, stream) == hipSuccess
+             ? MC_OK
+             : MC_ERR_HIP;
+}
+
+mc_status mc_kv_rope_append_run(const mc_attn_params* p, const mc_attn_plan* plan, const mc_rope_params* rope, const void* q,
+                                const void* k, const void* v, const int64_t* strides, const void* q_norm, const void* k_norm,
+                                void* q_out, void* k_pool, void* v_pool, const int32_t* block_tables, int32_t max_pages_per_req,
+                                const void* workspace, void* hip_stream) {
+  mc_status st = check_params(p);
+  if (st != MC_OK) return st;
+  if (plan == nullptr) return MC_ERR_NULL;
+  st = check_plan(p, plan, plan->kv_splits > 0);           // either form of plan holds the request table
+  if (st != MC_OK) return st;
+  st = check_rope(p, rope, strides);
+  if (st != MC_OK) return st;
+  if (max_pages_per_req < 0) return MC_ERR_SHAPE;
+  if (plan->n_items == 0) return MC_OK;
+  if (max_pages_per_req < plan->need_pages) return MC_ERR_SHAPE;
+  const int64_t total_new = plan->total_new_tokens;
+  st = check_rope_buffers(p, q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, block_tables, strides, total_new);
+  if (st != MC_OK) return st;
+  if (!aligned16(workspace)) return MC_ERR_ALIGN;
+  if (total_new > INT32_MAX || (int64_t)plan->batch * max_pages_per_req > INT32_MAX) return MC_ERR_RANGE;
+  if (workspace == nullptr) return MC_ERR_WORKSPACE;
+  const mc::RopeArgs args = rope_args(p, rope, q, k, v, strides, q_norm, k_norm, q_out, k_pool, v_pool, block_tables, max_pages_per_req,
+                                      total_new);
+  const char* ws = reinterpret_cast<const char*>(workspace);
+  return mc::launch_rope_append(p->dtype, p->head_dim, args, reinterpret_cast<const mc::AttnReq*>(ws + plan->reqs_offset), nullptr,
+                                plan->batch, reinterpret_cast<hipStream_t>(hip_stream)) == hipSuccess
+             ? MC_OK
+             : MC_ERR_HIP;
+}
+
+mc_status mc_kv_rope_append_decode(const mc_attn_params* p, const mc_rope_params* rope, const void* q, const void* k, const void* v,
+                                   const int64_t* strides, const void* q_norm, const void* k_norm, void* q_out, void* k_pool,
+                                   void* v_pool, const int32_t* block_tables, int32_t max_pages_per_req, const int32_t* seq_lens,
+                                   int32_t batch, void* hip_stream) {
+  mc_status st = check_params(p);
+  if (st != MC_OK) return st;
+  st = check_rope(p, rope, strides);
+  if (st != MC_OK) return st;
+  if (batch < 0 || max_pages_per_req < 0) return MC_ERR_SHAPE;
+  if (batch == 0) return MC_OK;
+  if (seq_lens == nullptr) return MC_ERR_NULL;
+  st = check_rope_buffers(p, q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, block_tables, strides, batch);
+  if (st != MC_OK) return st;
+  if (!aligned4(seq_lens)) return MC_ERR_ALIGN;
+  if ((int64_t)batch * max_pages_per_req > INT32_MAX) return MC_ERR_RANGE;
+  const mc::RopeArgs args = rope_args(p, rope, q, k, v, strides, q_norm, k_norm, q_out, k_pool, v_pool, block_tables, max_pages_per_req,
+                                      batch);
+  return mc::launch_rope_append_tokens(p->dtype, p->head_dim, args, seq_lens, reinterpret_cast<hipStream_t>(hip_stream)) == hipSuccess
+             ? MC_OK
+             : MC_ERR_HIP;
 }
 
 mc_status mc_kv_page_order(const int32_t* page_ids, int64_t n, int32_t* order, void* hip_stream) {

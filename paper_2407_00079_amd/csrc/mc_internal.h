@@ -81,6 +81,23 @@ hipError_t launch_kv_append(const void* k_new, const void* v_new, void* k_pool, 
                             const int32_t* block_tables, int32_t max_pages, const AttnReq* reqs, const AttnReqTable* arg,
                             int32_t batch, int64_t total_new, int32_t Hkv, int32_t row_bytes, hipStream_t stream);
 
+// Rotation and append (rope_append.hip).
+struct RopeArgs {
+  double turns[MC_ROPE_MAX_PAIRS];   // inv_freq / 2 pi
+  const void *q, *k, *v, *q_norm, *k_norm;
+  void *q_out, *k_pool, *v_pool;
+  const int32_t* block_tables;
+  int64_t q_stride, k_stride, v_stride;   // bytes from token to token
+  int64_t total_rows;                // tokens * (Hq + 2 Hkv)
+  int32_t Hq, Hkv, max_pages, rotary, layout;
+  float eps, gain;
+};
+// the request table as launch_kv_append has it
+hipError_t launch_rope_append(int dtype, int head_dim, const RopeArgs& args, const AttnReq* reqs, const AttnReqTable* arg, int32_t batch,
+                              hipStream_t stream);
+// one token a row, lengths in device memory
+hipError_t launch_rope_append_tokens(int dtype, int head_dim, const RopeArgs& args, const int32_t* seq_lens, hipStream_t stream);
+
 // The offset tables of a prefix call: both in device memory or, if `arg` is set, both in it (at most kMaxArgEntries + 1
 // entries each; they then travel with the launch).
 struct PrefixTables {
