@@ -413,6 +413,31 @@ mc_status mc_kv_rope_append_decode(const mc_attn_params* p, const mc_rope_params
                                    int32_t batch, void* hip_stream);
 
 /*
+ * Attention of one new token a row over the paged cache: what a decode step reads.  The lengths stand in DEVICE memory, so a
+ * captured step can be replayed while they grow; there is no host plan.
+ *
+ *   out[r,h,:] = sum_{j < len_r} softmax_j(scale * q[r,h,:] . K(j)) * V(j)
+ *   lse[r,h]   = log sum_{j < len_r} exp(scale * q[r,h,:] . K(j))          (natural log)
+ *
+ *   q            dev  [batch, Hq, D]
+ *   k_pool, v_pool, block_tables  as in mc_prefill_attn_paged; the new token's K and V are in their slots
+ *   seq_lens     dev  int32 [batch]: keys the row sees, its new token included.  A length that is not in
+ *                     [1, max_pages_per_req * 16] is a padding row's: out = 0, lse = -inf
+ *   out          dev  [batch, Hq, D] of p->dtype, every row written
+ *   lse          dev  [batch, Hq] fp32, or NULL
+ *   workspace    dev  >= mc_decode_attn_workspace_bytes(...) (the same for every batch and length), 16-byte aligned; calls that
+ *                     may overlap, and captured graphs that may, need one each
+ *
+ * Slots at or past a row's length are never used as values (they may hold NaN).  fp32 accumulation and softmax; output rounded
+ * once, to nearest even.  The same lengths and inputs give the same bits.  batch * Hq > 2^26 is MC_ERR_RANGE; batch == 0 enqueues
+ * nothing.  Nothing is allocated, uploaded or waited for; the call can be captured.
+ */
+size_t mc_decode_attn_workspace_bytes(const mc_attn_params* p, int32_t batch);
+mc_status mc_decode_attn_paged(const mc_attn_params* p, const void* q, const void* k_pool, const void* v_pool,
+                               const int32_t* block_tables, int32_t max_pages_per_req, const int32_t* seq_lens, int32_t batch,
+                               void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * Store path of layer-wise prefill (Section 5.2): gather pages of one layer's
  * scattered pools into contiguous buffers, page i of the output = page
  * page_ids[i] of the pool, bytes verbatim.

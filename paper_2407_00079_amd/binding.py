@@ -28,7 +28,7 @@ EXPORTS = ("mc_status_string", "mc_prefill_attn_workspace_bytes", "mc_prefill_at
            "mc_prefill_attn_plan", "mc_prefill_attn_prepare", "mc_prefill_attn_run", "mc_prefill_attn_run_split",
            "mc_kv_append_run", "mc_prefill_attn_auto_workspace_bytes", "mc_prefill_attn_auto",
            "mc_prefill_attn_paged_noalloc", "mc_rope_init", "mc_kv_rope_append_paged", "mc_kv_rope_append_run",
-           "mc_kv_rope_append_decode")
+           "mc_kv_rope_append_decode", "mc_decode_attn_workspace_bytes", "mc_decode_attn_paged")
 MC_ROPE_HALF, MC_ROPE_PAIRS = 0, 1
 MC_ROPE_PLAIN, MC_ROPE_LINEAR, MC_ROPE_BASE, MC_ROPE_BY_PARTS = 0, 1, 2, 3
 MC_MAX_KV_SPLITS = 256
@@ -143,6 +143,10 @@ def lib():
         l.mc_kv_rope_append_run.argtypes = [pp, pl_, rp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp]
         l.mc_kv_rope_append_decode.restype = ctypes.c_int
         l.mc_kv_rope_append_decode.argtypes = [pp, rp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, vp]
+        l.mc_decode_attn_workspace_bytes.restype = ctypes.c_size_t
+        l.mc_decode_attn_workspace_bytes.argtypes = [pp, i32]
+        l.mc_decode_attn_paged.restype = ctypes.c_int
+        l.mc_decode_attn_paged.argtypes = [pp, vp, vp, vp, vp, i32, vp, i32, vp, vp, vp, ctypes.c_size_t, vp]
         try:
             from . import _mccall
         except ModuleNotFoundError:                        # none was built for this Python
@@ -195,6 +199,7 @@ _CACHE_KINDS = {
     "mc_kv_rope_append_paged": "sspppsppppppiIIipii",
     "mc_kv_rope_append_run": "ssspppsppppppipi",
     "mc_kv_rope_append_decode": "sspppsppppppipii",
+    "mc_decode_attn_paged": "sppppipipppii",
 }
 _ALL_KINDS = {**_KINDS, **_CACHE_KINDS}
 
@@ -698,3 +703,22 @@ def mc_kv_rope_append_decode(params: McAttnParams, rope: McRopeParams, q, k, v, 
     _dense("seq_lens", device, seq_lens, _torch.int32, n)
     _enqueue("mc_kv_rope_append_decode", params, _rope(rope), q, k, v, strides, q_norm, k_norm, q_out, k_pool, v_pool, block_tables,
              _table(device, block_tables, n), seq_lens, n, _on(stream))
+
+
+def mc_decode_attn_workspace_bytes(params: McAttnParams, batch: int) -> int:
+    return int(lib().mc_decode_attn_workspace_bytes(ctypes.byref(params), batch))
+
+
+def mc_decode_attn_paged(params: McAttnParams, q, k_pool, v_pool, block_tables, seq_lens, out, lse, workspace, stream=None) -> None:
+    """Enqueue attention of one new token a row: q, out [rows, heads, head_dim], ``seq_lens`` int32 device tensor [rows]."""
+    dtype = _dtypes()[_params(params).dtype]
+    n, heads = seq_lens.shape[0], params.num_q_heads
+    device, size = q.get_device(), n * heads * params.head_dim
+    _dense("q", device, q, dtype, size)
+    _pools(params, device, dtype, k_pool, v_pool)
+    _dense("seq_lens", device, seq_lens, _torch.int32, n)
+    _dense("out", device, out, dtype, size)
+    if lse is not None:
+        _dense("lse", device, lse, _torch.float32, n * heads)
+    _enqueue("mc_decode_attn_paged", params, q, k_pool, v_pool, block_tables, _table(device, block_tables, n), seq_lens, n, out, lse,
+             workspace, _nbytes(workspace), _on(stream))

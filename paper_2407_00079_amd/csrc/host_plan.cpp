@@ -1020,6 +1020,15 @@ bool kernel_may_reach(uint32_t flags, uintptr_t at, uintptr_t start, size_t size
   return (flags & ~kPlainHostFlags) == 0 && at >= start && at - start <= size && bytes <= size - (at - start);
 }
 
+DecodeLayout decode_layout(const mc_attn_params* p) {
+  const size_t rows = (size_t)kDecodeWgs * 2 * kDecodeRows;
+  DecodeLayout lay;
+  lay.ml_off = rows * p->head_dim * sizeof(float);
+  lay.meta_off = lay.ml_off + rows * 2 * sizeof(float);
+  lay.total = lay.meta_off + kDecodeWgs * sizeof(DecodeMeta);
+  return lay;
+}
+
 mc_status check_rope(const mc_attn_params* p, const mc_rope_params* rope, const int64_t* strides) {
   if (rope == nullptr) return MC_ERR_NULL;
   if (rope->rotary_dim < 0 || rope->rotary_dim > p->head_dim || rope->rotary_dim % 16 != 0) return MC_ERR_UNSUPPORTED;

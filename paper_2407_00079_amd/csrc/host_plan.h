@@ -169,6 +169,12 @@ bool auto_layout(const mc_attn_params* p, const int32_t* prefix_lens, const int3
 bool hash_in_one_launch(int64_t max_blocks, int64_t max_tokens);
 
 // arguments of a page copy (pack / unpack and their relatives): a, b source pair, c, d destination pair
+// Where the parts of a decode call lie in its workspace.
+struct DecodeLayout {
+  size_t ml_off, meta_off, total;
+};
+DecodeLayout decode_layout(const mc_attn_params* p);
+
 // Head norms, rotation and strides (elements; null: dense) of a call that takes rows of Q, K and V.
 mc_status check_rope(const mc_attn_params* p, const mc_rope_params* rope, const int64_t* strides);
 // Frequencies as mc_rope_init has them.

@@ -742,6 +742,47 @@ mc_status mc_kv_rope_append_decode(const mc_attn_params* p, const mc_rope_params
              : MC_ERR_HIP;
 }
 
+size_t mc_decode_attn_workspace_bytes(const mc_attn_params* p, int32_t batch) {
+  if (check_params(p) != MC_OK || batch < 0) return 0;
+  return decode_layout(p).total;
+}
+
+mc_status mc_decode_attn_paged(const mc_attn_params* p, const void* q, const void* k_pool, const void* v_pool,
+                               const int32_t* block_tables, int32_t max_pages_per_req, const int32_t* seq_lens, int32_t batch,
+                               void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  mc_status st = check_params(p);
+  if (st != MC_OK) return st;
+  if (batch < 0 || max_pages_per_req < 0) return MC_ERR_SHAPE;
+  if (batch == 0) return MC_OK;
+  if (seq_lens == nullptr) return MC_ERR_NULL;
+  st = check_attn_buffers(false, q, k_pool, v_pool, block_tables, batch, max_pages_per_req, 0, out, lse, nullptr, nullptr, workspace);
+  if (st != MC_OK) return st;
+  if (!aligned4(seq_lens)) return MC_ERR_ALIGN;
+  if ((int64_t)batch * p->num_q_heads > 1 << 26) return MC_ERR_RANGE;
+  const DecodeLayout lay = decode_layout(p);
+  if (workspace == nullptr || workspace_bytes < lay.total) return MC_ERR_WORKSPACE;
+  char* ws = reinterpret_cast<char*>(workspace);
+  mc::DecodeArgs args = {};
+  args.q = q;
+  args.k_pool = k_pool;
+  args.v_pool = v_pool;
+  args.block_tables = block_tables;
+  args.seq_lens = seq_lens;
+  args.out = out;
+  args.lse = lse;
+  args.o_parts = reinterpret_cast<float*>(ws);
+  args.ml_parts = reinterpret_cast<float2*>(ws + lay.ml_off);
+  args.meta = reinterpret_cast<mc::DecodeMeta*>(ws + lay.meta_off);
+  args.Hq = p->num_q_heads;
+  args.Hkv = p->num_kv_heads;
+  args.G = p->num_q_heads / p->num_kv_heads;
+  args.tiles = (args.G + mc::kDecodeRows - 1) / mc::kDecodeRows;
+  args.batch = batch;
+  args.max_pages = max_pages_per_req;
+  args.scale_log2e = attn_scale_log2e(p);
+  return mc::launch_attn_decode(p->dtype, p->head_dim, args, reinterpret_cast<hipStream_t>(hip_stream)) == hipSuccess ? MC_OK : MC_ERR_HIP;
+}
+
 mc_status mc_kv_page_order(const int32_t* page_ids, int64_t n, int32_t* order, void* hip_stream) {
   if (n < 0) return MC_ERR_SHAPE;
   if (n == 0) return MC_OK;

@@ -98,6 +98,20 @@ hipError_t launch_rope_append(int dtype, int head_dim, const RopeArgs& args, con
 // one token a row, lengths in device memory
 hipError_t launch_rope_append_tokens(int dtype, int head_dim, const RopeArgs& args, const int32_t* seq_lens, hipStream_t stream);
 
+// Decode attention (attn_decode.hip).
+struct DecodeArgs {
+  const void *q, *k_pool, *v_pool;
+  const int32_t *block_tables, *seq_lens;
+  void* out;
+  float* lse;
+  float* o_parts;      // [kDecodeWgs][2][kDecodeRows][D]: what a workgroup has of a row that began before it, of one that goes on
+  float2* ml_parts;    // their references and sums
+  DecodeMeta* meta;    // [kDecodeWgs]
+  int32_t Hq, Hkv, G, tiles, batch, max_pages;
+  float scale_log2e;
+};
+hipError_t launch_attn_decode(int dtype, int head_dim, const DecodeArgs& args, hipStream_t stream);
+
 // The offset tables of a prefix call: both in device memory or, if `arg` is set, both in it (at most kMaxArgEntries + 1
 // entries each; they then travel with the launch).
 struct PrefixTables {

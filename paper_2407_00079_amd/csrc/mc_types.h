@@ -84,4 +84,21 @@ constexpr int64_t kMostHostSlices = 512;
 // the work list is kept in this many lists, one per XCD of the chip
 constexpr int kXcds = 8;
 
+// Decode attention (attn_decode.hip): `total` blocks of keys in one line, shared out over waves in equal stretches.  The first
+// sizes of all are chosen so that nothing overflows: lengths below 2^31 (2^26 blocks), batch x heads below 2^31, waves 2^11 give
+// total x waves below 2^63 where batch x heads stays below 2^26 (the front end refuses more).
+constexpr int kDecodeWgs = 256;              // one a compute unit
+constexpr int kDecodeRows = 16;              // query heads of a tile
+constexpr int kDecodeBlockKeys = 32;
+struct DecodeMeta {
+  int32_t more;                              // workgroups behind this one that have parts of the row that goes on; 0: none does
+  int32_t row, head, tile;
+};
+// how many waves have work
+constexpr int decode_waves(int64_t total, int all) { return total < all ? (int)total : all; }
+// where wave w's stretch begins
+constexpr int64_t decode_begin(int64_t total, int w, int waves) { return total * w / waves; }
+// the wave that has place x of the line
+constexpr int decode_wave_of(int64_t total, int64_t x, int waves) { return (int)(((x + 1) * waves - 1) / total); }
+
 }  // namespace mc
