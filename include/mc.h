@@ -438,6 +438,92 @@ mc_status mc_decode_attn_paged(const mc_attn_params* p, const void* q, const voi
                                void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
+ * The care of a cache's pages on the device.  The state, all of it in device memory and shared by the layers:
+ *
+ *   ref_counts    int32 [num_pages]                 how many table entries name the page; 0: the page is free
+ *   block_tables  int32 [rows, max_pages_per_req]   a row's entries 0 .. ceil(len / page_size) - 1 are its pages
+ *   seq_lens      int32 [rows]                      tokens of the row; 0: the row is empty
+ *   report        int32 [4]                         what the call did: { pages, flags, free pages, pages wanted }, as said below
+ *
+ * Pages are given out lowest first, so the same state gives the same tables.  Calls on one state are ordered by the caller (one
+ * stream, or events).  A row, length or page id that is not valid is never followed; the flags say so:
+ */
+#define MC_PAGES_SHORT 1    /* fewer free pages than wanted: nothing was changed */
+#define MC_PAGES_BAD_ROW 2  /* a row or length that the call cannot take; fork and grow changed nothing then */
+#define MC_PAGES_BAD_ID 4   /* a table entry outside the pool, or (free) of a page that was free already: left as it was */
+/* Workspace of fork, grow (rows: the table's) and compact (rows 0); 0 for arguments they would refuse. */
+size_t mc_kv_pages_workspace_bytes(int64_t num_pages, int32_t rows);
+
+/*
+ * Row dst_rows[i] becomes a copy of row src_rows[i], n of them (several may copy one row): full pages are shared (their counts go
+ * up), a partly filled last page gets a page of its own, the lowest free one in list order, and a move
+ * { the source's page, the new page } whose data mc_kv_copy_pages copies.
+ *
+ *   src_rows, dst_rows  dev  int32 [n], n <= rows; a dst row has to be empty and to be listed once (else MC_PAGES_BAD_ROW)
+ *   moves               dev  int32 [n][2]: report[0] moves, the rest { -1, -1 }
+ *   report              { moves, flags, free pages left, pages wanted }; where flags has SHORT or BAD_ROW nothing was changed, no move
+ *   n == 0 enqueues nothing.
+ */
+mc_status mc_kv_pages_fork(int32_t* ref_counts, int64_t num_pages, int32_t* block_tables, int32_t max_pages_per_req, int32_t page_size,
+                           int32_t* seq_lens, int32_t rows, const int32_t* src_rows, const int32_t* dst_rows, int32_t n, int32_t* moves,
+                           int32_t* report, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Row r gets add[r] more tokens (none where add[r] <= 0): its length grows, and the pages that takes are the lowest free ones in row
+ * order.  All or nothing: a row that would outgrow its table (or whose length is not valid) is MC_PAGES_BAD_ROW.
+ *
+ *   add     dev  int32 [rows]
+ *   report  { pages given, flags, free pages left, pages wanted }
+ */
+mc_status mc_kv_pages_grow(int32_t* ref_counts, int64_t num_pages, int32_t* block_tables, int32_t max_pages_per_req, int32_t page_size,
+                           int32_t* seq_lens, int32_t rows, const int32_t* add, int32_t* report, void* workspace, size_t workspace_bytes,
+                           void* hip_stream);
+
+/*
+ * The listed rows become empty and their pages' counts go down; a row listed twice, or empty, is freed once, or not at all.  Their
+ * table entries stay as they are.
+ *
+ *   free_rows  dev  int32 [n]; a row outside the table is passed over (MC_PAGES_BAD_ROW), as is a length that is not valid
+ *   report     { pages that became free, flags, 0, 0 }
+ */
+mc_status mc_kv_pages_free(int32_t* ref_counts, int64_t num_pages, const int32_t* block_tables, int32_t max_pages_per_req,
+                           int32_t page_size, int32_t* seq_lens, int32_t rows, const int32_t* free_rows, int32_t n, int32_t* report,
+                           void* hip_stream);
+
+/*
+ * The moves that bring the L live pages to the front of the pool: the k-th live page at or past L goes to the k-th free page before
+ * L.  Changes nothing but moves and report; mc_kv_copy_pages moves the data and mc_kv_pages_remap the tables and counts.
+ *
+ *   max_moves  at most so many moves are listed, the lowest sources first (a bounded step: later calls go on)
+ *   moves      dev  int32 [max_moves][2]: { source, destination } by ascending source, then { -1, -1 }
+ *   report     { moves listed, 0, free pages, moves it takes in all }
+ */
+mc_status mc_kv_pages_compact(const int32_t* ref_counts, int64_t num_pages, int32_t max_moves, int32_t* moves, int32_t* report,
+                              void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Tables and counts follow moves: entries that name a move's source name its destination afterwards, which takes over the count.
+ *
+ *   moves  dev  int32 [n][2], sources ascending, as mc_kv_pages_compact lists them (no page may be in two moves)
+ *   count  dev  int32: how many of the n are moves (report of the call that listed them), or NULL: all
+ */
+mc_status mc_kv_pages_remap(int32_t* ref_counts, int64_t num_pages, int32_t* block_tables, int32_t max_pages_per_req, int32_t page_size,
+                            const int32_t* seq_lens, int32_t rows, const int32_t* moves, const int32_t* count, int32_t n,
+                            void* hip_stream);
+
+/*
+ * The pages of all layers' pools by a list of moves: page moves[i][1] of every pool becomes a copy of its page moves[i][0], bytes
+ * verbatim.  A move with a page outside the pool is passed over.  A page that is the destination of one move may not be in another.
+ *
+ *   k_pools, v_pools  HOST  [n_layers] device addresses of num_pages * page_bytes each, 16-byte aligned
+ *   moves, count      as in mc_kv_pages_remap, in any order
+ * n_layers > MC_MAX_COPY_LAYERS is MC_ERR_RANGE; page_bytes has to be a multiple of 16.
+ */
+#define MC_MAX_COPY_LAYERS 128
+mc_status mc_kv_copy_pages(void* const* k_pools, void* const* v_pools, int32_t n_layers, int64_t num_pages, int64_t page_bytes,
+                           const int32_t* moves, const int32_t* count, int32_t n, void* hip_stream);
+
+/*
  * Store path of layer-wise prefill (Section 5.2): gather pages of one layer's
  * scattered pools into contiguous buffers, page i of the output = page
  * page_ids[i] of the pool, bytes verbatim.

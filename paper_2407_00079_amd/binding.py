@@ -28,7 +28,11 @@ EXPORTS = ("mc_status_string", "mc_prefill_attn_workspace_bytes", "mc_prefill_at
            "mc_prefill_attn_plan", "mc_prefill_attn_prepare", "mc_prefill_attn_run", "mc_prefill_attn_run_split",
            "mc_kv_append_run", "mc_prefill_attn_auto_workspace_bytes", "mc_prefill_attn_auto",
            "mc_prefill_attn_paged_noalloc", "mc_rope_init", "mc_kv_rope_append_paged", "mc_kv_rope_append_run",
-           "mc_kv_rope_append_decode", "mc_decode_attn_workspace_bytes", "mc_decode_attn_paged")
+           "mc_kv_rope_append_decode", "mc_decode_attn_workspace_bytes", "mc_decode_attn_paged",
+           "mc_kv_pages_workspace_bytes", "mc_kv_pages_fork", "mc_kv_pages_grow", "mc_kv_pages_free", "mc_kv_pages_compact",
+           "mc_kv_pages_remap", "mc_kv_copy_pages")
+MC_PAGES_SHORT, MC_PAGES_BAD_ROW, MC_PAGES_BAD_ID = 1, 2, 4
+MC_MAX_COPY_LAYERS = 128
 MC_ROPE_HALF, MC_ROPE_PAIRS = 0, 1
 MC_ROPE_PLAIN, MC_ROPE_LINEAR, MC_ROPE_BASE, MC_ROPE_BY_PARTS = 0, 1, 2, 3
 MC_MAX_KV_SPLITS = 256
@@ -147,6 +151,18 @@ def lib():
         l.mc_decode_attn_workspace_bytes.argtypes = [pp, i32]
         l.mc_decode_attn_paged.restype = ctypes.c_int
         l.mc_decode_attn_paged.argtypes = [pp, vp, vp, vp, vp, i32, vp, i32, vp, vp, vp, ctypes.c_size_t, vp]
+        sz = ctypes.c_size_t
+        l.mc_kv_pages_workspace_bytes.restype = sz
+        l.mc_kv_pages_workspace_bytes.argtypes = [i64, i32]
+        state = [vp, i64, vp, i32, i32, vp, i32]           # counts, pages, tables, their columns, page size, lengths, rows
+        for f, more in ((l.mc_kv_pages_fork, [vp, vp, i32, vp, vp, vp, sz]), (l.mc_kv_pages_grow, [vp, vp, vp, sz]),
+                        (l.mc_kv_pages_free, [vp, i32, vp]), (l.mc_kv_pages_remap, [vp, vp, i32])):
+            f.restype = ctypes.c_int
+            f.argtypes = [*state, *more, vp]
+        l.mc_kv_pages_compact.restype = ctypes.c_int
+        l.mc_kv_pages_compact.argtypes = [vp, i64, i32, vp, vp, vp, sz, vp]
+        l.mc_kv_copy_pages.restype = ctypes.c_int
+        l.mc_kv_copy_pages.argtypes = [vp, vp, i32, i64, i64, vp, vp, i32, vp]
         try:
             from . import _mccall
         except ModuleNotFoundError:                        # none was built for this Python
@@ -200,6 +216,12 @@ _CACHE_KINDS = {
     "mc_kv_rope_append_run": "ssspppsppppppipi",
     "mc_kv_rope_append_decode": "sspppsppppppipii",
     "mc_decode_attn_paged": "sppppipipppii",
+    "mc_kv_pages_fork": "pipiipippipppii",
+    "mc_kv_pages_grow": "pipiipipppii",
+    "mc_kv_pages_free": "pipiipipipi",
+    "mc_kv_pages_compact": "piipppii",
+    "mc_kv_pages_remap": "pipiipippii",
+    "mc_kv_copy_pages": "QQiiippii",
 }
 _ALL_KINDS = {**_KINDS, **_CACHE_KINDS}
 
@@ -722,3 +744,86 @@ def mc_decode_attn_paged(params: McAttnParams, q, k_pool, v_pool, block_tables, 
         _dense("lse", device, lse, _torch.float32, n * heads)
     _enqueue("mc_decode_attn_paged", params, q, k_pool, v_pool, block_tables, _table(device, block_tables, n), seq_lens, n, out, lse,
              workspace, _nbytes(workspace), _on(stream))
+
+
+def mc_kv_pages_workspace_bytes(num_pages: int, rows: int) -> int:
+    return int(lib().mc_kv_pages_workspace_bytes(num_pages, rows))
+
+
+def _state(ref_counts, block_tables, page_size: int, seq_lens):
+    """Looks a cache's bookkeeping over: (device, the seven arguments that stand for it)."""
+    _dtypes()
+    i32, device, rows = _torch.int32, ref_counts.get_device(), seq_lens.shape[0]
+    _dense("ref_counts", device, ref_counts, i32, 0)
+    _dense("seq_lens", device, seq_lens, i32, rows)
+    wide = _table(device, block_tables, rows)
+    return device, (ref_counts, ref_counts.shape[0], block_tables, wide, page_size, seq_lens, rows)
+
+
+def mc_kv_pages_fork(ref_counts, block_tables, page_size: int, seq_lens, src_rows, dst_rows, moves, report, workspace, stream=None) -> None:
+    """Enqueue rows ``dst_rows`` becoming copies of ``src_rows``; all int32 device tensors, ``moves`` [n, 2], ``report`` [4]."""
+    device, state = _state(ref_counts, block_tables, page_size, seq_lens)
+    n, i32 = src_rows.shape[0], _torch.int32
+    _dense("src_rows", device, src_rows, i32, n)
+    _dense("dst_rows", device, dst_rows, i32, n)
+    _dense("moves", device, moves, i32, 2 * n)
+    _dense("report", device, report, i32, 4)
+    _enqueue("mc_kv_pages_fork", *state, src_rows, dst_rows, n, moves, report, workspace, _nbytes(workspace), _on(stream))
+
+
+def mc_kv_pages_grow(ref_counts, block_tables, page_size: int, seq_lens, add, report, workspace, stream=None) -> None:
+    """Enqueue row r getting ``add[r]`` more tokens, and the pages that takes."""
+    device, state = _state(ref_counts, block_tables, page_size, seq_lens)
+    _dense("add", device, add, _torch.int32, state[-1])
+    _dense("report", device, report, _torch.int32, 4)
+    _enqueue("mc_kv_pages_grow", *state, add, report, workspace, _nbytes(workspace), _on(stream))
+
+
+def mc_kv_pages_free(ref_counts, block_tables, page_size: int, seq_lens, free_rows, report, stream=None) -> None:
+    """Enqueue the listed rows becoming empty."""
+    device, state = _state(ref_counts, block_tables, page_size, seq_lens)
+    n = free_rows.shape[0]
+    _dense("free_rows", device, free_rows, _torch.int32, n)
+    _dense("report", device, report, _torch.int32, 4)
+    _enqueue("mc_kv_pages_free", *state, free_rows, n, report, _on(stream))
+
+
+def mc_kv_pages_compact(ref_counts, moves, report, workspace, stream=None) -> None:
+    """Enqueue the list of at most ``moves.shape[0]`` moves that bring live pages to the front of the pool."""
+    _dtypes()
+    device, n = ref_counts.get_device(), moves.shape[0]
+    _dense("ref_counts", device, ref_counts, _torch.int32, 0)
+    _dense("moves", device, moves, _torch.int32, 2 * n)
+    _dense("report", device, report, _torch.int32, 4)
+    _enqueue("mc_kv_pages_compact", ref_counts, ref_counts.shape[0], n, moves, report, workspace, _nbytes(workspace), _on(stream))
+
+
+def _moves(device: int, moves, count) -> int:
+    n = moves.shape[0]
+    _dense("moves", device, moves, _torch.int32, 2 * n)
+    if count is not None:
+        _dense("count", device, count, _torch.int32, 1)
+    return n
+
+
+def mc_kv_pages_remap(ref_counts, block_tables, page_size: int, seq_lens, moves, count=None, stream=None) -> None:
+    """Enqueue tables and counts following ``moves`` [n, 2], of which ``count[0]`` are moves (None: all)."""
+    device, state = _state(ref_counts, block_tables, page_size, seq_lens)
+    n = _moves(device, moves, count)
+    _enqueue("mc_kv_pages_remap", *state, moves, count, n, _on(stream))
+
+
+def mc_kv_copy_pages(k_pools, v_pools, num_pages: int, page_bytes: int, moves, count=None, stream=None) -> None:
+    """Enqueue the copy of the moved pages in every layer: lists of device tensors of num_pages * page_bytes bytes."""
+    _dtypes()
+    if len(k_pools) != len(v_pools):
+        raise ValueError(f"{len(k_pools)} K pools and {len(v_pools)} V pools")
+    device = moves.get_device()
+    n = _moves(device, moves, count)
+    for pool in (*k_pools, *v_pools):
+        if pool.get_device() != device or not pool.is_contiguous() or pool.nbytes < num_pages * page_bytes:
+            raise ValueError(f"pools: {num_pages * page_bytes} dense bytes on device {device} wanted, not {pool.dtype} {tuple(pool.shape)} "
+                             f"strides {pool.stride()} on {pool.device}")
+    layers = len(k_pools)
+    _enqueue("mc_kv_copy_pages", _ints("q", [t.data_ptr() for t in k_pools], layers), _ints("q", [t.data_ptr() for t in v_pools], layers),
+             layers, num_pages, page_bytes, moves, count, n, _on(stream))

@@ -19,7 +19,7 @@ LIB = os.path.join(PKG, "libmooncake_hip.so")
 CALLER = os.path.join(PKG, "_mccall" + sysconfig.get_config_var("EXT_SUFFIX"))
 # host_plan.cpp holds no device code: hipcc compiles it as plain C++
 SOURCES = ["mc_api.hip", "host_plan.cpp", "attn_prefill.hip", "attn_prefill_bf16.hip", "attn_narrow.hip", "attn_decode.hip", "attn_noalloc.hip", "kv_copy.hip",
-           "prefix_hash.hip", "rope_append.hip"]
+           "prefix_hash.hip", "rope_append.hip", "kv_pages.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed-fp32 VALU forms are switched off on purpose (device code only)

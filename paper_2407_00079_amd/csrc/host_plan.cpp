@@ -1029,6 +1029,29 @@ DecodeLayout decode_layout(const mc_attn_params* p) {
   return lay;
 }
 
+mc_status check_pages(const int32_t* ref_counts, int64_t num_pages, const int32_t* block_tables, int32_t max_pages_per_req,
+                      int32_t page_size, const int32_t* seq_lens, int32_t rows) {
+  if (num_pages <= 0 || rows < 0 || max_pages_per_req < 0 || page_size <= 0) return MC_ERR_SHAPE;
+  // (twice the pages, and a table's tokens, have to fit 32 bits)
+  if (num_pages > INT32_MAX / 2 || (int64_t)rows * max_pages_per_req > INT32_MAX || (int64_t)max_pages_per_req * page_size > INT32_MAX / 2)
+    return MC_ERR_RANGE;
+  if (rows == 0) return MC_OK;
+  if (ref_counts == nullptr || block_tables == nullptr || seq_lens == nullptr) return MC_ERR_NULL;
+  if (!aligned4(ref_counts) || !aligned4(block_tables) || !aligned4(seq_lens)) return MC_ERR_ALIGN;
+  return MC_OK;
+}
+
+PagesLayout pages_layout(int64_t num_pages, int32_t rows) {
+  const size_t chunks = (size_t)((num_pages + kPagesChunk - 1) / kPagesChunk), n = (size_t)rows;
+  PagesLayout lay;
+  lay.wanted_off = 4 * chunks;
+  lay.lens_off = lay.wanted_off + 4 * n;
+  lay.claims_off = lay.lens_off + 4 * n;
+  lay.head_off = lay.claims_off + 4 * n;
+  lay.total = lay.head_off + sizeof(PagesHead);
+  return lay;
+}
+
 mc_status check_rope(const mc_attn_params* p, const mc_rope_params* rope, const int64_t* strides) {
   if (rope == nullptr) return MC_ERR_NULL;
   if (rope->rotary_dim < 0 || rope->rotary_dim > p->head_dim || rope->rotary_dim % 16 != 0) return MC_ERR_UNSUPPORTED;

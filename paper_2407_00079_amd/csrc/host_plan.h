@@ -175,6 +175,15 @@ struct DecodeLayout {
 };
 DecodeLayout decode_layout(const mc_attn_params* p);
 
+// Sizes and addresses of a call on a cache's pages.
+mc_status check_pages(const int32_t* ref_counts, int64_t num_pages, const int32_t* block_tables, int32_t max_pages_per_req,
+                      int32_t page_size, const int32_t* seq_lens, int32_t rows);
+// Where such a call's arrays lie in its workspace; n: rows and entries of a list at most.
+struct PagesLayout {
+  size_t wanted_off, lens_off, claims_off, head_off, total;
+};
+PagesLayout pages_layout(int64_t num_pages, int32_t rows);
+
 // Head norms, rotation and strides (elements; null: dense) of a call that takes rows of Q, K and V.
 mc_status check_rope(const mc_attn_params* p, const mc_rope_params* rope, const int64_t* strides);
 // Frequencies as mc_rope_init has them.

@@ -194,6 +194,25 @@ mc::RopeArgs rope_args(const mc_attn_params* p, const mc_rope_params* rope, cons
   return a;
 }
 
+// A call's arguments for the page kernels, its workspace arrays laid out.
+mc::PagesArgs pages_args(int32_t* ref_counts, int64_t num_pages, int32_t* block_tables, int32_t max_pages, int32_t page_size,
+                         int32_t* seq_lens, int32_t rows, int32_t n, int32_t* report, void* workspace) {
+  mc::PagesArgs a = {};
+  a.ref_counts = ref_counts, a.block_tables = block_tables, a.seq_lens = seq_lens, a.report = report;
+  a.num_pages = num_pages;
+  a.max_pages = max_pages, a.page_size = page_size, a.rows = rows, a.n = n;
+  a.chunks = (int32_t)((num_pages + mc::kPagesChunk - 1) / mc::kPagesChunk);
+  if (workspace == nullptr) return a;
+  const PagesLayout lay = pages_layout(num_pages, rows);
+  char* ws = reinterpret_cast<char*>(workspace);
+  a.free_before = reinterpret_cast<int32_t*>(ws);
+  a.wanted_before = reinterpret_cast<int32_t*>(ws + lay.wanted_off);
+  a.lens = reinterpret_cast<int32_t*>(ws + lay.lens_off);
+  a.claims = reinterpret_cast<int32_t*>(ws + lay.claims_off);
+  a.head = reinterpret_cast<mc::PagesHead*>(ws + lay.head_off);
+  return a;
+}
+
 // Two offset tables for a prefix call: in `arg` if they fit, else uploaded to the workspace back to back.
 mc_status place_tables(const int64_t* a, size_t n_a, const int64_t* b, size_t n_b, void* workspace, hipStream_t stream,
                        mc::OffsetTables* arg, mc::PrefixTables* out) {
@@ -781,6 +800,103 @@ mc_status mc_decode_attn_paged(const mc_attn_params* p, const void* q, const voi
   args.max_pages = max_pages_per_req;
   args.scale_log2e = attn_scale_log2e(p);
   return mc::launch_attn_decode(p->dtype, p->head_dim, args, reinterpret_cast<hipStream_t>(hip_stream)) == hipSuccess ? MC_OK : MC_ERR_HIP;
+}
+
+size_t mc_kv_pages_workspace_bytes(int64_t num_pages, int32_t rows) {
+  return num_pages <= 0 || num_pages > INT32_MAX / 2 || rows < 0 ? 0 : pages_layout(num_pages, rows).total;
+}
+
+mc_status mc_kv_pages_fork(int32_t* ref_counts, int64_t num_pages, int32_t* block_tables, int32_t max_pages_per_req, int32_t page_size,
+                           int32_t* seq_lens, int32_t rows, const int32_t* src_rows, const int32_t* dst_rows, int32_t n, int32_t* moves,
+                           int32_t* report, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const mc_status st = check_pages(ref_counts, num_pages, block_tables, max_pages_per_req, page_size, seq_lens, rows);
+  if (st != MC_OK) return st;
+  if (n < 0 || n > rows) return MC_ERR_SHAPE;
+  if (n == 0) return MC_OK;
+  if (src_rows == nullptr || dst_rows == nullptr || moves == nullptr || report == nullptr) return MC_ERR_NULL;
+  if (!aligned4(src_rows) || !aligned4(dst_rows) || !aligned4(moves) || !aligned4(report) || !aligned16(workspace)) return MC_ERR_ALIGN;
+  if (workspace == nullptr || workspace_bytes < pages_layout(num_pages, rows).total) return MC_ERR_WORKSPACE;
+  mc::PagesArgs a = pages_args(ref_counts, num_pages, block_tables, max_pages_per_req, page_size, seq_lens, rows, n, report, workspace);
+  a.list = src_rows, a.dst_list = dst_rows, a.moves = moves;
+  return mc::launch_pages_give(true, a, reinterpret_cast<hipStream_t>(hip_stream)) == hipSuccess ? MC_OK : MC_ERR_HIP;
+}
+
+mc_status mc_kv_pages_grow(int32_t* ref_counts, int64_t num_pages, int32_t* block_tables, int32_t max_pages_per_req, int32_t page_size,
+                           int32_t* seq_lens, int32_t rows, const int32_t* add, int32_t* report, void* workspace, size_t workspace_bytes,
+                           void* hip_stream) {
+  const mc_status st = check_pages(ref_counts, num_pages, block_tables, max_pages_per_req, page_size, seq_lens, rows);
+  if (st != MC_OK) return st;
+  if (rows == 0) return MC_OK;
+  if (add == nullptr || report == nullptr) return MC_ERR_NULL;
+  if (!aligned4(add) || !aligned4(report) || !aligned16(workspace)) return MC_ERR_ALIGN;
+  if (workspace == nullptr || workspace_bytes < pages_layout(num_pages, rows).total) return MC_ERR_WORKSPACE;
+  mc::PagesArgs a = pages_args(ref_counts, num_pages, block_tables, max_pages_per_req, page_size, seq_lens, rows, rows, report, workspace);
+  a.list = add;
+  return mc::launch_pages_give(false, a, reinterpret_cast<hipStream_t>(hip_stream)) == hipSuccess ? MC_OK : MC_ERR_HIP;
+}
+
+mc_status mc_kv_pages_free(int32_t* ref_counts, int64_t num_pages, const int32_t* block_tables, int32_t max_pages_per_req,
+                           int32_t page_size, int32_t* seq_lens, int32_t rows, const int32_t* free_rows, int32_t n, int32_t* report,
+                           void* hip_stream) {
+  const mc_status st = check_pages(ref_counts, num_pages, block_tables, max_pages_per_req, page_size, seq_lens, rows);
+  if (st != MC_OK) return st;
+  if (n < 0) return MC_ERR_SHAPE;
+  if (n == 0 || rows == 0) return MC_OK;
+  if (free_rows == nullptr || report == nullptr) return MC_ERR_NULL;
+  if (!aligned4(free_rows) || !aligned4(report)) return MC_ERR_ALIGN;
+  mc::PagesArgs a = pages_args(ref_counts, num_pages, const_cast<int32_t*>(block_tables), max_pages_per_req, page_size, seq_lens, rows, n,
+                               report, nullptr);
+  a.list = free_rows;
+  return mc::launch_pages_free(a, reinterpret_cast<hipStream_t>(hip_stream)) == hipSuccess ? MC_OK : MC_ERR_HIP;
+}
+
+mc_status mc_kv_pages_compact(const int32_t* ref_counts, int64_t num_pages, int32_t max_moves, int32_t* moves, int32_t* report,
+                              void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (num_pages <= 0 || max_moves < 0) return MC_ERR_SHAPE;
+  if (num_pages > INT32_MAX / 2) return MC_ERR_RANGE;
+  if (max_moves == 0) return MC_OK;
+  if (ref_counts == nullptr || moves == nullptr || report == nullptr) return MC_ERR_NULL;
+  if (!aligned4(ref_counts) || !aligned4(moves) || !aligned4(report) || !aligned16(workspace)) return MC_ERR_ALIGN;
+  if (workspace == nullptr || workspace_bytes < pages_layout(num_pages, 0).total) return MC_ERR_WORKSPACE;
+  mc::PagesArgs a = pages_args(const_cast<int32_t*>(ref_counts), num_pages, nullptr, 0, 1, nullptr, 0, max_moves, report, workspace);
+  a.moves = moves;
+  return mc::launch_pages_compact(a, reinterpret_cast<hipStream_t>(hip_stream)) == hipSuccess ? MC_OK : MC_ERR_HIP;
+}
+
+mc_status mc_kv_pages_remap(int32_t* ref_counts, int64_t num_pages, int32_t* block_tables, int32_t max_pages_per_req, int32_t page_size,
+                            const int32_t* seq_lens, int32_t rows, const int32_t* moves, const int32_t* count, int32_t n,
+                            void* hip_stream) {
+  const mc_status st = check_pages(ref_counts, num_pages, block_tables, max_pages_per_req, page_size, seq_lens, rows);
+  if (st != MC_OK) return st;
+  if (n < 0) return MC_ERR_SHAPE;
+  if (n == 0) return MC_OK;
+  if (ref_counts == nullptr || moves == nullptr) return MC_ERR_NULL;
+  if (!aligned4(ref_counts) || !aligned4(moves) || !aligned4(count)) return MC_ERR_ALIGN;
+  mc::PagesArgs a = pages_args(ref_counts, num_pages, block_tables, max_pages_per_req, page_size, const_cast<int32_t*>(seq_lens), rows, n,
+                               nullptr, nullptr);
+  a.moves = const_cast<int32_t*>(moves);
+  return mc::launch_pages_remap(a, count, reinterpret_cast<hipStream_t>(hip_stream)) == hipSuccess ? MC_OK : MC_ERR_HIP;
+}
+
+mc_status mc_kv_copy_pages(void* const* k_pools, void* const* v_pools, int32_t n_layers, int64_t num_pages, int64_t page_bytes,
+                           const int32_t* moves, const int32_t* count, int32_t n, void* hip_stream) {
+  if (n_layers < 0 || n < 0 || num_pages <= 0 || page_bytes < 0) return MC_ERR_SHAPE;
+  if (n_layers > MC_MAX_COPY_LAYERS || num_pages > INT32_MAX || page_bytes > (int64_t)1 << 34) return MC_ERR_RANGE;
+  if (page_bytes % 16 != 0) return MC_ERR_ALIGN;
+  if (n_layers == 0 || n == 0 || page_bytes == 0) return MC_OK;
+  if (k_pools == nullptr || v_pools == nullptr || moves == nullptr) return MC_ERR_NULL;
+  mc::LayerPools pools = {};
+  for (int32_t l = 0; l < n_layers; ++l) {
+    if (k_pools[l] == nullptr || v_pools[l] == nullptr) return MC_ERR_NULL;
+    if (!aligned16(k_pools[l]) || !aligned16(v_pools[l])) return MC_ERR_ALIGN;
+    pools.at[2 * l] = k_pools[l];
+    pools.at[2 * l + 1] = v_pools[l];
+  }
+  if (!aligned4(moves) || !aligned4(count)) return MC_ERR_ALIGN;
+  return mc::launch_pages_copy(pools, n_layers, num_pages, page_bytes, moves, count, n, reinterpret_cast<hipStream_t>(hip_stream)) ==
+                 hipSuccess
+             ? MC_OK
+             : MC_ERR_HIP;
 }
 
 mc_status mc_kv_page_order(const int32_t* page_ids, int64_t n, int32_t* order, void* hip_stream) {

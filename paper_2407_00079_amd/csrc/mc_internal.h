@@ -112,6 +112,27 @@ struct DecodeArgs {
 };
 hipError_t launch_attn_decode(int dtype, int head_dim, const DecodeArgs& args, hipStream_t stream);
 
+// Page bookkeeping (kv_pages.hip); a call uses the fields it has something for.
+struct PagesArgs {
+  int32_t *ref_counts, *block_tables, *seq_lens, *moves, *report;
+  const int32_t *list, *dst_list;    // a fork's rows from and to; tokens to grow by; rows to free
+  int64_t num_pages;
+  int32_t max_pages, page_size, rows, n, chunks;
+  // in the workspace
+  int32_t *free_before;              // free pages of each chunk
+  int32_t *wanted_before, *lens, *claims;
+  PagesHead* head;
+};
+hipError_t launch_pages_give(bool fork, const PagesArgs& args, hipStream_t stream);
+hipError_t launch_pages_free(const PagesArgs& args, hipStream_t stream);
+hipError_t launch_pages_compact(const PagesArgs& args, hipStream_t stream);
+hipError_t launch_pages_remap(const PagesArgs& args, const int32_t* count, hipStream_t stream);
+struct LayerPools {
+  void* at[2 * MC_MAX_COPY_LAYERS];  // K and V of each layer in turn
+};
+hipError_t launch_pages_copy(const LayerPools& pools, int n_layers, int64_t num_pages, int64_t page_bytes, const int32_t* moves,
+                             const int32_t* count, int n, hipStream_t stream);
+
 // The offset tables of a prefix call: both in device memory or, if `arg` is set, both in it (at most kMaxArgEntries + 1
 // entries each; they then travel with the launch).
 struct PrefixTables {

@@ -101,4 +101,10 @@ constexpr int64_t decode_begin(int64_t total, int w, int waves) { return total *
 // the wave that has place x of the line
 constexpr int decode_wave_of(int64_t total, int64_t x, int waves) { return (int)(((x + 1) * waves - 1) / total); }
 
+// Page bookkeeping (kv_pages.hip): pages whose free ones one workgroup counts and gives out
+constexpr int kPagesChunk = 4096;
+struct PagesHead {
+  int32_t wanted, refused;
+};
+
 }  // namespace mc

@@ -130,7 +130,7 @@ class Host(torch.Tensor):
 
 
 def host(shape, dtype=torch.bfloat16, strides=None):
-    x = torch.empty(shape, dtype=dtype) if strides is None else torch.empty(1 << 16, dtype=dtype).as_strided(shape, strides)
+    x = torch.empty(shape, dtype=dtype) if strides is None else torch.empty(1 << 18, dtype=dtype).as_strided(shape, strides)
     return x.as_subclass(Host)
 
 
