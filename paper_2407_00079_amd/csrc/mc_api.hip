@@ -172,13 +172,15 @@ mc_status check_rope_buffers(const mc_attn_params* p, const void* q, const void*
   // in place only where a token's rows are read and written at one place
   if (q == q_out && strides != nullptr && strides[0] != (int64_t)p->num_q_heads * p->head_dim) return MC_ERR_SHAPE;
   const int64_t rows = p->num_q_heads + 2 * (int64_t)p->num_kv_heads;
-  return rows > INT32_MAX / 2 || tokens * rows / 16 + 1 > INT32_MAX ? MC_ERR_RANGE : MC_OK;     // (a workgroup takes 16 rows at least)
+  // (a token's rows: rows_inverse below; a workgroup takes 16 rows at least)
+  return rows > 1 << 15 || tokens > INT32_MAX || tokens * rows / 16 + 1 > INT32_MAX ? MC_ERR_RANGE : MC_OK;
 }
 
 mc::RopeArgs rope_args(const mc_attn_params* p, const mc_rope_params* rope, const void* q, const void* k, const void* v,
                        const int64_t* strides, const void* q_norm, const void* k_norm, void* q_out, void* k_pool, void* v_pool,
                        const int32_t* block_tables, int32_t max_pages, int64_t tokens) {
   mc::RopeArgs a = {};
+  const uint64_t rows = p->num_q_heads + 2 * (uint64_t)p->num_kv_heads;
   for (int32_t i = 0; i < rope->rotary_dim / 2; ++i) a.turns[i] = rope->inv_freq[i] / 6.283185307179586476925;
   a.q = q, a.k = k, a.v = v, a.q_norm = q_norm, a.k_norm = k_norm;
   a.q_out = q_out, a.k_pool = k_pool, a.v_pool = v_pool;
@@ -187,7 +189,9 @@ mc::RopeArgs rope_args(const mc_attn_params* p, const mc_rope_params* rope, cons
   a.q_stride = strides != nullptr ? strides[0] * elem : p->num_q_heads * row;
   a.k_stride = strides != nullptr ? strides[1] * elem : p->num_kv_heads * row;
   a.v_stride = strides != nullptr ? strides[2] * elem : p->num_kv_heads * row;
-  a.total_rows = tokens * ((int64_t)p->num_q_heads + 2 * (int64_t)p->num_kv_heads);
+  a.total_tokens = (int32_t)tokens;
+  // exact for dividends x with x * rows < 2^32: a workgroup divides less than its own 160 rows plus one token's (check_rope_buffers)
+  a.rows_inverse = (uint32_t)((((uint64_t)1 << 32) + rows - 1) / rows);
   a.Hq = p->num_q_heads, a.Hkv = p->num_kv_heads, a.max_pages = max_pages;
   a.rotary = rope->rotary_dim, a.layout = rope->layout;
   a.eps = rope->norm_eps, a.gain = rope->gain;

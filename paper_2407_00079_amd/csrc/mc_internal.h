@@ -88,7 +88,8 @@ struct RopeArgs {
   void *q_out, *k_pool, *v_pool;
   const int32_t* block_tables;
   int64_t q_stride, k_stride, v_stride;   // bytes from token to token
-  int64_t total_rows;                // tokens * (Hq + 2 Hkv)
+  int32_t total_tokens;
+  uint32_t rows_inverse;             // 2^32 / (Hq + 2 Hkv) rounded up: rows to tokens by a product
   int32_t Hq, Hkv, max_pages, rotary, layout;
   float eps, gain;
 };

@@ -25,38 +25,56 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 
-// What the kernel asks of a source: where token `tok` stands.  Called by the first wave, lane by lane for tokens first + lane.
+// Where a token stands.
 struct Place {
   int32_t row;        // block-table row
   int32_t pos;        // position, negative: the token is left out
 };
+// What a workgroup's waves ask of a source of places: ahead() before anything else, then place() of one token at a time, the same for
+// all lanes of a wave.  The vector unit's loads come back in order, so the table is asked for before the rows (ahead), and all
+// that depends on it goes through the scalar unit, which does not wait for the rows.
+typedef const __attribute__((address_space(4))) int32_t* const_i32_ptr;
+struct Requests {
+  // up to 64 requests stand in a wave's lanes; of more, every stride-th, and the last steps of the search read the table
+  static __device__ __forceinline__ Place place(const AttnReq* reqs, const AttnReq& mine, int batch, int stride, int32_t tok) {
+    const int lane = threadIdx.x & 63;
+    const int k = __popcll(__builtin_amdgcn_ballot_w64((int64_t)lane * stride < batch && mine.q_off <= tok)) - 1;
+    if (stride == 1)
+      return {k, __builtin_amdgcn_readlane(mine.prefix, k) + (tok - __builtin_amdgcn_readlane(mine.q_off, k))};
+    const const_i32_ptr at = (const_i32_ptr)reqs;
+    int lo = k * stride, hi = lo + stride < batch ? lo + stride - 1 : batch - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (at[4 * (int64_t)mid] <= tok) lo = mid; else hi = mid - 1;
+    }
+    return {lo, at[4 * (int64_t)lo + 1] + (tok - at[4 * (int64_t)lo])};
+  }
+};
+static_assert(sizeof(AttnReq) == 16, "q_off and prefix are the first two of four integers");
 struct FromArg {
   AttnReqTable t;
   int32_t batch;
-  __device__ __forceinline__ Place place(int32_t first, int32_t tok, int32_t) const {
-    const int lane = threadIdx.x & 63;
-    int r = __popcll(__builtin_amdgcn_ballot_w64(lane < batch && t.r[lane].q_off <= first)) - 1;
-    while (r + 1 < batch && t.r[r + 1].q_off <= tok) ++r;
-    return {r, t.r[r].prefix + (tok - t.r[r].q_off)};
-  }
+  typedef AttnReq Ahead;
+  __device__ __forceinline__ Ahead ahead() const { return t.r[threadIdx.x & 63]; }           // (zeros past the batch)
+  __device__ __forceinline__ Place place(const Ahead& mine, int32_t tok, int32_t) const { return Requests::place(nullptr, mine, batch, 1, tok); }
 };
 struct FromList {
   const AttnReq* reqs;
-  int32_t batch;
-  __device__ __forceinline__ Place place(int32_t, int32_t tok, int32_t) const {
-    int lo = 0, hi = batch - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (reqs[mid].q_off <= tok) lo = mid; else hi = mid - 1;
-    }
-    return {lo, reqs[lo].prefix + (tok - reqs[lo].q_off)};
+  int32_t batch, stride;
+  typedef AttnReq Ahead;
+  __device__ __forceinline__ Ahead ahead() const {
+    const int64_t i = (int64_t)(threadIdx.x & 63) * stride;
+    return reqs[i < batch ? i : batch - 1];
   }
+  __device__ __forceinline__ Place place(const Ahead& mine, int32_t tok, int32_t) const { return Requests::place(reqs, mine, batch, stride, tok); }
 };
 // one new token a row, its length (the token included) in device memory; lengths the table has no room for are left out
 struct FromLens {
   const int32_t* lens;
-  __device__ __forceinline__ Place place(int32_t, int32_t tok, int32_t max_pages) const {
-    const int32_t len = lens[tok];
+  struct Ahead {};
+  __device__ __forceinline__ Ahead ahead() const { return {}; }
+  __device__ __forceinline__ Place place(const Ahead&, int32_t tok, int32_t max_pages) const {
+    const int32_t len = ((const_i32_ptr)lens)[tok];
     return {tok, len > 0 && (len - 1) >> 4 < max_pages ? len - 1 : -1};
   }
 };
@@ -79,63 +97,82 @@ struct Granule {
   }
 };
 
+// a value of another lane of the 16 (or 8) that hold a row, exchanged in registers
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, false));
+}
+// sum over a row's lanes: pairs, quads, halves of a row of 16, all of it
+template <int LANES>
+__device__ __forceinline__ float sum_over_row(float x) {
+  x += dpp<0xB1>(x);                                         // quad_perm 1 0 3 2
+  x += dpp<0x4E>(x);                                         // quad_perm 2 3 0 1
+  x += dpp<0x141>(x);                                        // row_half_mirror
+  if constexpr (LANES == 16) x += dpp<0x140>(x);             // row_mirror
+  return x;
+}
+// of the lane half a row away
+template <int LANES>
+__device__ __forceinline__ float across(float x) {
+  if constexpr (LANES == 16) return dpp<0x128>(x);           // row_ror:8
+  else return __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, x), 0x101F));        // lane ^ 4
+}
+
 template <typename T, int D, int U, typename Source>
 __global__ __launch_bounds__(kThreads) void rope_append_kernel(const RopeArgs a, const Source source) {
   typedef Granule<T> Gr;
-  constexpr int kElems = Gr::kElems, kLanes = D / kElems, kStep = kThreads / kLanes, kRows = kStep * U;
-  constexpr int kRowB = D * (int)sizeof(T);
+  constexpr int kElems = Gr::kElems, kLanes = D / kElems, kSlots = kThreads / kLanes, kRows = kSlots * U, kRowB = D * (int)sizeof(T);
   constexpr int kMostTokens = (kRows - 1) / 3 + 2;           // a token has three rows at least
-  static_assert(kMostTokens <= 64, "the first wave looks a workgroup's tokens up");
   __shared__ __attribute__((aligned(16))) float cosine[kMostTokens][D / 2], sine[kMostTokens][D / 2];
+  __shared__ double turns_of[D / 2];
   __shared__ int32_t pos_of[kMostTokens];
   __shared__ int64_t page_of[kMostTokens];
 
+  const typename Source::Ahead table = source.ahead();
+  const double turns = a.turns[threadIdx.x % (D / 2)];
   const int rows = a.Hq + 2 * a.Hkv;                         // of a token
   const int64_t first = (int64_t)blockIdx.x * kRows;
   const int32_t tok0 = (int32_t)((uint64_t)first / (uint32_t)rows);
   const int ahead = (int)(first - (int64_t)tok0 * rows);
-  const int left = (int)(a.total_rows - first < kRows ? a.total_rows - first : kRows);
-  const int n_tok = (ahead + left - 1) / rows + 1;
-  const int gran = threadIdx.x % kLanes;
+  const int64_t rest = (int64_t)a.total_tokens * rows - first;
+  const int left = rest < kRows ? (int)rest : kRows;
+  const int slot = threadIdx.x / kLanes, gran = threadIdx.x % kLanes;
 
+  // (Every lane loads, those without a row of their own the last one: behind a branch each load would be waited for by itself.)
   u32x4 raw[U];
   int local[U], row[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int item = (int)threadIdx.x / kLanes + u * kStep;
-    local[u] = (int)((uint32_t)(ahead + item) / (uint32_t)rows);
+    const int item = slot + u * kSlots < left ? slot + u * kSlots : left - 1;
+    local[u] = (int)__umulhi((uint32_t)(ahead + item), a.rows_inverse);
     row[u] = ahead + item - local[u] * rows;
-    raw[u] = u32x4{};
-    if (item < left) {
-      const int64_t tok = tok0 + local[u];
-      const char* at = row[u] < a.Hq ? (const char*)a.q + tok * a.q_stride + (int64_t)row[u] * kRowB
-                       : row[u] < a.Hq + a.Hkv ? (const char*)a.k + tok * a.k_stride + (int64_t)(row[u] - a.Hq) * kRowB
-                                               : (const char*)a.v + tok * a.v_stride + (int64_t)(row[u] - a.Hq - a.Hkv) * kRowB;
-      raw[u] = *reinterpret_cast<const u32x4*>(at + gran * 16);
-    } else {
-      row[u] = -1;
-    }
+    const int64_t tok = tok0 + local[u];
+    const int r = row[u];
+    const char* const at = r < a.Hq ? (const char*)a.q + tok * a.q_stride + (int64_t)r * kRowB
+                           : r < a.Hq + a.Hkv ? (const char*)a.k + tok * a.k_stride + (int64_t)(r - a.Hq) * kRowB
+                                              : (const char*)a.v + tok * a.v_stride + (int64_t)(r - a.Hq - a.Hkv) * kRowB;
+    raw[u] = *reinterpret_cast<const u32x4*>(at + gran * 16);
   }
-  float wq[kElems], wk[kElems];
-#pragma unroll
-  for (int e = 0; e < kElems; ++e) wq[e] = wk[e] = 1.f;
-  if (a.q_norm != nullptr) Gr::widen(reinterpret_cast<const u32x4*>(a.q_norm)[gran], wq);
-  if (a.k_norm != nullptr) Gr::widen(reinterpret_cast<const u32x4*>(a.k_norm)[gran], wk);
+  // (no weights: whatever lies at hand, unused)
+  const u32x4 wq = reinterpret_cast<const u32x4*>(a.q_norm != nullptr ? a.q_norm : a.q)[gran];
+  const u32x4 wk = reinterpret_cast<const u32x4*>(a.k_norm != nullptr ? a.k_norm : a.k)[gran];
 
-  if (threadIdx.x < 64) {
-    const int l = (int)threadIdx.x < n_tok ? (int)threadIdx.x : n_tok - 1;
-    const Place p = source.place(tok0, tok0 + l, a.max_pages);
-    if ((int)threadIdx.x < n_tok) {
+  const int n_tok = (int)__umulhi((uint32_t)(ahead + left - 1), a.rows_inverse) + 1;
+  if (threadIdx.x < D / 2) turns_of[threadIdx.x] = turns;
+  for (int l = __builtin_amdgcn_readfirstlane(threadIdx.x / 64); l < n_tok; l += kThreads / 64) {
+    const Place p = source.place(table, tok0 + l, a.max_pages);
+    const int64_t page = p.pos < 0 ? 0 : ((const_i32_ptr)a.block_tables)[(int64_t)p.row * a.max_pages + (p.pos >> 4)];
+    if (threadIdx.x % 64 == 0) {
       pos_of[l] = p.pos;
-      page_of[l] = p.pos < 0 ? 0 : a.block_tables[(int64_t)p.row * a.max_pages + (p.pos >> 4)];
+      page_of[l] = page;
     }
   }
   __syncthreads();
   const int half = a.rotary / 2;
   for (int i = threadIdx.x; i < n_tok * half; i += kThreads) {
-    const int l = (int)((uint32_t)i / (uint32_t)half), f = i - l * half;
-    const double turns = (double)pos_of[l] * a.turns[f];
-    const float part = (float)(turns - __builtin_rint(turns));                      // -1/2 .. 1/2
+    const int l = n_tok == 1 ? 0 : (int)((uint32_t)i / (uint32_t)half), f = i - l * half;
+    const double at = (double)pos_of[l] * turns_of[f];
+    const float part = (float)(at - __builtin_rint(at));     // -1/2 .. 1/2
     float s, c;
     sincospif(2.f * part, &s, &c);
     cosine[l][f] = c * a.gain;
@@ -144,66 +181,69 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(const RopeArgs a,
   __syncthreads();
 
   const int half_lanes = half / kElems;
+  const bool halves = a.layout == MC_ROPE_HALF, all = half_lanes * 2 == kLanes;
   const bool rotated = gran < 2 * half_lanes;
   const bool second = gran >= half_lanes;                    // (half layout) of the two halves
   const int lane = threadIdx.x & 63;
   const int partner = !rotated ? lane : second ? lane - half_lanes : lane + half_lanes;
+  const int angle = !rotated ? 0 : halves ? (second ? gran - half_lanes : gran) * kElems : gran * kElems / 2;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    if (U > 1 && __builtin_amdgcn_ballot_w64(row[u] >= 0) == 0) break;
-    const bool is_q = row[u] < a.Hq, is_v = row[u] >= a.Hq + a.Hkv;
+    if (slot + u * kSlots >= left) break;                    // (whole lane groups: no exchange below crosses them)
+    const int r = row[u], pos = pos_of[local[u]];
+    if (pos < 0) continue;
+    const int64_t pool_row = page_of[local[u]] * a.Hkv * 16 + (pos & 15);
+    if (r >= a.Hq + a.Hkv) {
+      *reinterpret_cast<u32x4*>((char*)a.v_pool + (pool_row + (int64_t)(r - a.Hq - a.Hkv) * 16) * kRowB + gran * 16) = raw[u];
+      continue;
+    }
+    const bool is_q = r < a.Hq;
     float x[kElems];
     Gr::widen(raw[u], x);
-    if (is_q ? a.q_norm != nullptr : a.k_norm != nullptr) {  // (the lanes of a row agree)
-      float sum = 0.f;
+    if (is_q ? a.q_norm != nullptr : a.k_norm != nullptr) {
+      float sum = 0.f, w[kElems];
+      Gr::widen(is_q ? wq : wk, w);
 #pragma unroll
       for (int e = 0; e < kElems; ++e) sum = __builtin_fmaf(x[e], x[e], sum);
+      const float inv = rsqrtf(sum_over_row<kLanes>(sum) * (1.f / D) + a.eps);
 #pragma unroll
-      for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor(sum, d, 64);
-      const float inv = rsqrtf(sum * (1.f / D) + a.eps);
-#pragma unroll
-      for (int e = 0; e < kElems; ++e) x[e] *= inv * (is_q ? wq[e] : wk[e]);
+      for (int e = 0; e < kElems; ++e) x[e] *= inv * w[e];
     }
-    if (a.layout == MC_ROPE_HALF) {
-      const int base = second ? gran - half_lanes : gran;
+    float y[kElems];
+    if (halves) {
 #pragma unroll
-      for (int e = 0; e < kElems; ++e) {
-        const float other = __shfl(x[e], partner, 64);
-        if (rotated) {
-          const float c = cosine[local[u]][base * kElems + e], s = sine[local[u]][base * kElems + e];
-          x[e] = __builtin_fmaf(x[e], c, second ? other * s : -(other * s));
-        }
+      for (int e = 0; e < kElems; ++e) y[e] = all ? across<kLanes>(x[e]) : __shfl(x[e], partner, 64);
+      if (rotated) {
+        const float sign = second ? 1.f : -1.f;
+#pragma unroll
+        for (int e = 0; e < kElems; ++e) x[e] = __builtin_fmaf(x[e], cosine[local[u]][angle + e], sign * y[e] * sine[local[u]][angle + e]);
       }
     } else if (rotated) {
 #pragma unroll
       for (int e = 0; e < kElems; e += 2) {
-        const float c = cosine[local[u]][(gran * kElems + e) / 2], s = sine[local[u]][(gran * kElems + e) / 2];
-        const float p = x[e], q = x[e + 1];
+        const float c = cosine[local[u]][angle + e / 2], s = sine[local[u]][angle + e / 2], p = x[e], q = x[e + 1];
         x[e] = __builtin_fmaf(p, c, -(q * s));
         x[e + 1] = __builtin_fmaf(q, c, p * s);
       }
     }
-    if (row[u] < 0) continue;
-    const int32_t pos = pos_of[local[u]];
-    if (pos < 0) continue;
-    const u32x4 done = is_v ? raw[u] : Gr::rounded(x);
-    if (is_q) {
-      *reinterpret_cast<u32x4*>((char*)a.q_out + ((int64_t)(tok0 + local[u]) * a.Hq + row[u]) * kRowB + gran * 16) = done;
-    } else {
-      const int64_t head = row[u] - a.Hq - (is_v ? a.Hkv : 0);
-      *reinterpret_cast<u32x4*>((char*)(is_v ? a.v_pool : a.k_pool) + ((page_of[local[u]] * a.Hkv + head) * 16 + (pos & 15)) * kRowB + gran * 16) =
-          done;
-    }
+    char* const to = is_q ? (char*)a.q_out + ((tok0 + local[u]) * (int64_t)a.Hq + r) * kRowB
+                          : (char*)a.k_pool + (pool_row + (int64_t)(r - a.Hq) * 16) * kRowB;
+    *reinterpret_cast<u32x4*>(to + gran * 16) = Gr::rounded(x);
   }
 }
 
 template <typename T, int D, typename Source>
 void enqueue(const RopeArgs& args, const Source& source, hipStream_t stream) {
-  constexpr int kStep = kThreads / (D / Granule<T>::kElems);
-  auto grid = [&](int rows) { return (unsigned)((args.total_rows + rows - 1) / rows); };
-  // Few rows: one to a lane group, so that they spread over the chip; else four, whose loads are in flight together.
-  if (grid(4 * kStep) < 2 * 256) rope_append_kernel<T, D, 1><<<grid(kStep), kThreads, 0, stream>>>(args, source);
-  else rope_append_kernel<T, D, 4><<<grid(4 * kStep), kThreads, 0, stream>>>(args, source);
+  constexpr int kSlots = kThreads / (D / Granule<T>::kElems);
+  const int rows = args.Hq + 2 * args.Hkv;
+  auto grid = [&](int u) { return (unsigned)(((int64_t)args.total_tokens * rows + kSlots * u - 1) / (kSlots * u)); };
+  // Few rows: one a lane group, so that they spread over the chip.  Else several, whose loads are in flight together: as many as
+  // make a workgroup's rows whole tokens or a token's rows whole workgroups, where 3 to 5 do.
+  auto even = [&](int u) { return rows % (kSlots * u) == 0 || kSlots * u % rows == 0; };
+  if (grid(4) < 2 * 256) rope_append_kernel<T, D, 1><<<grid(1), kThreads, 0, stream>>>(args, source);
+  else if (even(5)) rope_append_kernel<T, D, 5><<<grid(5), kThreads, 0, stream>>>(args, source);
+  else if (even(3) && !even(4)) rope_append_kernel<T, D, 3><<<grid(3), kThreads, 0, stream>>>(args, source);
+  else rope_append_kernel<T, D, 4><<<grid(4), kThreads, 0, stream>>>(args, source);
 }
 template <typename Source>
 hipError_t launch(int dtype, int head_dim, const RopeArgs& args, const Source& source, hipStream_t stream) {
@@ -220,7 +260,7 @@ hipError_t launch(int dtype, int head_dim, const RopeArgs& args, const Source& s
 hipError_t launch_rope_append(int dtype, int head_dim, const RopeArgs& args, const AttnReq* reqs, const AttnReqTable* arg, int32_t batch,
                               hipStream_t stream) {
   if (arg != nullptr) return launch(dtype, head_dim, args, FromArg{*arg, batch}, stream);
-  return launch(dtype, head_dim, args, FromList{reqs, batch}, stream);
+  return launch(dtype, head_dim, args, FromList{reqs, batch, (batch + 63) / 64}, stream);
 }
 
 hipError_t launch_rope_append_tokens(int dtype, int head_dim, const RopeArgs& args, const int32_t* seq_lens, hipStream_t stream) {
