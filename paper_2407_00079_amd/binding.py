@@ -68,7 +68,7 @@ _lib = None
 
 def lib():
     """The loaded library; raises if it was never built (run ``__graft_entry__.build()``)."""
-    global _lib, _call
+    global _lib, _call, _misfit, _row_stride
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2407_00079_amd.build` "
@@ -170,7 +170,7 @@ def lib():
             _call = _call_by_ctypes
         else:
             _function.update((name, ctypes.cast(getattr(l, name), ctypes.c_void_p).value) for name in EXPORTS)
-            _call = _mccall.call
+            _call, _misfit, _row_stride = _mccall.call, _mccall.misfit, _mccall.row_stride
         _lib = l
     return _lib
 
@@ -637,56 +637,74 @@ def _dtypes() -> dict:
     global _torch
     if _torch is None:
         import torch
+        lib()
         _DTYPES.update({MC_DTYPE_BF16: torch.bfloat16, MC_DTYPE_F32: torch.float32})
         _torch = torch
     return _DTYPES
 
 
-def _dense(name: str, device: int, t, dtype, least: int) -> None:
-    """A dense tensor of a call: its type, its device, and that it has the elements the call will use."""
-    if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or t.numel() < least:
-        raise ValueError(f"{name}: dense {dtype} of at least {least} elements on device {device} wanted, "
-                         f"not {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+def _misfit_by_python(device: int, dtype, *tensors) -> int:
+    """What csrc/pycall.cpp does, for an interpreter it was not built for."""
+    for i, (t, least) in enumerate(zip(tensors[::2], tensors[1::2])):
+        if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or t.numel() < least:
+            return i
+    return -1
 
 
-def _row_stride(name: str, device: int, t, dtype, tokens: int, heads: int, dim: int) -> int:
-    """Elements from token to token of [tokens, heads, dim] or [tokens, heads * dim], a token's heads dense."""
-    shape, stride = t.shape, t.stride()
+def _row_stride_by_python(device: int, dtype, t, tokens: int, heads: int, dim: int) -> int:
+    shape, stride = tuple(t.shape), t.stride()
     fits = (len(shape) == 2 and shape[1] == heads * dim and stride[1] == 1) or (
         len(shape) == 3 and shape[1] == heads and shape[2] == dim and stride[2] == 1 and (stride[1] == dim or heads == 1))
     if not fits or shape[0] != tokens or t.dtype is not dtype or t.get_device() != device:
-        raise ValueError(f"{name}: {dtype} [{tokens}, {heads}, {dim}] with dense heads on device {device} wanted, "
-                         f"not {t.dtype} {tuple(shape)} strides {stride} on {t.device}")
+        return -1
     return stride[0] if tokens > 1 else heads * dim
 
 
-def _pools(params, device: int, dtype, k_pool, v_pool) -> None:
-    least = params.num_pages * params.num_kv_heads * params.page_size * params.head_dim
-    _dense("k_pool", device, k_pool, dtype, least)
-    _dense("v_pool", device, v_pool, dtype, least)
+_misfit, _row_stride = _misfit_by_python, _row_stride_by_python
 
 
-def _table(device: int, block_tables, rows: int) -> int:
+def _is(t) -> str:
+    return f"{t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}"
+
+
+def _dense(names: str, device: int, dtype, *tensors) -> None:
+    """Tensors of a call, each followed by the number of elements the call will use: dense, of this type, on this device."""
+    bad = _misfit(device, dtype, *tensors)
+    if bad >= 0:
+        raise ValueError(f"{names.split()[bad]}: dense {dtype} of at least {tensors[2 * bad + 1]} elements on device {device} wanted, "
+                         f"not {_is(tensors[2 * bad])}")
+
+
+def _pool_size(params) -> int:
+    return params.num_pages * params.num_kv_heads * params.page_size * params.head_dim
+
+
+def _table(block_tables, rows: int) -> int:
     """Columns of a block table that has ``rows`` rows."""
-    if block_tables.dim() != 2 or block_tables.shape[0] < rows:
-        raise ValueError(f"block_tables: [{rows}, pages] wanted, not {tuple(block_tables.shape)}")
-    _dense("block_tables", device, block_tables, _torch.int32, 0)
-    return block_tables.shape[1]
+    shape = block_tables.shape
+    if len(shape) != 2 or shape[0] < rows:
+        raise ValueError(f"block_tables: [{rows}, pages] wanted, not {tuple(shape)}")
+    return shape[1]
 
 
 def _rope_tensors(params, q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, tokens: int):
     """Looks the tensors of a rotation call over: (device, strides or None where all of them are dense)."""
-    dtype = _dtypes()[params.dtype]
+    dtype = (_DTYPES or _dtypes())[params.dtype]
     device, Hq, Hkv, D = q.get_device(), params.num_q_heads, params.num_kv_heads, params.head_dim
-    strides = (_row_stride("q", device, q, dtype, tokens, Hq, D), _row_stride("k", device, k, dtype, tokens, Hkv, D),
-               _row_stride("v", device, v, dtype, tokens, Hkv, D))
-    if q_norm is not None:
-        _dense("q_norm", device, q_norm, dtype, D)
-    if k_norm is not None:
-        _dense("k_norm", device, k_norm, dtype, D)
-    _dense("q_out", device, q_out, dtype, tokens * Hq * D)
-    _pools(params, device, dtype, k_pool, v_pool)
-    return device, None if strides == (Hq * D, Hkv * D, Hkv * D) else (ctypes.c_int64 * 3)(*strides)
+    a, b, c = (_row_stride(device, dtype, q, tokens, Hq, D), _row_stride(device, dtype, k, tokens, Hkv, D),
+               _row_stride(device, dtype, v, tokens, Hkv, D))
+    if a < 0 or b < 0 or c < 0:
+        name, t, heads = ("q", q, Hq) if a < 0 else ("k", k, Hkv) if b < 0 else ("v", v, Hkv)
+        raise ValueError(f"{name}: {dtype} [{tokens}, {heads}, {D}] with dense heads on device {device} wanted, not {_is(t)}")
+    size = _pool_size(params)
+    if q_norm is not None and k_norm is not None:
+        _dense("q_out k_pool v_pool q_norm k_norm", device, dtype, q_out, tokens * Hq * D, k_pool, size, v_pool, size, q_norm, D, k_norm, D)
+    else:
+        _dense("q_out k_pool v_pool", device, dtype, q_out, tokens * Hq * D, k_pool, size, v_pool, size)
+        for name, t in (("q_norm", q_norm), ("k_norm", k_norm)):
+            if t is not None:
+                _dense(name, device, dtype, t, D)
+    return device, None if a == Hq * D and b == c == Hkv * D else (ctypes.c_int64 * 3)(a, b, c)
 
 
 def _rope(rope):
@@ -704,8 +722,10 @@ def mc_kv_rope_append_paged(params: McAttnParams, rope: McRopeParams, q, k, v, q
     if len(new_lens) != n:
         raise ValueError(f"{n} prefix lengths and {len(new_lens)} new lengths")
     device, strides = _rope_tensors(_params(params), q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, sum(new_lens))
-    _enqueue("mc_kv_rope_append_paged", params, _rope(rope), q, k, v, strides, q_norm, k_norm, q_out, k_pool, v_pool, block_tables,
-             _table(device, block_tables, n), _ints("i", prefix_lens, n), _ints("i", new_lens, n), n, workspace, _nbytes(workspace),
+    wide = _table(block_tables, n)
+    _dense("block_tables", device, _torch.int32, block_tables, 0)
+    _enqueue("mc_kv_rope_append_paged", params, _rope(rope), q, k, v, strides, q_norm, k_norm, q_out, k_pool, v_pool, block_tables, wide,
+             _ints("i", prefix_lens, n), _ints("i", new_lens, n), n, workspace, _nbytes(workspace),
              _on(stream))
 
 
@@ -713,8 +733,10 @@ def mc_kv_rope_append_run(params: McAttnParams, plan: McAttnPlan, rope: McRopePa
                           block_tables, workspace, stream=None) -> None:
     """mc_kv_rope_append_paged for a prepared batch."""
     device, strides = _rope_tensors(_params(params), q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, _plan(plan).total_new_tokens)
-    _enqueue("mc_kv_rope_append_run", params, plan, _rope(rope), q, k, v, strides, q_norm, k_norm, q_out, k_pool, v_pool, block_tables,
-             _table(device, block_tables, plan.batch), workspace, _on(stream))
+    wide = _table(block_tables, plan.batch)
+    _dense("block_tables", device, _torch.int32, block_tables, 0)
+    _enqueue("mc_kv_rope_append_run", params, plan, _rope(rope), q, k, v, strides, q_norm, k_norm, q_out, k_pool, v_pool, block_tables, wide,
+             workspace, _on(stream))
 
 
 def mc_kv_rope_append_decode(params: McAttnParams, rope: McRopeParams, q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, block_tables,
@@ -722,9 +744,10 @@ def mc_kv_rope_append_decode(params: McAttnParams, rope: McRopeParams, q, k, v, 
     """The same for one new token a row, at position ``seq_lens[r] - 1``; ``seq_lens``: int32 device tensor."""
     n = seq_lens.shape[0]
     device, strides = _rope_tensors(_params(params), q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, n)
-    _dense("seq_lens", device, seq_lens, _torch.int32, n)
-    _enqueue("mc_kv_rope_append_decode", params, _rope(rope), q, k, v, strides, q_norm, k_norm, q_out, k_pool, v_pool, block_tables,
-             _table(device, block_tables, n), seq_lens, n, _on(stream))
+    wide = _table(block_tables, n)
+    _dense("seq_lens block_tables", device, _torch.int32, seq_lens, n, block_tables, 0)
+    _enqueue("mc_kv_rope_append_decode", params, _rope(rope), q, k, v, strides, q_norm, k_norm, q_out, k_pool, v_pool, block_tables, wide,
+             seq_lens, n, _on(stream))
 
 
 def mc_decode_attn_workspace_bytes(params: McAttnParams, batch: int) -> int:
@@ -733,83 +756,68 @@ def mc_decode_attn_workspace_bytes(params: McAttnParams, batch: int) -> int:
 
 def mc_decode_attn_paged(params: McAttnParams, q, k_pool, v_pool, block_tables, seq_lens, out, lse, workspace, stream=None) -> None:
     """Enqueue attention of one new token a row: q, out [rows, heads, head_dim], ``seq_lens`` int32 device tensor [rows]."""
-    dtype = _dtypes()[_params(params).dtype]
-    n, heads = seq_lens.shape[0], params.num_q_heads
-    device, size = q.get_device(), n * heads * params.head_dim
-    _dense("q", device, q, dtype, size)
-    _pools(params, device, dtype, k_pool, v_pool)
-    _dense("seq_lens", device, seq_lens, _torch.int32, n)
-    _dense("out", device, out, dtype, size)
+    dtype = (_DTYPES or _dtypes())[_params(params).dtype]
+    n, heads, wide = seq_lens.shape[0], params.num_q_heads, _table(block_tables, seq_lens.shape[0])
+    device, size, pool = q.get_device(), n * heads * params.head_dim, _pool_size(params)
+    _dense("q k_pool v_pool out", device, dtype, q, size, k_pool, pool, v_pool, pool, out, size)
+    _dense("seq_lens block_tables", device, _torch.int32, seq_lens, n, block_tables, 0)
     if lse is not None:
-        _dense("lse", device, lse, _torch.float32, n * heads)
-    _enqueue("mc_decode_attn_paged", params, q, k_pool, v_pool, block_tables, _table(device, block_tables, n), seq_lens, n, out, lse,
-             workspace, _nbytes(workspace), _on(stream))
+        _dense("lse", device, _torch.float32, lse, n * heads)
+    _enqueue("mc_decode_attn_paged", params, q, k_pool, v_pool, block_tables, wide, seq_lens, n, out, lse, workspace, _nbytes(workspace),
+             _on(stream))
 
 
 def mc_kv_pages_workspace_bytes(num_pages: int, rows: int) -> int:
     return int(lib().mc_kv_pages_workspace_bytes(num_pages, rows))
 
 
-def _state(ref_counts, block_tables, page_size: int, seq_lens):
-    """Looks a cache's bookkeeping over: (device, the seven arguments that stand for it)."""
-    _dtypes()
-    i32, device, rows = _torch.int32, ref_counts.get_device(), seq_lens.shape[0]
-    _dense("ref_counts", device, ref_counts, i32, 0)
-    _dense("seq_lens", device, seq_lens, i32, rows)
-    wide = _table(device, block_tables, rows)
-    return device, (ref_counts, ref_counts.shape[0], block_tables, wide, page_size, seq_lens, rows)
+def _state(ref_counts, block_tables, page_size: int, seq_lens, names: str, *more):
+    """Looks a cache's bookkeeping over, and the int32 tensors that follow with what is used of each: the seven arguments that
+    stand for it."""
+    if _torch is None:
+        _dtypes()
+    rows = seq_lens.shape[0]
+    wide = _table(block_tables, rows)
+    _dense("ref_counts block_tables seq_lens " + names, ref_counts.get_device(), _torch.int32, ref_counts, 0, block_tables, 0, seq_lens, rows, *more)
+    return ref_counts, ref_counts.numel(), block_tables, wide, page_size, seq_lens, rows
 
 
 def mc_kv_pages_fork(ref_counts, block_tables, page_size: int, seq_lens, src_rows, dst_rows, moves, report, workspace, stream=None) -> None:
     """Enqueue rows ``dst_rows`` becoming copies of ``src_rows``; all int32 device tensors, ``moves`` [n, 2], ``report`` [4]."""
-    device, state = _state(ref_counts, block_tables, page_size, seq_lens)
-    n, i32 = src_rows.shape[0], _torch.int32
-    _dense("src_rows", device, src_rows, i32, n)
-    _dense("dst_rows", device, dst_rows, i32, n)
-    _dense("moves", device, moves, i32, 2 * n)
-    _dense("report", device, report, i32, 4)
+    n = src_rows.numel()
+    state = _state(ref_counts, block_tables, page_size, seq_lens, "src_rows dst_rows moves report", src_rows, n, dst_rows, n, moves, 2 * n, report, 4)
     _enqueue("mc_kv_pages_fork", *state, src_rows, dst_rows, n, moves, report, workspace, _nbytes(workspace), _on(stream))
 
 
 def mc_kv_pages_grow(ref_counts, block_tables, page_size: int, seq_lens, add, report, workspace, stream=None) -> None:
     """Enqueue row r getting ``add[r]`` more tokens, and the pages that takes."""
-    device, state = _state(ref_counts, block_tables, page_size, seq_lens)
-    _dense("add", device, add, _torch.int32, state[-1])
-    _dense("report", device, report, _torch.int32, 4)
+    state = _state(ref_counts, block_tables, page_size, seq_lens, "add report", add, seq_lens.shape[0], report, 4)
     _enqueue("mc_kv_pages_grow", *state, add, report, workspace, _nbytes(workspace), _on(stream))
 
 
 def mc_kv_pages_free(ref_counts, block_tables, page_size: int, seq_lens, free_rows, report, stream=None) -> None:
     """Enqueue the listed rows becoming empty."""
-    device, state = _state(ref_counts, block_tables, page_size, seq_lens)
-    n = free_rows.shape[0]
-    _dense("free_rows", device, free_rows, _torch.int32, n)
-    _dense("report", device, report, _torch.int32, 4)
+    n = free_rows.numel()
+    state = _state(ref_counts, block_tables, page_size, seq_lens, "free_rows report", free_rows, n, report, 4)
     _enqueue("mc_kv_pages_free", *state, free_rows, n, report, _on(stream))
 
 
 def mc_kv_pages_compact(ref_counts, moves, report, workspace, stream=None) -> None:
     """Enqueue the list of at most ``moves.shape[0]`` moves that bring live pages to the front of the pool."""
-    _dtypes()
-    device, n = ref_counts.get_device(), moves.shape[0]
-    _dense("ref_counts", device, ref_counts, _torch.int32, 0)
-    _dense("moves", device, moves, _torch.int32, 2 * n)
-    _dense("report", device, report, _torch.int32, 4)
-    _enqueue("mc_kv_pages_compact", ref_counts, ref_counts.shape[0], n, moves, report, workspace, _nbytes(workspace), _on(stream))
-
-
-def _moves(device: int, moves, count) -> int:
+    if _torch is None:
+        _dtypes()
     n = moves.shape[0]
-    _dense("moves", device, moves, _torch.int32, 2 * n)
-    if count is not None:
-        _dense("count", device, count, _torch.int32, 1)
-    return n
+    _dense("ref_counts moves report", ref_counts.get_device(), _torch.int32, ref_counts, 0, moves, 2 * n, report, 4)
+    _enqueue("mc_kv_pages_compact", ref_counts, ref_counts.numel(), n, moves, report, workspace, _nbytes(workspace), _on(stream))
 
 
 def mc_kv_pages_remap(ref_counts, block_tables, page_size: int, seq_lens, moves, count=None, stream=None) -> None:
     """Enqueue tables and counts following ``moves`` [n, 2], of which ``count[0]`` are moves (None: all)."""
-    device, state = _state(ref_counts, block_tables, page_size, seq_lens)
-    n = _moves(device, moves, count)
+    n = moves.shape[0]
+    if count is None:
+        state = _state(ref_counts, block_tables, page_size, seq_lens, "moves", moves, 2 * n)
+    else:
+        state = _state(ref_counts, block_tables, page_size, seq_lens, "moves count", moves, 2 * n, count, 1)
     _enqueue("mc_kv_pages_remap", *state, moves, count, n, _on(stream))
 
 
@@ -818,12 +826,13 @@ def mc_kv_copy_pages(k_pools, v_pools, num_pages: int, page_bytes: int, moves, c
     _dtypes()
     if len(k_pools) != len(v_pools):
         raise ValueError(f"{len(k_pools)} K pools and {len(v_pools)} V pools")
-    device = moves.get_device()
-    n = _moves(device, moves, count)
+    device, n = moves.get_device(), moves.shape[0]
+    _dense("moves", device, _torch.int32, moves, 2 * n)
+    if count is not None:
+        _dense("count", device, _torch.int32, count, 1)
     for pool in (*k_pools, *v_pools):
         if pool.get_device() != device or not pool.is_contiguous() or pool.nbytes < num_pages * page_bytes:
-            raise ValueError(f"pools: {num_pages * page_bytes} dense bytes on device {device} wanted, not {pool.dtype} {tuple(pool.shape)} "
-                             f"strides {pool.stride()} on {pool.device}")
+            raise ValueError(f"pools: {num_pages * page_bytes} dense bytes on device {device} wanted, not {_is(pool)}")
     layers = len(k_pools)
     _enqueue("mc_kv_copy_pages", _ints("q", [t.data_ptr() for t in k_pools], layers), _ints("q", [t.data_ptr() for t in v_pools], layers),
              layers, num_pages, page_bytes, moves, count, n, _on(stream))

@@ -29,6 +29,25 @@ namespace {
 constexpr int kRows = 16;              // query heads of a tile
 constexpr int kBlockKeys = 32, kBlockPages = kBlockKeys / kPageTokens;
 
+template <int N>
+struct Int {
+  static constexpr int value = N;
+};
+
+// inclusive prefix sum over a wave: within rows of 16 lanes, then what lies in the rows before
+__device__ __forceinline__ int scan(int x) {
+  auto shifted = [](int v, auto ctrl, auto rows) __attribute__((always_inline)) {
+    return __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+  };
+  x += shifted(x, Int<0x111>{}, Int<0xf>{});                 // row_shr 1, 2, 4, 8
+  x += shifted(x, Int<0x112>{}, Int<0xf>{});
+  x += shifted(x, Int<0x114>{}, Int<0xf>{});
+  x += shifted(x, Int<0x118>{}, Int<0xf>{});
+  x += shifted(x, Int<0x142>{}, Int<0xa>{});                 // row_bcast 15: into rows 1 and 3
+  x += shifted(x, Int<0x143>{}, Int<0xc>{});                 // row_bcast 31: into rows 2 and 3
+  return x;
+}
+
 // What stands at one place of the line.
 struct At {
   int row, head, tile;
@@ -57,6 +76,54 @@ struct Line {
       at.len = at.row < batch ? valid(lens[at.row]) : 1;
     } while (at.len == 0);
     at.blocks = blocks(at.len);
+  }
+  // Blocks of all rows (of one head and tile), and the place `begin` of the line, found by the lanes: each sums up `per` rows,
+  // then those of the lane that has the place are searched 64 at a time.  (No sum overflows: rows x pages fits 31 bits.)
+  struct Sums {
+    int per, upto, mine, all;
+  };
+  __device__ __forceinline__ Sums sums() const {
+    const int lane = threadIdx.x & 63;
+    Sums s = {(batch + 63) / 64, 0, 0, 0};
+    for (int i = 0; i < s.per; ++i) {
+      const int r = lane * s.per + i;
+      const int n = blocks(valid(lens[r < batch ? r : batch - 1]));
+      s.mine += r < batch ? n : 0;
+    }
+    s.upto = scan(s.mine);
+    s.all = __builtin_amdgcn_readlane(s.upto, 63);
+    return s;
+  }
+  __device__ __forceinline__ At place(const Sums& s, int64_t begin) const {
+    const int lane = threadIdx.x & 63;
+    const int lines = heads * tiles;
+    const int whole = begin >> 31 == 0 ? (int)((uint32_t)begin / (uint32_t)lines) : (int)(begin / lines);       // of one head's line: finds the row
+    int k = __popcll(__builtin_amdgcn_ballot_w64(s.upto <= whole));
+    At at;
+    at.row = k * s.per;
+    int before = __builtin_amdgcn_readlane(s.upto - s.mine, k);
+    if (s.per > 1) {
+      for (;;) {
+        const int r = at.row + lane;
+        const int n = blocks(valid(lens[r < batch ? r : batch - 1])), mine = r < batch ? n : 0, upto = before + scan(mine);
+        k = __popcll(__builtin_amdgcn_ballot_w64(upto <= whole));
+        if (k < 64) {
+          at.row += k;
+          before = __builtin_amdgcn_readlane(upto - mine, k);
+          break;
+        }
+        at.row += 64;
+        before = __builtin_amdgcn_readlane(upto, 63);
+      }
+    }
+    at.len = valid(lens[at.row]);
+    at.blocks = blocks(at.len);
+    const int64_t off = begin - (int64_t)before * lines;
+    const int which = off >> 31 == 0 ? (int)((uint32_t)off / (uint32_t)at.blocks) : (int)(off / at.blocks);
+    at.block = (int)(off - (int64_t)which * at.blocks);
+    at.head = which / tiles;
+    at.tile = which - at.head * tiles;
+    return at;
   }
   // the table is never read past the row's pages
   __device__ __forceinline__ void pages_of(const At& at, int (&pid)[kBlockPages]) const {
@@ -87,9 +154,8 @@ struct Shape {
     char corner[kWaves][kCorner];           // a wave's block of keys in turn, then its last partial output
     float first[kWaves][kRows][kStride];    // its first
     float m[2][kWaves][kRows], l[2][kWaves][kRows];
-    int64_t before[kWaves * 64 + 1];        // blocks (of one head and tile) before each thread's share of the rows
-    int64_t of_wave[kWaves];
     Cut cut[kWaves];
+    int flags[kWaves];
     __device__ __forceinline__ float* o(int last, int wave, int row) {
       return last ? reinterpret_cast<float*>(corner[wave]) + row * kStride : first[wave][row];
     }
@@ -104,7 +170,7 @@ template <int D>
 struct Math<__bf16, D> {
   static constexpr int kSteps = D / 32, kVec = D / 16;
   typedef uint32_t vvec __attribute__((ext_vector_type(kVec / 2)));
-  bf16x8 qf[kSteps], ones;
+  bf16x8 qf[kSteps], ahead[kSteps], ones;
   f32x4 l;
   __device__ __forceinline__ Math() {
 #pragma unroll
@@ -112,9 +178,13 @@ struct Math<__bf16, D> {
   }
   __device__ __forceinline__ void query(const char* row, int g) {
 #pragma unroll
-    for (int c = 0; c < kSteps; ++c) qf[c] = *reinterpret_cast<const bf16x8*>(row + c * 64 + g * 16);
+    for (int c = 0; c < kSteps; ++c) ahead[c] = *reinterpret_cast<const bf16x8*>(row + c * 64 + g * 16);
   }
-  __device__ __forceinline__ void reset() { l = f32x4{0.f, 0.f, 0.f, 0.f}; }
+  __device__ __forceinline__ void reset() {
+    l = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < kSteps; ++c) qf[c] = ahead[c];
+  }
   __device__ __forceinline__ void rescale(float alpha) { l *= alpha; }
   __device__ __forceinline__ float sum() const { return l[0]; }
   template <typename Stage>
@@ -155,13 +225,17 @@ template <>
 struct Math<float, 64> {
   static constexpr int kVec = 4;
   typedef float vvec __attribute__((ext_vector_type(kVec)));
-  f32x4 qf[4];                              // step (i, e) of the contraction takes column 16 i + 4 g + e
+  f32x4 qf[4], ahead[4];                    // step (i, e) of the contraction takes column 16 i + 4 g + e
   float l;                                  // this lane group's keys
   __device__ __forceinline__ void query(const char* row, int g) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) qf[i] = *reinterpret_cast<const f32x4*>(row + i * 64 + g * 16);
+    for (int i = 0; i < 4; ++i) ahead[i] = *reinterpret_cast<const f32x4*>(row + i * 64 + g * 16);
   }
-  __device__ __forceinline__ void reset() { l = 0.f; }
+  __device__ __forceinline__ void reset() {
+    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) qf[i] = ahead[i];
+  }
   __device__ __forceinline__ void rescale(float alpha) { l *= alpha; }
   __device__ __forceinline__ float sum() const { return sum_with_other_half(l + __shfl_xor(l, 16, 64)); }
   template <typename Stage>
@@ -186,12 +260,6 @@ struct Math<float, 64> {
   }
 };
 
-// a value that all lanes agree on, in scalar registers
-__device__ __forceinline__ int64_t uniform(int64_t x) {
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
-  return (int64_t)(((uint64_t)hi << 32) | lo);
-}
-
 // kPer columns of a finished row
 template <typename T, int kPer>
 __device__ __forceinline__ void put_out(T* to, const float (&x)[kPer], float scale) {
@@ -202,7 +270,8 @@ __device__ __forceinline__ void put_out(T* to, const float (&x)[kPer], float sca
 }
 __device__ __forceinline__ float log_sum(float m, float l) { return (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f; }
 
-template <typename T, int D>
+// kRows form: a workgroup has one (row, head, tile), whose blocks its waves share, and nothing is left to join behind it.
+template <typename T, int D, bool kByRow>
 __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeArgs a) {
   typedef Shape<T, D> S;
   typedef Math<T, D> M;
@@ -214,87 +283,44 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeAr
   const Line line(a);
   const int64_t lines = (int64_t)a.Hkv * a.tiles;          // times a row's blocks stand in the line
 
-  // padding rows, shared out over the workgroups
-  for (int64_t base = blockIdx.x; base < a.batch; base += (int64_t)gridDim.x * kWaves * 64) {
-    const int64_t r = base + (int64_t)threadIdx.x * gridDim.x;
-    const bool empty = r < a.batch && line.valid(a.seq_lens[r]) == 0;
-    for (uint64_t some = __builtin_amdgcn_ballot_w64(empty); some != 0; some &= some - 1) {
-      const int64_t row = base + (int64_t)(wave * 64 + __builtin_ctzll(some)) * gridDim.x;
-      u32x4* to = reinterpret_cast<u32x4*>((char*)a.out + row * a.Hq * kRowB);
-      for (int64_t i = lane; i < (int64_t)a.Hq * kRowB / 16; i += 64) to[i] = u32x4{};
-      if (a.lse != nullptr)
-        for (int i = lane; i < a.Hq; i += 64) a.lse[row * a.Hq + i] = -INFINITY;
-    }
+  typename Line::Sums sums = {};
+  At own = {};                                             // (by row) the workgroup's place
+  if (kByRow) {
+    own.row = (int)(blockIdx.x / (uint32_t)lines);
+    const int which = (int)blockIdx.x - own.row * (int)lines;
+    own.head = which / a.tiles;
+    own.tile = which - own.head * a.tiles;
+    own.len = line.valid(line.lens[own.row]);
+    own.blocks = Line::blocks(own.len);
+  } else {
+    sums = line.sums();
   }
-
-  // the line: a thread sums up the blocks of its share of the rows
-  const int per = (a.batch + kWaves * 64 - 1) / (kWaves * 64);
-  int64_t mine = 0;
-  for (int i = 0; i < per; ++i) {
-    const int r = (int)threadIdx.x * per + i;
-    if (r < a.batch) mine += Line::blocks(line.valid(a.seq_lens[r]));
-  }
-  int64_t upto = mine;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t other = __shfl_up((long long)upto, d, 64);
-    upto += lane >= d ? other : 0;
-  }
-  if (lane == 63) sh.of_wave[wave] = upto;
-  __syncthreads();
-  int64_t all = 0, ahead = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    ahead += w < wave ? sh.of_wave[w] : 0;
-    all += sh.of_wave[w];
-  }
-  sh.before[threadIdx.x] = ahead + upto - mine;
-  __syncthreads();
-  const int64_t total = uniform(all) * lines;
-  const int n_waves = decode_waves(total, (int)gridDim.x * kWaves);
-  const int at_wave = (int)blockIdx.x * kWaves + wave;
+  const int64_t total = kByRow ? own.blocks : sums.all * lines;
+  const int n_waves = decode_waves(total, kByRow ? kWaves : (int)gridDim.x * kWaves);
+  const int at_wave = kByRow ? wave : (int)blockIdx.x * kWaves + wave;
   const int64_t begin = at_wave < n_waves ? decode_begin(total, at_wave, n_waves) : total;
   const int64_t end = at_wave < n_waves ? decode_begin(total, at_wave + 1, n_waves) : total;
 
   Cut cut = {0, 0, 0, 0, 0, 0, 0};
   if (begin < end) {
-    // where the stretch begins: the last share of rows that does not lie behind it, then row by row
-    int lo = 0, hi = kWaves * 64 - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (sh.before[mid] * lines <= begin) lo = mid; else hi = mid - 1;
-    }
-    lo = __builtin_amdgcn_readfirstlane(lo);
-    At at;
-    at.row = lo * per;
-    int64_t off = begin - uniform(sh.before[lo]) * lines;
-    at.len = line.valid(line.lens[at.row]);
-    while (off >= Line::blocks(at.len) * lines) {
-      off -= Line::blocks(at.len) * lines;
-      ++at.row;
-      at.len = line.valid(line.lens[at.row]);
-    }
-    at.blocks = Line::blocks(at.len);
-    const int which = (int)(off / at.blocks);
-    at.block = (int)(off - (int64_t)which * at.blocks);
-    at.head = which / a.tiles;
-    at.tile = which - at.head * a.tiles;
+    At at = own;
+    if (kByRow) at.block = (int)begin; else at = line.place(sums, begin);
 
     char* const k_lds = sh.corner[wave];
     const int64_t page_stride = (int64_t)a.Hkv * S::kPageHeadB;
     const uint32_t v_lane = (uint32_t)(4 * g * kRowB + j * (kVec * (int)sizeof(T)));
     StageK<kRowB, kBlockPages> stage;
-    typename M::vvec vr[8];                                // 4 page + r: key 4 g + r of that page
+    typename M::vvec v_even[8], v_odd[8];                  // 4 page + r: key 4 g + r of that page; of every other block
     auto load_k = [&](const At& of, const int (&pid)[kBlockPages]) __attribute__((always_inline)) {
-      stage.load(page_stride, reinterpret_cast<const char*>(a.k_pool) + (int64_t)of.head * S::kPageHeadB, pid);
+      stage.template load<true>(page_stride, reinterpret_cast<const char*>(a.k_pool) + (int64_t)of.head * S::kPageHeadB, pid);
     };
-    auto load_v = [&](const At& of, const int (&pid)[kBlockPages]) __attribute__((always_inline)) {
+    auto load_v = [&](const At& of, const int (&pid)[kBlockPages], typename M::vvec (&vr)[8]) __attribute__((always_inline)) {
       const char* base = reinterpret_cast<const char*>(a.v_pool) + (int64_t)of.head * S::kPageHeadB;
 #pragma unroll
       for (int h = 0; h < kBlockPages; ++h) {
         const char* page = base + (int64_t)pid[h] * page_stride;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) vr[4 * h + r] = *reinterpret_cast<const typename M::vvec*>(page + v_lane + r * kRowB);
+        for (int r = 0; r < 4; ++r) vr[4 * h + r] = __builtin_nontemporal_load(reinterpret_cast<const typename M::vvec*>(page + v_lane + r * kRowB));
       }
     };
     auto rows_of = [&](const At& of) __attribute__((always_inline)) {
@@ -306,9 +332,11 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeAr
     M math;
     f32x4 o[kVec];
     float m_run;
-    auto start = [&](const At& of) __attribute__((always_inline)) {
+    auto ask = [&](const At& of) __attribute__((always_inline)) {
       const int rows = rows_of(of);                        // rows past the last compute it again
       math.query(reinterpret_cast<const char*>(a.q) + (first_head(of) + (j < rows ? j : rows - 1)) * kRowB, g);
+    };
+    auto start = [&]() __attribute__((always_inline)) {    // with the queries asked for last
       math.reset();
       m_run = -INFINITY;
 #pragma unroll
@@ -340,19 +368,28 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeAr
     At nx = at;
     int pid[kBlockPages];
     line.pages_of(at, pid);
+    ask(at);
     load_k(at, pid);
-    load_v(at, pid);
-    start(at);
+    load_v(at, pid, v_even);
+    start();
     if (left > 1) line.next(nx);
     line.pages_of(nx, pid);
-    for (; left > 0; --left) {
-      // (Loads are never skipped: behind a branch the compiler could not count those in flight.  The last turn's nobody uses.)
+    // One block: its V has been asked for a turn ago, and the next block's K and V are asked for before anything is done with it.
+    // (Loads are never skipped: behind a branch the compiler could not count those in flight.  The last turn's nobody uses.)
+    auto turn = [&](typename M::vvec (&vr)[8], typename M::vvec (&v_next)[8], int64_t todo) __attribute__((always_inline)) {
       stage.put(k_lds);
+      if (nx.block == 0) ask(nx);                          // (ahead of all that is asked for below, so waited for with none of it)
       load_k(nx, pid);
+      load_v(nx, pid, v_next);
       wave_sees_lds();
       __builtin_amdgcn_sched_barrier(0);
       f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};     // keys 16 kt + 4 g + r of the block
       math.template scores<StageK<kRowB, kBlockPages>>(k_lds, s);
+      // (behind the fragments: the scalar unit's loads and those from LDS are waited for together)
+      __builtin_amdgcn_sched_barrier(0);
+      At nn = nx;
+      if (todo > 2) line.next(nn);
+      line.pages_of(nn, pid);
       if ((at.block + 1) * kBlockKeys > at.len) {          // slots at or past the length may hold anything
         asm volatile("");                                  // (a branch, not selects on every block's path)
         const int seen = at.len - at.block * kBlockKeys - 4 * g;
@@ -376,10 +413,6 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeAr
 #pragma unroll
       for (int q = 0; q < 8; ++q) s[q >> 2][q & 3] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q >> 2][q & 3], c, -ref));
       math.values(s, vr, o);
-      load_v(nx, pid);
-      At nn = nx;
-      if (left > 2) line.next(nn);
-      line.pages_of(nn, pid);
       wave_sees_lds();
       __builtin_amdgcn_sched_barrier(0);
       if (at.block + 1 == at.blocks) {
@@ -400,9 +433,9 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeAr
           keep(0);
           cut.has_first = 1;
         }
-        if (left > 1) start(nx);
+        start();
         whole = true;
-      } else if (left == 1) {
+      } else if (todo == 1) {
         keep(1);
         cut.has_last = 1;
         cut.through = !whole;
@@ -411,41 +444,72 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeAr
       }
       at = nx;
       nx = nn;
+    };
+    // (In pairs: with a way out between the two the compiler moves V from one set of registers to the other, and waits for it.)
+    for (; left > 1; left -= 2) {
+      turn(v_even, v_odd, left);
+      turn(v_odd, v_even, left - 1);
     }
+    if (left > 0) turn(v_even, v_odd, left);
   }
-  if (lane == 0) sh.cut[wave] = cut;
+  if (lane == 0) {
+    sh.cut[wave] = cut;
+    sh.flags[wave] = cut.has_first | cut.has_last << 8 | (cut.has_last & cut.through) << 16;
+  }
   __syncthreads();
 
-  // The workgroup's cut rows: the one that began before it, then those that begin in its waves.
+  // The workgroup's cut rows: the one that began before it, then those that begin in its waves.  A bit a wave:
+  int flags = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) flags |= sh.flags[w] << w;
+  flags = __builtin_amdgcn_readfirstlane(flags);
+  const int firsts = flags & 0xff, lasts = flags >> 8 & 0xff, throughs = flags >> 16;
   constexpr int kPer = kRows * D / (kWaves * 64);
   const int row = threadIdx.x / (D / kPer), col = threadIdx.x % (D / kPer) * kPer;
-  if (threadIdx.x == 0) a.meta[blockIdx.x] = DecodeMeta{0, 0, 0, 0};
-  for (int chain = -1; chain < kWaves; ++chain) {
+  if (!kByRow && threadIdx.x == 0) a.meta[blockIdx.x] = DecodeMeta{0, 0, 0, 0};
+  // bit 0 of `chains`: a row from before; bit w + 1: the one that wave w leaves open
+  for (int chains = ((firsts | throughs) & 1) | (lasts & ~throughs) << 1; chains != 0; chains &= chains - 1) {
+    const int chain = __builtin_ctz(chains) - 1;
     const bool front = chain < 0;
     const int from = front ? 0 : chain;
-    const Cut& head = sh.cut[from];
-    const bool ends_at_once = front && head.has_first;
-    if (!(ends_at_once || (head.has_last && (head.through != 0) == front))) continue;
-    int to = from;                                         // its last wave
-    bool closed = ends_at_once;
-    while (!closed && to + 1 < kWaves) {
-      ++to;
-      closed = sh.cut[to].has_first;
-    }
-    float top = -INFINITY;
-    for (int w = from; w <= to; ++w) top = fmaxf(top, sh.m[!(closed && w == to)][w][row]);
-    const float ref = top == -INFINITY ? 0.f : top;        // (every score is -inf or NaN)
-    float l = 0.f, x[kPer];
+    // its last wave: the next one that has a row's end, if any
+    const int ends = firsts >> (from + !front) << (from + !front);
+    const bool closed = ends != 0;
+    const int to = closed ? __builtin_ctz(ends) : kWaves - 1;
+    float top = -INFINITY, l = 0.f, x[kPer];
 #pragma unroll
     for (int e = 0; e < kPer; ++e) x[e] = 0.f;
-    for (int w = from; w <= to; ++w) {
-      const int last = !(closed && w == to);
-      const float weight = __builtin_amdgcn_exp2f(sh.m[last][w][row] - ref);
-      l += weight * sh.l[last][w][row];
-      const float* part = sh.o(last, w, row) + col;
+    auto add = [&](float m, float l_part, const float* part, float ref) __attribute__((always_inline)) {
+      const float weight = __builtin_amdgcn_exp2f(m - ref);
+      l += weight * l_part;
 #pragma unroll
       for (int e = 0; e < kPer; ++e) x[e] += weight * part[e];
+    };
+    if (to - from >= kWaves / 2) {
+      // many parts: all eight waves' are read at once (in place of what is none of this row's, one of its own again, for nothing)
+      float m[kWaves], ls[kWaves], parts[kWaves][kPer];
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const int at = w < from ? from : w > to ? to : w, last = !(closed && at == to);
+        m[w] = sh.m[last][at][row];
+        ls[w] = sh.l[last][at][row];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) parts[w][e] = sh.o(last, at, row)[col + e];
+        top = fmaxf(top, m[w]);
+      }
+      const float ref = top == -INFINITY ? 0.f : top;      // (every score is -inf or NaN)
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w)
+        if (w >= from && w <= to) add(m[w], ls[w], parts[w], ref);
+    } else {
+      for (int w = from; w <= to; ++w) top = fmaxf(top, sh.m[!(closed && w == to)][w][row]);
+      const float ref = top == -INFINITY ? 0.f : top;
+      for (int w = from; w <= to; ++w) {
+        const int last = !(closed && w == to);
+        add(sh.m[last][w][row], sh.l[last][w][row], sh.o(last, w, row) + col, ref);
+      }
     }
+    const Cut& head = sh.cut[from];
     if (closed && !front) {
       const int rows = a.G - head.tile * kRows;
       if (row < rows) {
@@ -455,6 +519,7 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeAr
       }
       continue;
     }
+    if (kByRow) continue;                                  // (not reached: a workgroup's row ends in it)
     const int64_t part = ((int64_t)blockIdx.x * 2 + (front ? 0 : 1)) * kRows + row;
     put_out<float, kPer>(a.o_parts + part * D + col, x, 1.0f);
     if (col == 0) a.ml_parts[part] = float2{top, l};
@@ -464,45 +529,119 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeAr
       a.meta[blockIdx.x] = DecodeMeta{decode_wave_of(total, last, n_waves) / kWaves - (int)blockIdx.x, head.row, head.head, head.tile};
     }
   }
+
+  // padding rows, shared out over the workgroups
+  auto clear = [&](int64_t row) __attribute__((always_inline)) {
+    u32x4* to = reinterpret_cast<u32x4*>((char*)a.out + row * a.Hq * kRowB);
+    for (int64_t i = lane; i < (int64_t)a.Hq * kRowB / 16; i += 64) to[i] = u32x4{};
+    if (a.lse != nullptr)
+      for (int i = lane; i < a.Hq; i += 64) a.lse[row * a.Hq + i] = -INFINITY;
+  };
+  if (kByRow) {
+    if (own.len == 0 && own.head == 0 && own.tile == 0 && wave == 0) clear(own.row);
+    return;
+  }
+  for (int64_t base = blockIdx.x; base < a.batch; base += (int64_t)gridDim.x * kWaves * 64) {
+    const int64_t r = base + (int64_t)threadIdx.x * gridDim.x;
+    const bool empty = r < a.batch && line.valid(a.seq_lens[r]) == 0;
+    for (uint64_t some = __builtin_amdgcn_ballot_w64(empty); some != 0; some &= some - 1)
+      clear(base + (int64_t)(wave * 64 + __builtin_ctzll(some)) * gridDim.x);
+  }
 }
 
-// Rows that several workgroups have parts of: one wave a query head.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void attn_decode_join_kernel(const DecodeArgs a) {
-  const int wg = blockIdx.x / (kRows / 4);
-  const DecodeMeta meta = a.meta[wg];
-  const int row = blockIdx.x % (kRows / 4) * 4 + threadIdx.x / 64, lane = threadIdx.x & 63;
-  if (meta.more == 0 || meta.tile * kRows + row >= a.G) return;
-  constexpr int kPer = D / 64;
-  typedef float fvec __attribute__((ext_vector_type(kPer)));
-  auto part_of = [&](int i) { return ((int64_t)(wg + i) * 2 + (i == 0 ? 1 : 0)) * kRows + row; };
-  float top = -INFINITY;
-  for (int i = lane; i <= meta.more; i += 64) top = fmaxf(top, a.ml_parts[part_of(i)].x);
+// Rows that several workgroups have parts of: workgroup w joins what goes on behind workgroup w of the other kernel.  Its waves
+// take every eighth part, all query heads of it; then they are joined as a workgroup's parts are.
+template <typename T, int D, int ROWS>
+__global__ __launch_bounds__(kWaves * 64) void attn_decode_join_kernel(const DecodeArgs a) {
+  constexpr int kStride = D + 4, kLoads = ROWS * D / 256;  // 16-byte loads of a lane for a part: element 256 k + 4 lane of its rows
+  constexpr int kAtOnce = kLoads > 4 ? 2 : 4;              // parts whose loads are in flight together
+  __shared__ __attribute__((aligned(16))) float outs[kWaves][ROWS][kStride];
+  __shared__ float tops[kWaves][ROWS], sums[kWaves][ROWS];
+  const DecodeMeta meta = a.meta[blockIdx.x];
+  if (meta.more == 0) return;
+  const int wave = threadIdx.x / 64, lane = threadIdx.x & 63;
+  float top[kLoads], l[kLoads];
+  f32x4 x[kLoads];
 #pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-  const float ref = top == -INFINITY ? 0.f : top;
-  float l = 0.f, x[kPer];
+  for (int k = 0; k < kLoads; ++k) {
+    top[k] = -INFINITY;
+    l[k] = 0.f;
+    x[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  for (int base = wave; base <= meta.more; base += kWaves * kAtOnce) {
+    f32x4 v[kAtOnce][kLoads];
+    float2 ml[kAtOnce][kLoads];
 #pragma unroll
-  for (int e = 0; e < kPer; ++e) x[e] = 0.f;
-#pragma unroll 4
-  for (int i = 0; i <= meta.more; ++i) {
-    const int64_t part = part_of(i);
-    const float2 ml = a.ml_parts[part];
-    const float weight = __builtin_amdgcn_exp2f(ml.x - ref);
-    l += weight * ml.y;
-    const fvec v = *reinterpret_cast<const fvec*>(a.o_parts + part * D + lane * kPer);
+    for (int n = 0; n < kAtOnce; ++n) {
+      int i = base + n * kWaves;
+      i = i <= meta.more ? i : base;                       // (behind the last: one again, for nothing)
+      const int64_t part = (((int64_t)blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * kRows;
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) x[e] += weight * v[e];
+      for (int k = 0; k < kLoads; ++k) {
+        const int at = 256 * k + 4 * lane;
+        v[n][k] = *reinterpret_cast<const f32x4*>(a.o_parts + part * D + at);
+        ml[n][k] = a.ml_parts[part + at / D];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      float most = top[k];
+#pragma unroll
+      for (int n = 0; n < kAtOnce; ++n) most = fmaxf(most, ml[n][k].x);
+      const float ref = most == -INFINITY ? 0.f : most;    // (every score so far is -inf or NaN)
+      const float before = __builtin_amdgcn_exp2f(top[k] - ref);
+      l[k] *= before;
+      x[k] *= before;
+      top[k] = most;
+#pragma unroll
+      for (int n = 0; n < kAtOnce; ++n) {
+        if (base + n * kWaves > meta.more) break;
+        const float weight = __builtin_amdgcn_exp2f(ml[n][k].x - ref);
+        l[k] += weight * ml[n][k].y;
+        x[k] += weight * v[n][k];
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kLoads; ++k) {
+    const int at = 256 * k + 4 * lane, row = at / D;
+    *reinterpret_cast<f32x4*>(&outs[wave][row][at % D]) = x[k];
+    if (at % D == 0) {
+      tops[wave][row] = top[k];
+      sums[wave][row] = l[k];
+    }
+  }
+  __syncthreads();
+  constexpr int kPer = ROWS * D / (kWaves * 64);
+  const int row = threadIdx.x / (D / kPer), col = threadIdx.x % (D / kPer) * kPer;
+  if (meta.tile * kRows + row >= a.G) return;
+  float most = tops[0][row], sum = 0.f, y[kPer];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) most = fmaxf(most, tops[w][row]);
+  const float ref = most == -INFINITY ? 0.f : most;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) y[e] = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const float weight = __builtin_amdgcn_exp2f(tops[w][row] - ref);
+    sum += weight * sums[w][row];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) y[e] += weight * outs[w][row][col + e];
   }
   const int64_t at = (int64_t)meta.row * a.Hq + meta.head * a.G + meta.tile * kRows + row;
-  put_out<T, kPer>(reinterpret_cast<T*>(a.out) + at * D + lane * kPer, x, 1.0f / l);
-  if (a.lse != nullptr && lane == 0) a.lse[at] = log_sum(top, l);
+  put_out<T, kPer>(reinterpret_cast<T*>(a.out) + at * D + col, y, 1.0f / sum);
+  if (a.lse != nullptr && col == 0) a.lse[at] = log_sum(most, sum);
 }
 
 template <typename T, int D>
 void enqueue(const DecodeArgs& args, hipStream_t stream) {
-  attn_decode_kernel<T, D><<<kDecodeWgs, kWaves * 64, 0, stream>>>(args);
-  attn_decode_join_kernel<T, D><<<kDecodeWgs * (kRows / 4), 256, 0, stream>>>(args);
+  if (args.by_row) {
+    attn_decode_kernel<T, D, true><<<args.batch * args.Hkv * args.tiles, kWaves * 64, 0, stream>>>(args);
+    return;
+  }
+  attn_decode_kernel<T, D, false><<<kDecodeWgs, kWaves * 64, 0, stream>>>(args);
+  if (args.G <= kRows / 2) attn_decode_join_kernel<T, D, kRows / 2><<<kDecodeWgs, kWaves * 64, 0, stream>>>(args);
+  else attn_decode_join_kernel<T, D, kRows><<<kDecodeWgs, kWaves * 64, 0, stream>>>(args);
 }
 
 }  // namespace

@@ -42,13 +42,17 @@ struct StageK {
   static constexpr int kChunks = kPageTokens * ROW_BYTES / 1024, kSteps = ROW_BYTES / 64;
   static __device__ __forceinline__ int swz(int row) { return (row >> kShift) & (kGran - 1); }
   u32x4 raw[PAGES][kChunks];
+  template <bool ONCE = false>
   __device__ __forceinline__ void load(int64_t page_stride, const char* kbase, const int (&pid)[PAGES]) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int h = 0; h < PAGES; ++h) {
       const char* page = kbase + (int64_t)pid[h] * page_stride;
 #pragma unroll
-      for (int i = 0; i < kChunks; ++i) raw[h][i] = *reinterpret_cast<const u32x4*>(page + (uint32_t)(lane * 16) + i * 1024);
+      for (int i = 0; i < kChunks; ++i) {
+        const u32x4* const at = reinterpret_cast<const u32x4*>(page + (uint32_t)(lane * 16) + i * 1024);
+        raw[h][i] = ONCE ? __builtin_nontemporal_load(at) : *at;
+      }
     }
   }
   __device__ __forceinline__ void put(char* lds) const {

@@ -174,6 +174,8 @@ struct DecodeLayout {
   size_t ml_off, meta_off, total;
 };
 DecodeLayout decode_layout(const mc_attn_params* p);
+// Whether a decode call of so many (row, KV head, tile) and so wide a table gives each a workgroup of its own.
+bool decode_by_row(int64_t items, int32_t max_pages);
 
 // Sizes and addresses of a call on a cache's pages.
 mc_status check_pages(const int32_t* ref_counts, int64_t num_pages, const int32_t* block_tables, int32_t max_pages_per_req,

@@ -803,6 +803,7 @@ mc_status mc_decode_attn_paged(const mc_attn_params* p, const void* q, const voi
   args.batch = batch;
   args.max_pages = max_pages_per_req;
   args.scale_log2e = attn_scale_log2e(p);
+  args.by_row = decode_by_row((int64_t)batch * p->num_kv_heads * args.tiles, max_pages_per_req);
   return mc::launch_attn_decode(p->dtype, p->head_dim, args, reinterpret_cast<hipStream_t>(hip_stream)) == hipSuccess ? MC_OK : MC_ERR_HIP;
 }
 

@@ -110,6 +110,7 @@ struct DecodeArgs {
   DecodeMeta* meta;    // [kDecodeWgs]
   int32_t Hq, Hkv, G, tiles, batch, max_pages;
   float scale_log2e;
+  bool by_row;         // a workgroup a (row, KV head, tile of query heads) instead of equal stretches of the line
 };
 hipError_t launch_attn_decode(int dtype, int head_dim, const DecodeArgs& args, hipStream_t stream);
 
