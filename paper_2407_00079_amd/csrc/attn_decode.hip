@@ -81,14 +81,15 @@ struct Line {
   // then those of the lane that has the place are searched 64 at a time.  (No sum overflows: rows x pages fits 31 bits.)
   struct Sums {
     int per, upto, mine, all;
+    int len;                                                 // of the lane's last row
   };
   __device__ __forceinline__ Sums sums() const {
     const int lane = threadIdx.x & 63;
-    Sums s = {(batch + 63) / 64, 0, 0, 0};
+    Sums s = {(batch + 63) / 64, 0, 0, 0, 0};
     for (int i = 0; i < s.per; ++i) {
       const int r = lane * s.per + i;
-      const int n = blocks(valid(lens[r < batch ? r : batch - 1]));
-      s.mine += r < batch ? n : 0;
+      s.len = valid(lens[r < batch ? r : batch - 1]);
+      s.mine += r < batch ? blocks(s.len) : 0;
     }
     s.upto = scan(s.mine);
     s.all = __builtin_amdgcn_readlane(s.upto, 63);
@@ -102,21 +103,22 @@ struct Line {
     At at;
     at.row = k * s.per;
     int before = __builtin_amdgcn_readlane(s.upto - s.mine, k);
+    at.len = __builtin_amdgcn_readlane(s.len, k);
     if (s.per > 1) {
       for (;;) {
-        const int r = at.row + lane;
-        const int n = blocks(valid(lens[r < batch ? r : batch - 1])), mine = r < batch ? n : 0, upto = before + scan(mine);
+        const int r = at.row + lane, len = valid(lens[r < batch ? r : batch - 1]);
+        const int mine = r < batch ? blocks(len) : 0, upto = before + scan(mine);
         k = __popcll(__builtin_amdgcn_ballot_w64(upto <= whole));
         if (k < 64) {
           at.row += k;
           before = __builtin_amdgcn_readlane(upto - mine, k);
+          at.len = __builtin_amdgcn_readlane(len, k);
           break;
         }
         at.row += 64;
         before = __builtin_amdgcn_readlane(upto, 63);
       }
     }
-    at.len = valid(lens[at.row]);
     at.blocks = blocks(at.len);
     const int64_t off = begin - (int64_t)before * lines;
     const int which = off >> 31 == 0 ? (int)((uint32_t)off / (uint32_t)at.blocks) : (int)(off / at.blocks);

@@ -305,25 +305,26 @@ __global__ __launch_bounds__(256) void pages_remap_kernel(const PagesArgs a, con
   }
 }
 
-// Pages of all layers by a list of moves.  A workgroup takes slices of 8 KiB of one pool's page, all of K and V of a move's layer
-// next to each other; what bounds it is the HBM's rate for a read and write mix (kv_copy.hip).
+// Pages of all layers by a list of moves: a workgroup takes an 8 KiB slice of one pool's page, in the order of the list (a
+// compaction's sources ascend), pool after pool.  What bounds it is the HBM's rate for a read and write mix (kv_copy.hip).  Forks of
+// one row copy one page many times, so it is read through the caches: 240 forks over 32 layers 128 us a pass, with the nt hint on
+// the loads too 199; 4000 moves of 8 layers 741 and 709.  Workgroups that go round leave the order in which addresses are
+// touched to chance: two slices in flight a thread 781, four 800 us, a persistent grid over all pools 820.
 constexpr int kCopyThreads = 512;
-__global__ __launch_bounds__(kCopyThreads) void pages_copy_kernel(const LayerPools pools, int n_layers, int64_t num_pages, int64_t page_vecs,
+__global__ __launch_bounds__(kCopyThreads) void pages_copy_kernel(const LayerPools pools, int64_t num_pages, int64_t page_vecs,
                                                                   const int32_t* __restrict__ moves, const int32_t* __restrict__ count, int n,
                                                                   int slices) {
   int todo = count != nullptr ? *count : n;
   todo = todo < 0 ? 0 : todo < n ? todo : n;
-  const int64_t all = (int64_t)todo * n_layers * 2 * slices;
+  u32x4* const base = reinterpret_cast<u32x4*>(pools.at[blockIdx.y]);
+  const int64_t all = (int64_t)todo * slices;
   for (int64_t unit = blockIdx.x; unit < all; unit += gridDim.x) {
-    const int slice = (int)(unit % slices);
-    const int64_t rest = unit / slices;
-    const int pool = (int)(rest % (2 * n_layers));
-    const int64_t move = rest / (2 * n_layers);
+    const int64_t move = unit >> 31 == 0 ? (int64_t)((uint32_t)unit / (uint32_t)slices) : unit / slices;
+    const int slice = (int)(unit - move * slices);
     const int src = moves[2 * move], dst = moves[2 * move + 1];
     if (src < 0 || src >= num_pages || dst < 0 || dst >= num_pages) continue;
-    u32x4* base = reinterpret_cast<u32x4*>(pools.at[pool]);
     const int64_t vec = (int64_t)slice * kCopyThreads + threadIdx.x;
-    if (vec < page_vecs) __builtin_nontemporal_store(__builtin_nontemporal_load(base + src * page_vecs + vec), base + dst * page_vecs + vec);
+    if (vec < page_vecs) __builtin_nontemporal_store(base[src * page_vecs + vec], base + dst * page_vecs + vec);
   }
 }
 
@@ -371,9 +372,11 @@ hipError_t launch_pages_copy(const LayerPools& pools, int n_layers, int64_t num_
   (void)hipGetLastError();
   const int64_t page_vecs = page_bytes / 16;
   const int slices = (int)((page_vecs + kCopyThreads - 1) / kCopyThreads);
-  const int64_t all = (int64_t)n * n_layers * 2 * slices;
-  pages_copy_kernel<<<(unsigned)(all < 8192 ? all : 8192), kCopyThreads, 0, stream>>>(pools, n_layers, num_pages, page_vecs, moves, count, n,
-                                                                                   slices);
+  // n is what the list may hold, not what it does: a workgroup a slice, but not more than take about 60 us if there is none (0.43
+  // ns each); beyond that they go round.
+  const int64_t units = (int64_t)n * slices, most = (1 << 17) / (2 * n_layers);
+  const dim3 grid((unsigned)(units < most ? units : most), (unsigned)(2 * n_layers));
+  pages_copy_kernel<<<grid, kCopyThreads, 0, stream>>>(pools, num_pages, page_vecs, moves, count, n, slices);
   return hipGetLastError();
 }
 

@@ -9,8 +9,8 @@
 //     I  a list of n integers as int32[n], or an integer address
 //     Q  a list of n integers as int64[n], or an integer address
 //
-// and two looks at tensors before a call, made here because a dozen of them through Python cost more than the call itself (one
-// new token a row, rotation and append: 11.1 us of it on the host, now 5.6):
+// and two looks at tensors before a call, made here because a dozen of them through Python are a sixth of a small call (one new
+// token a row, rotation and append, launch included: 8.9 us of the host, so 7.6):
 //
 //   misfit(device, dtype, tensor, least, tensor, least, ...) -> the first that is not a dense tensor of dtype on the device with
 //                                                              at least so many elements, or -1
