@@ -66,7 +66,7 @@ class Device:
 
 # pages, rows, columns, tokens a page, filled
 SIZES = [(1, 1, 1, 16, 1.0), (40, 5, 6, 16, 0.5), (300, 33, 20, 16, 0.6), (4096, 40, 90, 16, 0.5), (4097, 70, 90, 1, 0.4), (9000, 200, 60, 7, 0.7),
-         (20000, 1300, 30, 16, 0.5)]
+         (16384, 60, 200, 16, 0.5), (16385, 60, 200, 16, 0.5), (9000, 400, 130, 16, 0.8), (20000, 1300, 30, 16, 0.5), (40000, 300, 220, 16, 0.6)]
 
 
 @pytest.mark.parametrize("pages,rows,wide,page,fill", SIZES)
