@@ -466,70 +466,65 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeAr
   for (int w = 0; w < kWaves; ++w) flags |= sh.flags[w] << w;
   flags = __builtin_amdgcn_readfirstlane(flags);
   const int firsts = flags & 0xff, lasts = flags >> 8 & 0xff, throughs = flags >> 16;
-  constexpr int kPer = kRows * D / (kWaves * 64);
-  const int row = threadIdx.x / (D / kPer), col = threadIdx.x % (D / kPer) * kPer;
-  if (!kByRow && threadIdx.x == 0) a.meta[blockIdx.x] = DecodeMeta{0, 0, 0, 0};
   // bit 0 of `chains`: a row from before; bit w + 1: the one that wave w leaves open
-  for (int chains = ((firsts | throughs) & 1) | (lasts & ~throughs) << 1; chains != 0; chains &= chains - 1) {
-    const int chain = __builtin_ctz(chains) - 1;
-    const bool front = chain < 0;
-    const int from = front ? 0 : chain;
-    // its last wave: the next one that has a row's end, if any
-    const int ends = firsts >> (from + !front) << (from + !front);
-    const bool closed = ends != 0;
-    const int to = closed ? __builtin_ctz(ends) : kWaves - 1;
-    float top = -INFINITY, l = 0.f, x[kPer];
+  const int chains = ((firsts | throughs) & 1) | (lasts & ~throughs) << 1;
+  // (the last of them goes on behind the workgroup if no row ends after it began)
+  if (!kByRow && threadIdx.x == 0 && (chains < 2 || firsts >> (31 - __builtin_clz(chains | 1)) != 0)) a.meta[blockIdx.x] = DecodeMeta{0, 0, 0, 0};
+  // Its threads `first` .. by `step` join 4 columns each of the parts of up to N waves, all read at once; in place of what is
+  // none of this row's one of its own is read again, for nothing.
+  auto join = [&](auto many, int bit, int to, bool closed, int first, int step) __attribute__((always_inline)) {
+    constexpr int N = decltype(many)::value;
+    const bool front = bit == 0;
+    const int from = front ? 0 : bit - 1;
+    const Cut head = sh.cut[from];
+    const int left = front ? a.G : a.G - head.tile * kRows, rows = left < kRows ? left : kRows;   // (from before: the tile is not known)
+    const int64_t part0 = ((int64_t)blockIdx.x * 2 + (front ? 0 : 1)) * kRows;
+    const int64_t out0 = (int64_t)head.row * a.Hq + head.head * a.G + head.tile * kRows;
+    for (int at = 4 * first; at < rows * D; at += 4 * step) {
+      const int row = at / D, col = at % D;
+      float m[N], ls[N], top = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+      f32x4 parts[N];
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) x[e] = 0.f;
-    auto add = [&](float m, float l_part, const float* part, float ref) __attribute__((always_inline)) {
-      const float weight = __builtin_amdgcn_exp2f(m - ref);
-      l += weight * l_part;
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) x[e] += weight * part[e];
-    };
-    if (to - from >= kWaves / 2) {
-      // many parts: all eight waves' are read at once (in place of what is none of this row's, one of its own again, for nothing)
-      float m[kWaves], ls[kWaves], parts[kWaves][kPer];
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const int at = w < from ? from : w > to ? to : w, last = !(closed && at == to);
-        m[w] = sh.m[last][at][row];
-        ls[w] = sh.l[last][at][row];
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) parts[w][e] = sh.o(last, at, row)[col + e];
-        top = fmaxf(top, m[w]);
+      for (int n = 0; n < N; ++n) {
+        const int w = from + n < to ? from + n : to, last = !(closed && w == to);
+        m[n] = sh.m[last][w][row];
+        ls[n] = sh.l[last][w][row];
+        parts[n] = *reinterpret_cast<const f32x4*>(sh.o(last, w, row) + col);
       }
+#pragma unroll
+      for (int n = 0; n < N; ++n) top = fmaxf(top, m[n]);
       const float ref = top == -INFINITY ? 0.f : top;      // (every score is -inf or NaN)
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w)
-        if (w >= from && w <= to) add(m[w], ls[w], parts[w], ref);
-    } else {
-      for (int w = from; w <= to; ++w) top = fmaxf(top, sh.m[!(closed && w == to)][w][row]);
-      const float ref = top == -INFINITY ? 0.f : top;
-      for (int w = from; w <= to; ++w) {
-        const int last = !(closed && w == to);
-        add(sh.m[last][w][row], sh.l[last][w][row], sh.o(last, w, row) + col, ref);
+      for (int n = 0; n < N; ++n) {
+        if (from + n > to) break;
+        const float weight = __builtin_amdgcn_exp2f(m[n] - ref);
+        l += weight * ls[n];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] += weight * parts[n][e];
+      }
+      if (closed && !front) {
+        put_out<T, 4>(reinterpret_cast<T*>(a.out) + (out0 + row) * D + col, x, 1.0f / l);
+        if (a.lse != nullptr && col == 0) a.lse[out0 + row] = log_sum(top, l);
+      } else if (!kByRow) {                                // (by row nothing goes on behind a workgroup)
+        put_out<float, 4>(a.o_parts + (part0 + row) * D + col, x, 1.0f);
+        if (col == 0) a.ml_parts[part0 + row] = float2{top, l};
       }
     }
-    const Cut& head = sh.cut[from];
-    if (closed && !front) {
-      const int rows = a.G - head.tile * kRows;
-      if (row < rows) {
-        const int64_t at = (int64_t)head.row * a.Hq + head.head * a.G + head.tile * kRows + row;
-        put_out<T, kPer>(reinterpret_cast<T*>(a.out) + at * D + col, x, 1.0f / l);
-        if (a.lse != nullptr && col == 0) a.lse[at] = log_sum(top, l);
-      }
-      continue;
-    }
-    if (kByRow) continue;                                  // (not reached: a workgroup's row ends in it)
-    const int64_t part = ((int64_t)blockIdx.x * 2 + (front ? 0 : 1)) * kRows + row;
-    put_out<float, kPer>(a.o_parts + part * D + col, x, 1.0f);
-    if (col == 0) a.ml_parts[part] = float2{top, l};
-    if (!front && threadIdx.x == 0) {
-      // (it goes on behind the workgroup: the last wave's stretch ends the workgroup's)
+    if (!kByRow && !front && !closed && first == 0) {
+      // (the last wave's stretch ends the workgroup's)
       const int64_t last = decode_begin(total, (int)(blockIdx.x + 1) * kWaves, n_waves) + sh.cut[kWaves - 1].rest - 1;
       a.meta[blockIdx.x] = DecodeMeta{decode_wave_of(total, last, n_waves) / kWaves - (int)blockIdx.x, head.row, head.head, head.tile};
     }
+  };
+  // A row of many waves (one at most) by all of them, the others a wave each.
+  for (int rest = chains; rest != 0; rest &= rest - 1) {
+    const int bit = __builtin_ctz(rest), from = bit == 0 ? 0 : bit - 1;
+    // its last wave: the next one that has a row's end, if any
+    const int ends = firsts >> bit << bit;
+    const bool closed = ends != 0;
+    const int to = closed ? __builtin_ctz(ends) : kWaves - 1;
+    if (to - from >= kWaves / 2) join(Int<kWaves>{}, bit, to, closed, threadIdx.x, kWaves * 64);
+    else if (bit % kWaves == wave) join(Int<kWaves / 2>{}, bit, to, closed, lane, 64);
   }
 
   // padding rows, shared out over the workgroups
