@@ -1,8 +1,10 @@
 /*
  * mc.h - C ABI of the MI355X (gfx950) KVCache-reuse hot path.
  *
- * Three operations behind Mooncake's KVCache reuse, as the paper states the
- * problem (it gives no kernel design):
+ * The operations behind Mooncake's KVCache reuse, as the paper states the
+ * problem (it gives no kernel design), and what a serving program does with the
+ * same cache before and after them (head norms and positions, attention of single
+ * new tokens, the care of the pages):
  *
  *   - a prefill node is handed the ids of the prefix blocks it may reuse and of
  *     all blocks of the request, loads the former and computes prefill for the
@@ -429,8 +431,8 @@ mc_status mc_kv_rope_append_decode(const mc_attn_params* p, const mc_rope_params
  *                     may overlap, and captured graphs that may, need one each
  *
  * Slots at or past a row's length are never used as values (they may hold NaN).  fp32 accumulation and softmax; output rounded
- * once, to nearest even.  The same lengths and inputs give the same bits.  batch * Hq > 2^26 is MC_ERR_RANGE; batch == 0 enqueues
- * nothing.  Nothing is allocated, uploaded or waited for; the call can be captured.
+ * once, to nearest even.  The same lengths and inputs give the same bits.  batch * Hq > 2^26, or tables so wide that all rows' blocks
+ * of 32 keys times Hq exceed 2^51, is MC_ERR_RANGE; batch == 0 enqueues nothing.  Nothing is allocated, uploaded or waited for; the call can be captured.
  */
 size_t mc_decode_attn_workspace_bytes(const mc_attn_params* p, int32_t batch);
 mc_status mc_decode_attn_paged(const mc_attn_params* p, const void* q, const void* k_pool, const void* v_pool,

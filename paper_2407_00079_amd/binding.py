@@ -675,6 +675,15 @@ def _dense(names: str, device: int, dtype, *tensors) -> None:
                          f"not {_is(tensors[2 * bad])}")
 
 
+def _here(device: int, workspace) -> None:
+    """The tensors' device has to be the current one (streams and launches are its own), and the workspace has to lie there."""
+    current = _device() if _device is not None else _torch.cuda.current_device() if _torch.cuda.is_initialized() else device
+    if device != current:
+        raise ValueError(f"tensors on device {device}, but the current device is {current}")
+    if workspace is not None and (workspace.get_device() != device or not workspace.is_contiguous()):
+        raise ValueError(f"workspace: a dense tensor on device {device} wanted, not {_is(workspace)}")
+
+
 def _pool_size(params) -> int:
     return params.num_pages * params.num_kv_heads * params.page_size * params.head_dim
 
@@ -724,6 +733,7 @@ def mc_kv_rope_append_paged(params: McAttnParams, rope: McRopeParams, q, k, v, q
     device, strides = _rope_tensors(_params(params), q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, sum(new_lens))
     wide = _table(block_tables, n)
     _dense("block_tables", device, _torch.int32, block_tables, 0)
+    _here(device, workspace)
     _enqueue("mc_kv_rope_append_paged", params, _rope(rope), q, k, v, strides, q_norm, k_norm, q_out, k_pool, v_pool, block_tables, wide,
              _ints("i", prefix_lens, n), _ints("i", new_lens, n), n, workspace, _nbytes(workspace),
              _on(stream))
@@ -735,6 +745,7 @@ def mc_kv_rope_append_run(params: McAttnParams, plan: McAttnPlan, rope: McRopePa
     device, strides = _rope_tensors(_params(params), q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, _plan(plan).total_new_tokens)
     wide = _table(block_tables, plan.batch)
     _dense("block_tables", device, _torch.int32, block_tables, 0)
+    _here(device, workspace)
     _enqueue("mc_kv_rope_append_run", params, plan, _rope(rope), q, k, v, strides, q_norm, k_norm, q_out, k_pool, v_pool, block_tables, wide,
              workspace, _on(stream))
 
@@ -742,10 +753,11 @@ def mc_kv_rope_append_run(params: McAttnParams, plan: McAttnPlan, rope: McRopePa
 def mc_kv_rope_append_decode(params: McAttnParams, rope: McRopeParams, q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, block_tables,
                              seq_lens, stream=None) -> None:
     """The same for one new token a row, at position ``seq_lens[r] - 1``; ``seq_lens``: int32 device tensor."""
-    n = seq_lens.shape[0]
+    n = seq_lens.numel()
     device, strides = _rope_tensors(_params(params), q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, n)
     wide = _table(block_tables, n)
     _dense("seq_lens block_tables", device, _torch.int32, seq_lens, n, block_tables, 0)
+    _here(device, None)
     _enqueue("mc_kv_rope_append_decode", params, _rope(rope), q, k, v, strides, q_norm, k_norm, q_out, k_pool, v_pool, block_tables, wide,
              seq_lens, n, _on(stream))
 
@@ -757,12 +769,14 @@ def mc_decode_attn_workspace_bytes(params: McAttnParams, batch: int) -> int:
 def mc_decode_attn_paged(params: McAttnParams, q, k_pool, v_pool, block_tables, seq_lens, out, lse, workspace, stream=None) -> None:
     """Enqueue attention of one new token a row: q, out [rows, heads, head_dim], ``seq_lens`` int32 device tensor [rows]."""
     dtype = (_DTYPES or _dtypes())[_params(params).dtype]
-    n, heads, wide = seq_lens.shape[0], params.num_q_heads, _table(block_tables, seq_lens.shape[0])
+    n, heads = seq_lens.numel(), params.num_q_heads
+    wide = _table(block_tables, n)
     device, size, pool = q.get_device(), n * heads * params.head_dim, _pool_size(params)
     _dense("q k_pool v_pool out", device, dtype, q, size, k_pool, pool, v_pool, pool, out, size)
     _dense("seq_lens block_tables", device, _torch.int32, seq_lens, n, block_tables, 0)
     if lse is not None:
         _dense("lse", device, _torch.float32, lse, n * heads)
+    _here(device, workspace)
     _enqueue("mc_decode_attn_paged", params, q, k_pool, v_pool, block_tables, wide, seq_lens, n, out, lse, workspace, _nbytes(workspace),
              _on(stream))
 
@@ -771,34 +785,35 @@ def mc_kv_pages_workspace_bytes(num_pages: int, rows: int) -> int:
     return int(lib().mc_kv_pages_workspace_bytes(num_pages, rows))
 
 
-def _state(ref_counts, block_tables, page_size: int, seq_lens, names: str, *more):
+def _state(ref_counts, block_tables, page_size: int, seq_lens, workspace, names: str, *more):
     """Looks a cache's bookkeeping over, and the int32 tensors that follow with what is used of each: the seven arguments that
     stand for it."""
     if _torch is None:
         _dtypes()
-    rows = seq_lens.shape[0]
+    rows, device = seq_lens.numel(), ref_counts.get_device()
     wide = _table(block_tables, rows)
-    _dense("ref_counts block_tables seq_lens " + names, ref_counts.get_device(), _torch.int32, ref_counts, 0, block_tables, 0, seq_lens, rows, *more)
+    _dense("ref_counts block_tables seq_lens " + names, device, _torch.int32, ref_counts, 0, block_tables, 0, seq_lens, rows, *more)
+    _here(device, workspace)
     return ref_counts, ref_counts.numel(), block_tables, wide, page_size, seq_lens, rows
 
 
 def mc_kv_pages_fork(ref_counts, block_tables, page_size: int, seq_lens, src_rows, dst_rows, moves, report, workspace, stream=None) -> None:
     """Enqueue rows ``dst_rows`` becoming copies of ``src_rows``; all int32 device tensors, ``moves`` [n, 2], ``report`` [4]."""
     n = src_rows.numel()
-    state = _state(ref_counts, block_tables, page_size, seq_lens, "src_rows dst_rows moves report", src_rows, n, dst_rows, n, moves, 2 * n, report, 4)
+    state = _state(ref_counts, block_tables, page_size, seq_lens, workspace, "src_rows dst_rows moves report", src_rows, n, dst_rows, n, moves, 2 * n, report, 4)
     _enqueue("mc_kv_pages_fork", *state, src_rows, dst_rows, n, moves, report, workspace, _nbytes(workspace), _on(stream))
 
 
 def mc_kv_pages_grow(ref_counts, block_tables, page_size: int, seq_lens, add, report, workspace, stream=None) -> None:
     """Enqueue row r getting ``add[r]`` more tokens, and the pages that takes."""
-    state = _state(ref_counts, block_tables, page_size, seq_lens, "add report", add, seq_lens.shape[0], report, 4)
+    state = _state(ref_counts, block_tables, page_size, seq_lens, workspace, "add report", add, seq_lens.numel(), report, 4)
     _enqueue("mc_kv_pages_grow", *state, add, report, workspace, _nbytes(workspace), _on(stream))
 
 
 def mc_kv_pages_free(ref_counts, block_tables, page_size: int, seq_lens, free_rows, report, stream=None) -> None:
     """Enqueue the listed rows becoming empty."""
     n = free_rows.numel()
-    state = _state(ref_counts, block_tables, page_size, seq_lens, "free_rows report", free_rows, n, report, 4)
+    state = _state(ref_counts, block_tables, page_size, seq_lens, None, "free_rows report", free_rows, n, report, 4)
     _enqueue("mc_kv_pages_free", *state, free_rows, n, report, _on(stream))
 
 
@@ -807,7 +822,9 @@ def mc_kv_pages_compact(ref_counts, moves, report, workspace, stream=None) -> No
     if _torch is None:
         _dtypes()
     n = moves.shape[0]
-    _dense("ref_counts moves report", ref_counts.get_device(), _torch.int32, ref_counts, 0, moves, 2 * n, report, 4)
+    device = ref_counts.get_device()
+    _dense("ref_counts moves report", device, _torch.int32, ref_counts, 0, moves, 2 * n, report, 4)
+    _here(device, workspace)
     _enqueue("mc_kv_pages_compact", ref_counts, ref_counts.numel(), n, moves, report, workspace, _nbytes(workspace), _on(stream))
 
 
@@ -815,9 +832,9 @@ def mc_kv_pages_remap(ref_counts, block_tables, page_size: int, seq_lens, moves,
     """Enqueue tables and counts following ``moves`` [n, 2], of which ``count[0]`` are moves (None: all)."""
     n = moves.shape[0]
     if count is None:
-        state = _state(ref_counts, block_tables, page_size, seq_lens, "moves", moves, 2 * n)
+        state = _state(ref_counts, block_tables, page_size, seq_lens, None, "moves", moves, 2 * n)
     else:
-        state = _state(ref_counts, block_tables, page_size, seq_lens, "moves count", moves, 2 * n, count, 1)
+        state = _state(ref_counts, block_tables, page_size, seq_lens, None, "moves count", moves, 2 * n, count, 1)
     _enqueue("mc_kv_pages_remap", *state, moves, count, n, _on(stream))
 
 
@@ -833,6 +850,7 @@ def mc_kv_copy_pages(k_pools, v_pools, num_pages: int, page_bytes: int, moves, c
     for pool in (*k_pools, *v_pools):
         if pool.get_device() != device or not pool.is_contiguous() or pool.nbytes < num_pages * page_bytes:
             raise ValueError(f"pools: {num_pages * page_bytes} dense bytes on device {device} wanted, not {_is(pool)}")
+    _here(device, None)
     layers = len(k_pools)
     _enqueue("mc_kv_copy_pages", _ints("q", [t.data_ptr() for t in k_pools], layers), _ints("q", [t.data_ptr() for t in v_pools], layers),
              layers, num_pages, page_bytes, moves, count, n, _on(stream))

@@ -1029,6 +1029,13 @@ DecodeLayout decode_layout(const mc_attn_params* p) {
   return lay;
 }
 
+bool decode_fits(const mc_attn_params* p, int32_t batch, int32_t max_pages) {
+  static_assert(kDecodeWgs * 8 == 1 << 11, "the waves of a launch");
+  if ((int64_t)batch * p->num_q_heads > 1 << 26) return false;
+  const int64_t blocks = (int64_t)batch * (max_pages / (kDecodeBlockKeys / 16) + 1);       // at most, of one head
+  return blocks <= ((int64_t)1 << 51) / p->num_q_heads;      // (a tile of query heads has one at least)
+}
+
 // One launch instead of two, at the pace of one compute unit a (row, head): us, by row / in equal stretches, 64/8 heads unless said,
 // all rows as long as the table: one row of 256 tokens 5.7 / 7.8, of 1024 10.3 / 9.8; 16 rows of 512 9.9 / 11.0; 32 of 256 7.0 / 8.8;
 // 8/1 heads, one row of 64 3.8 / 6.1, of 512 7.6 / 9.1, of 2048 14.2 / 10.3; fp32, 4/1 heads, 4 rows of 1000 16.2 / 10.2.

@@ -174,6 +174,8 @@ struct DecodeLayout {
   size_t ml_off, meta_off, total;
 };
 DecodeLayout decode_layout(const mc_attn_params* p);
+// Whether the places of a decode call's line, times the waves that share it, fit 63 bits (batch x pages fits 31).
+bool decode_fits(const mc_attn_params* p, int32_t batch, int32_t max_pages);
 // Whether a decode call of so many (row, KV head, tile) and so wide a table gives each a workgroup of its own.
 bool decode_by_row(int64_t items, int32_t max_pages);
 

@@ -781,7 +781,7 @@ mc_status mc_decode_attn_paged(const mc_attn_params* p, const void* q, const voi
   st = check_attn_buffers(false, q, k_pool, v_pool, block_tables, batch, max_pages_per_req, 0, out, lse, nullptr, nullptr, workspace);
   if (st != MC_OK) return st;
   if (!aligned4(seq_lens)) return MC_ERR_ALIGN;
-  if ((int64_t)batch * p->num_q_heads > 1 << 26) return MC_ERR_RANGE;
+  if (!decode_fits(p, batch, max_pages_per_req)) return MC_ERR_RANGE;
   const DecodeLayout lay = decode_layout(p);
   if (workspace == nullptr || workspace_bytes < lay.total) return MC_ERR_WORKSPACE;
   char* ws = reinterpret_cast<char*>(workspace);

@@ -84,9 +84,8 @@ constexpr int64_t kMostHostSlices = 512;
 // the work list is kept in this many lists, one per XCD of the chip
 constexpr int kXcds = 8;
 
-// Decode attention (attn_decode.hip): `total` blocks of keys in one line, shared out over waves in equal stretches.  The first
-// sizes of all are chosen so that nothing overflows: lengths below 2^31 (2^26 blocks), batch x heads below 2^31, waves 2^11 give
-// total x waves below 2^63 where batch x heads stays below 2^26 (the front end refuses more).
+// Decode attention (attn_decode.hip): `total` blocks of keys in one line, shared out over waves in equal stretches.  total is at most
+// 2^51 (decode_fits), so its product with the waves, 2^11, fits.
 constexpr int kDecodeWgs = 256;              // one a compute unit
 constexpr int kDecodeRows = 16;              // query heads of a tile
 constexpr int kDecodeBlockKeys = 32;

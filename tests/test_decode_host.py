@@ -33,7 +33,7 @@ int main() {
           if (decode_wave_of(total, x, n) != w) return 3;
       }
     }
-  const int64_t most = (int64_t)1 << 52;                                   // 2^26 rows and heads of 2^26 blocks
+  const int64_t most = (int64_t)1 << 51;                                   // what the front end lets through
   for (int w = 0; w < 2048; ++w) {
     const int64_t lo = decode_begin(most - 77, w, 2048), hi = decode_begin(most - 77, w + 1, 2048);
     if (lo < 0 || hi <= lo || decode_wave_of(most - 77, lo, 2048) != w || decode_wave_of(most - 77, hi - 1, 2048) != w) return 4;
@@ -58,7 +58,9 @@ def call(p=None, q=FAKE, k=FAKE, v=FAKE, bt=FAKE, max_pages=64, lens=FAKE, batch
     (dict(q=FAKE + 8), B.MC_ERR_ALIGN), (dict(out=FAKE + 8), B.MC_ERR_ALIGN), (dict(ws=FAKE + 8), B.MC_ERR_ALIGN),
     (dict(lens=FAKE + 2), B.MC_ERR_ALIGN), (dict(lse=FAKE + 2), B.MC_ERR_ALIGN), (dict(ws=None), B.MC_ERR_WORKSPACE),
     (dict(ws_bytes=1000), B.MC_ERR_WORKSPACE), (dict(batch=2 ** 26, max_pages=1), B.MC_ERR_RANGE),
-    (dict(batch=2 ** 16, max_pages=2 ** 16), B.MC_ERR_RANGE), (dict(p=B.attn_params(8, 2, 128, 32, 64, "bf16")), B.MC_ERR_UNSUPPORTED),
+    (dict(batch=2 ** 16, max_pages=2 ** 16), B.MC_ERR_RANGE),
+    (dict(p=B.attn_params(2 ** 25, 1, 128, 16, 64, "bf16"), batch=1, max_pages=2 ** 28), B.MC_ERR_RANGE),
+    (dict(p=B.attn_params(8, 2, 128, 32, 64, "bf16")), B.MC_ERR_UNSUPPORTED),
     (dict(p=B.attn_params(8, 2, 128, 16, 64, "f32")), B.MC_ERR_UNSUPPORTED), (dict(p=B.attn_params(8, 3, 128, 16, 64, "bf16")), B.MC_ERR_SHAPE),
     (dict(p=B.attn_params(8, 2, 128, 16, 64, "bf16", -1.0)), B.MC_ERR_SHAPE), (dict(batch=0, q=None, lens=None, ws=None), B.MC_OK)])
 def test_refusals(change, status):
@@ -88,3 +90,37 @@ def test_the_binding_refuses_tensors_that_do_not_fit(name, tensor):
     with pytest.raises(ValueError):
         B.mc_decode_attn_paged(B.attn_params(8, 2, 128, 16, 9, "bf16"), t["q"], t["pool"], t["pool"], t["table"], t["lens"], t["out"], t["lse"],
                                None, type("S", (), {"cuda_stream": 0})())
+
+
+@pytest.mark.parametrize("what", ["device", "workspace", "lens"])
+def test_other_devices_and_shapes_are_refused(what, monkeypatch):
+    kinds = dict(table=torch.int32, lens=torch.int32, lse=torch.float32)
+    t = {n: host(s, kinds.get(n, torch.bfloat16)) for n, s in GOOD.items()}
+    ws = host((1 << 24,), torch.uint8)
+    if what == "device":                                      # the tensors lie on device 0
+        monkeypatch.setattr(B, "_device", lambda: 1)
+    elif what == "workspace":
+        ws = torch.empty(1 << 24, dtype=torch.uint8)
+    else:
+        t["lens"] = host((3, 2), torch.int32)
+    with pytest.raises(ValueError):
+        B.mc_decode_attn_paged(B.attn_params(8, 2, 128, 16, 9, "bf16"), t["q"], t["pool"], t["pool"], t["table"], t["lens"], t["out"], t["lse"],
+                               ws, type("S", (), {"cuda_stream": 0})())
+
+
+def test_by_python_as_by_the_native_caller():
+    """The two looks at tensors agree, for an interpreter that the caller was not built for."""
+    from paper_2407_00079_amd import _mccall
+    bf16, good = torch.bfloat16, host((4, 8, 64))
+    for t in (good, host((4, 8, 64), torch.float32), torch.empty((4, 8, 64), dtype=bf16), host((4, 8, 64), strides=(1024, 64, 1)), host((4, 512)),
+              host((4, 512), strides=(700, 1)), host((4, 8, 64), strides=(1024, 128, 1)), host((3, 8, 64)), host((4, 4, 128)), host((2048,)),
+              host((1, 8, 64), strides=(3, 64, 1)), host((4, 1, 512), strides=(600, 7, 1)), host((0, 8, 64)), host((1, 4, 8, 64))):
+        for least in (0, 2048, 2049):
+            assert _mccall.misfit(0, bf16, good, 2048, t, least) == B._misfit_by_python(0, bf16, good, 2048, t, least)
+        for tokens, heads, dim in ((4, 8, 64), (1, 8, 64), (4, 1, 512), (0, 8, 64)):
+            assert _mccall.row_stride(0, bf16, t, tokens, heads, dim) == B._row_stride_by_python(0, bf16, t, tokens, heads, dim)
+    for bad in ((0, bf16, good), (0, bf16, None, 1), ("x", bf16, good, 1)):
+        with pytest.raises((TypeError, AttributeError)):
+            _mccall.misfit(*bad)
+    with pytest.raises(TypeError):
+        _mccall.row_stride(0, bf16, good, 4, 8)

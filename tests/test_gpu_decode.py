@@ -88,7 +88,7 @@ def test_long(dtype, dim, heads, lens):
 
 
 @pytest.mark.parametrize("dtype,dim", KINDS)
-@pytest.mark.parametrize("n", [511, 512, 513, 3000])
+@pytest.mark.parametrize("n", [511, 512, 513, 3000, 20000])
 def test_many_rows(dtype, dim, n):
     c = Call(dtype, (2, 1), dim, [(r * 11) % 70 for r in range(n)], seed=n)
     c.run()
