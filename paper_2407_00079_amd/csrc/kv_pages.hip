@@ -492,8 +492,10 @@ __global__ __launch_bounds__(kCopyThreads) void pages_copy_kernel(const LayerPoo
 
 }  // namespace
 
-// entries of tables that one workgroup goes through about as fast as a second launch begins
-constexpr int64_t kAloneEntries = 1 << 15;
+// One workgroup or several (us, alone / in two launches, a pool of 16384 pages): 4 rows of 64 pages forked 8.0 / 9.3 and freed 2.9 /
+// 4.1, 16 rows of 256 pages 13.2 / 10.2 and 8.4 / 4.6: at most so many table entries.  Growth of 64 rows 7.3 / 10.6, a compaction
+// 6.5 / 8.2 (4096 pages: 4.3 / 7.7).
+constexpr int64_t kAloneEntries = 1 << 10;
 
 hipError_t launch_pages_give(bool fork, const PagesArgs& args, hipStream_t stream) {
   (void)hipGetLastError();
