@@ -6,10 +6,13 @@
 // What bounds it: the bytes of the cache, each read once.  So all waves of the chip stream, and all of them the same number of
 // bytes whatever the lengths are.  The keys of every (row, KV head) are cut into blocks of 32, all blocks of the batch stand in one
 // line (row by row, head by head), and each of the 256 x 8 waves takes an equal stretch of the line.  Where its stretch begins
-// a wave finds from the lengths (each workgroup sums them up first), so no host plan is made and a captured launch follows the
-// lengths as they grow.
+// a wave finds from the lengths (all of them look them over), so no host plan is made and a captured launch follows the lengths as
+// they grow.  131071 keys of 64/8 heads: 537 MB in 86 us and 5 us for what is joined behind, 5.9 TB/s of the 6.7 that reading alone
+// reaches; 48 rows of 120 to 8000 tokens 66 us (5.6); 128 rows of 20 to 2500 tokens, head_dim 64, 31 us (4.4: the first blocks of all
+// waves arrive after 6 us, the join takes 4).
 //
-//   * A wave walks its stretch by itself: no barrier in the loop.  The next block's K and V are on their way to registers while
+//   * A wave walks its stretch by itself: no barrier in the loop (one a block, to keep a workgroup's waves together, gains nothing).
+//     The next block's K and V are on their way to registers while
 //     this one is used, across the ends of heads and rows too; K is turned into fragments in the wave's own corner of LDS, V
 //     needs no turning (attn_narrow.hip has the layout; the products are the same: S^T = K Q^T, O^T += V^T P^T, the rows of the
 //     tile being the query heads of the KV head).
@@ -272,8 +275,11 @@ __device__ __forceinline__ void put_out(T* to, const float (&x)[kPer], float sca
 }
 __device__ __forceinline__ float log_sum(float m, float l) { return (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f; }
 
-// kRows form: a workgroup has one (row, head, tile), whose blocks its waves share, and nothing is left to join behind it.
-template <typename T, int D, bool kByRow>
+// kByRow: a workgroup has one (row, head, tile), whose blocks its waves share, and nothing is left to join behind it.
+// kOnce: K and V pass the caches by (the nt hint).  131071 keys of 64/8 heads 101 -> 93 us, 48 uneven rows 74 -> 67; rows that share
+// pages lose by it (16 rows on the same 8000 tokens 34 -> 40 us, four on the same 131072 146 -> 197), which the call cannot see;
+// query heads that share them in several tiles it can, and then it reads through the caches (64/1 heads, four rows of 131071 98 -> 80).
+template <typename T, int D, bool kByRow, bool kOnce>
 __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeArgs a) {
   typedef Shape<T, D> S;
   typedef Math<T, D> M;
@@ -314,7 +320,7 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeAr
     StageK<kRowB, kBlockPages> stage;
     typename M::vvec v_even[8], v_odd[8];                  // 4 page + r: key 4 g + r of that page; of every other block
     auto load_k = [&](const At& of, const int (&pid)[kBlockPages]) __attribute__((always_inline)) {
-      stage.template load<true>(page_stride, reinterpret_cast<const char*>(a.k_pool) + (int64_t)of.head * S::kPageHeadB, pid);
+      stage.template load<kOnce>(page_stride, reinterpret_cast<const char*>(a.k_pool) + (int64_t)of.head * S::kPageHeadB, pid);
     };
     auto load_v = [&](const At& of, const int (&pid)[kBlockPages], typename M::vvec (&vr)[8]) __attribute__((always_inline)) {
       const char* base = reinterpret_cast<const char*>(a.v_pool) + (int64_t)of.head * S::kPageHeadB;
@@ -322,7 +328,10 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeAr
       for (int h = 0; h < kBlockPages; ++h) {
         const char* page = base + (int64_t)pid[h] * page_stride;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) vr[4 * h + r] = __builtin_nontemporal_load(reinterpret_cast<const typename M::vvec*>(page + v_lane + r * kRowB));
+        for (int r = 0; r < 4; ++r) {
+          const typename M::vvec* const at = reinterpret_cast<const typename M::vvec*>(page + v_lane + r * kRowB);
+          vr[4 * h + r] = kOnce ? __builtin_nontemporal_load(at) : *at;
+        }
       }
     };
     auto rows_of = [&](const At& of) __attribute__((always_inline)) {
@@ -633,10 +642,11 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_join_kernel(const Dec
 template <typename T, int D>
 void enqueue(const DecodeArgs& args, hipStream_t stream) {
   if (args.by_row) {
-    attn_decode_kernel<T, D, true><<<args.batch * args.Hkv * args.tiles, kWaves * 64, 0, stream>>>(args);
+    attn_decode_kernel<T, D, true, false><<<args.batch * args.Hkv * args.tiles, kWaves * 64, 0, stream>>>(args);
     return;
   }
-  attn_decode_kernel<T, D, false><<<kDecodeWgs, kWaves * 64, 0, stream>>>(args);
+  if (args.tiles == 1) attn_decode_kernel<T, D, false, true><<<kDecodeWgs, kWaves * 64, 0, stream>>>(args);
+  else attn_decode_kernel<T, D, false, false><<<kDecodeWgs, kWaves * 64, 0, stream>>>(args);
   if (args.G <= kRows / 2) attn_decode_join_kernel<T, D, kRows / 2><<<kDecodeWgs, kWaves * 64, 0, stream>>>(args);
   else attn_decode_join_kernel<T, D, kRows><<<kDecodeWgs, kWaves * 64, 0, stream>>>(args);
 }
