@@ -66,7 +66,7 @@ struct Line {
       : lens((const_i32_ptr)a.seq_lens), tables((const_i32_ptr)a.block_tables), batch(a.batch), max_pages(a.max_pages), heads(a.Hkv), tiles(a.tiles) {}
   // a length the table has no room for is a padding row's
   __device__ __forceinline__ int valid(int len) const { return len > 0 && (len - 1) / kPageTokens < max_pages ? len : 0; }
-  static __device__ __forceinline__ int blocks(int len) { return (len + kBlockKeys - 1) / kBlockKeys; }
+  static __device__ __forceinline__ int blocks(int len) { return (int)(((uint32_t)len + kBlockKeys - 1) / kBlockKeys); }
   __device__ __forceinline__ void next(At& at) const {
     if (++at.block < at.blocks) return;
     at.block = 0;
@@ -401,7 +401,7 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeAr
       At nn = nx;
       if (todo > 2) line.next(nn);
       line.pages_of(nn, pid);
-      if ((at.block + 1) * kBlockKeys > at.len) {          // slots at or past the length may hold anything
+      if ((uint32_t)(at.block + 1) * kBlockKeys > (uint32_t)at.len) {   // slots at or past the length may hold anything
         asm volatile("");                                  // (a branch, not selects on every block's path)
         const int seen = at.len - at.block * kBlockKeys - 4 * g;
 #pragma unroll

@@ -193,6 +193,26 @@ def test_pages_past_32_bits_of_bytes():
     c.check()
 
 
+def test_a_row_of_the_longest_length():
+    """2^31 - 1 keys: a table of 2^27 entries that name one page, the last another, whose one slot past the length is not a number.
+
+    Scores are 0, so sums of p and of p V are whole numbers below 2^24 up to a workgroup's (2^23 keys, values up to 7 in the waves'
+    2^20); 256 workgroups' parts are joined with at most 40 roundings.  The mean of the values is 3.5, of 2^31 - 1 of them 2^-29 beside."""
+    pages, n = 2 ** 27, 2 ** 31 - 1
+    p = B.attn_params(1, 1, 64, PAGE, 2, "bf16")
+    value = ((torch.arange(PAGE)[:, None] + torch.arange(64)[None, :]) % 8).to(torch.bfloat16)
+    k, v = torch.zeros((2, 1, PAGE, 64), dtype=torch.bfloat16), value.expand(2, 1, PAGE, 64).contiguous()
+    k[1, 0, 15], v[1, 0, 15] = math.nan, math.nan
+    table = torch.zeros((1, pages), dtype=torch.int32, device=DEV)
+    table[0, -1] = 1
+    out, lse = torch.empty((1, 1, 64), dtype=torch.bfloat16, device=DEV), torch.empty((1, 1), device=DEV)
+    ws = torch.empty(B.mc_decode_attn_workspace_bytes(p, 1), dtype=torch.uint8, device=DEV)
+    B.mc_decode_attn_paged(p, torch.ones((1, 1, 64), dtype=torch.bfloat16, device=DEV), k.to(DEV), v.to(DEV), table,
+                           torch.tensor([n], dtype=torch.int32, device=DEV), out, lse, ws)
+    assert bool((out == 3.5).all())
+    assert abs(float(lse) - math.log(n)) <= 40 * 2.0 ** -24 + 2.0 ** -22 * (1 + math.log(n))
+
+
 @pytest.mark.parametrize("dtype,dim", KINDS)
 def test_replayed_while_lengths_grow(dtype, dim):
     """A captured call reads the lengths of its replay; rows come and go."""
