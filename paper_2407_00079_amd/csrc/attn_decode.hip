@@ -130,6 +130,13 @@ struct Line {
     at.tile = which - at.head * tiles;
     return at;
   }
+  // whether one of the 63 rows around it begins with the same page (an empty row's entry may be anything: a hint hangs on it, no more)
+  __device__ __forceinline__ bool shared(int row) const {
+    const int r = row - 32 + (int)(threadIdx.x & 63), there = r < 0 ? 0 : r < batch ? r : batch - 1;
+    const int first = ((const int32_t*)tables)[(int64_t)there * max_pages];
+    const int own = __builtin_amdgcn_readlane(first, 32);    // (outside of any branch: lane 32 has to have loaded it)
+    return __builtin_amdgcn_ballot_w64((there == r) & (r != row) & (first == own)) != 0;
+  }
   // the table is never read past the row's pages
   __device__ __forceinline__ void pages_of(const At& at, int (&pid)[kBlockPages]) const {
     const const_i32_ptr ids = tables + (int64_t)at.row * max_pages;
@@ -276,10 +283,11 @@ __device__ __forceinline__ void put_out(T* to, const float (&x)[kPer], float sca
 __device__ __forceinline__ float log_sum(float m, float l) { return (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f; }
 
 // kByRow: a workgroup has one (row, head, tile), whose blocks its waves share, and nothing is left to join behind it.
-// kOnce: K and V pass the caches by (the nt hint).  131071 keys of 64/8 heads 101 -> 93 us, 48 uneven rows 74 -> 67; rows that share
-// pages lose by it (16 rows on the same 8000 tokens 34 -> 40 us, four on the same 131072 146 -> 197), which the call cannot see;
-// query heads that share them in several tiles it can, and then it reads through the caches (64/1 heads, four rows of 131071 98 -> 80).
-template <typename T, int D, bool kByRow, bool kOnce>
+// K and V that are read once pass the caches by (the nt hint): 131071 keys of 64/8 heads 101 -> 93 us, 48 uneven rows 74 -> 67.  What
+// several read - query heads in several tiles, rows that begin with the same page - goes through them: four rows of 131071, 64/1
+// heads, 98 -> 80 us; rows on the same pages, 16 of 8000 tokens 39 -> 33, 32 of them 62 -> 51, four of 131072 196 -> 147.  A wave
+// decides for its stretch, by the row it begins in; that it looks costs the others 0.3 to 0.5 us.
+template <typename T, int D, bool kByRow>
 __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeArgs a) {
   typedef Shape<T, D> S;
   typedef Math<T, D> M;
@@ -314,26 +322,6 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeAr
     At at = own;
     if (kByRow) at.block = (int)begin; else at = line.place(sums, begin);
 
-    char* const k_lds = sh.corner[wave];
-    const int64_t page_stride = (int64_t)a.Hkv * S::kPageHeadB;
-    const uint32_t v_lane = (uint32_t)(4 * g * kRowB + j * (kVec * (int)sizeof(T)));
-    StageK<kRowB, kBlockPages> stage;
-    typename M::vvec v_even[8], v_odd[8];                  // 4 page + r: key 4 g + r of that page; of every other block
-    auto load_k = [&](const At& of, const int (&pid)[kBlockPages]) __attribute__((always_inline)) {
-      stage.template load<kOnce>(page_stride, reinterpret_cast<const char*>(a.k_pool) + (int64_t)of.head * S::kPageHeadB, pid);
-    };
-    auto load_v = [&](const At& of, const int (&pid)[kBlockPages], typename M::vvec (&vr)[8]) __attribute__((always_inline)) {
-      const char* base = reinterpret_cast<const char*>(a.v_pool) + (int64_t)of.head * S::kPageHeadB;
-#pragma unroll
-      for (int h = 0; h < kBlockPages; ++h) {
-        const char* page = base + (int64_t)pid[h] * page_stride;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const typename M::vvec* const at = reinterpret_cast<const typename M::vvec*>(page + v_lane + r * kRowB);
-          vr[4 * h + r] = kOnce ? __builtin_nontemporal_load(at) : *at;
-        }
-      }
-    };
     auto rows_of = [&](const At& of) __attribute__((always_inline)) {
       const int left = a.G - of.tile * kRows;
       return left < kRows ? left : kRows;
@@ -341,127 +329,161 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeAr
     auto first_head = [&](const At& of) __attribute__((always_inline)) { return (int64_t)of.row * a.Hq + of.head * a.G + of.tile * kRows; };
 
     M math;
-    f32x4 o[kVec];
-    float m_run;
     auto ask = [&](const At& of) __attribute__((always_inline)) {
       const int rows = rows_of(of);                        // rows past the last compute it again
       math.query(reinterpret_cast<const char*>(a.q) + (first_head(of) + (j < rows ? j : rows - 1)) * kRowB, g);
     };
-    auto start = [&]() __attribute__((always_inline)) {    // with the queries asked for last
-      math.reset();
-      m_run = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-    };
-    // column kVec (4 g + r) + e of row j
-    auto keep = [&](int last) __attribute__((always_inline)) {
-      constexpr int kStore = kVec < 4 ? kVec : 4;
-      typedef float fvec __attribute__((ext_vector_type(kStore)));
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int e = 0; e < kVec; e += kStore) {
-          fvec v;
-#pragma unroll
-          for (int i = 0; i < kStore; ++i) v[i] = o[e + i][r];
-          *reinterpret_cast<fvec*>(sh.o(last, wave, j) + kVec * (4 * g + r) + e) = v;
-        }
-      const float l = math.sum();
-      if (g == 0) {
-        sh.m[last][wave][j] = m_run;
-        sh.l[last][wave][j] = l;
-      }
-    };
-    const float c = a.scale_log2e;
-
-    bool whole = at.block == 0;                            // the present row began in this stretch
-    int64_t left = end - begin;
-    At nx = at;
     int pid[kBlockPages];
     line.pages_of(at, pid);
+    const bool once = !kByRow && a.tiles == 1 && !line.shared(at.row);
     ask(at);
-    load_k(at, pid);
-    load_v(at, pid, v_even);
-    start();
-    if (left > 1) line.next(nx);
-    line.pages_of(nx, pid);
-    // One block: its V has been asked for a turn ago, and the next block's K and V are asked for before anything is done with it.
-    // (Loads are never skipped: behind a branch the compiler could not count those in flight.  The last turn's nobody uses.)
-    auto turn = [&](typename M::vvec (&vr)[8], typename M::vvec (&v_next)[8], int64_t todo) __attribute__((always_inline)) {
-      stage.put(k_lds);
-      if (nx.block == 0) ask(nx);                          // (ahead of all that is asked for below, so waited for with none of it)
-      load_k(nx, pid);
-      load_v(nx, pid, v_next);
-      wave_sees_lds();
-      __builtin_amdgcn_sched_barrier(0);
-      f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};     // keys 16 kt + 4 g + r of the block
-      math.template scores<StageK<kRowB, kBlockPages>>(k_lds, s);
-      // (behind the fragments: the scalar unit's loads and those from LDS are waited for together)
-      __builtin_amdgcn_sched_barrier(0);
-      At nn = nx;
-      if (todo > 2) line.next(nn);
-      line.pages_of(nn, pid);
-      if ((uint32_t)(at.block + 1) * kBlockKeys > (uint32_t)at.len) {   // slots at or past the length may hold anything
-        asm volatile("");                                  // (a branch, not selects on every block's path)
-        const int seen = at.len - at.block * kBlockKeys - 4 * g;
+    auto walk = [&](auto hint) __attribute__((always_inline)) {
+      constexpr bool kOnce = decltype(hint)::value != 0;
+      char* const k_lds = sh.corner[wave];
+      const int64_t page_stride = (int64_t)a.Hkv * S::kPageHeadB;
+      const uint32_t v_lane = (uint32_t)(4 * g * kRowB + j * (kVec * (int)sizeof(T)));
+      StageK<kRowB, kBlockPages> stage;
+      typename M::vvec v_even[8], v_odd[8];                  // 4 page + r: key 4 g + r of that page; of every other block
+      auto load_k = [&](const At& of, const int (&pid)[kBlockPages]) __attribute__((always_inline)) {
+        stage.template load<kOnce>(page_stride, reinterpret_cast<const char*>(a.k_pool) + (int64_t)of.head * S::kPageHeadB, pid);
+      };
+      auto load_v = [&](const At& of, const int (&pid)[kBlockPages], typename M::vvec (&vr)[8]) __attribute__((always_inline)) {
+        const char* base = reinterpret_cast<const char*>(a.v_pool) + (int64_t)of.head * S::kPageHeadB;
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
-          if (16 * (q >> 2) + (q & 3) >= seen) {
-            s[q >> 2][q & 3] = -INFINITY;
-            vr[q] = typename M::vvec{};
+        for (int h = 0; h < kBlockPages; ++h) {
+          const char* page = base + (int64_t)pid[h] * page_stride;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const typename M::vvec* const at = reinterpret_cast<const typename M::vvec*>(page + v_lane + r * kRowB);
+            vr[4 * h + r] = kOnce ? __builtin_nontemporal_load(at) : *at;
           }
-      }
-      const float mx = max_over_groups(max8(s[0], s[1])) * c;
-      if (__builtin_amdgcn_ballot_w64(mx > m_run + kRescaleSlack) != 0) {
-        const float m_new = fmaxf(m_run, mx);
-        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-        m_run = m_new;
-        math.rescale(alpha);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) o[e] *= alpha;
-      }
-      const float ref = fmaxf(m_run, kNoKeyYet);
-#pragma unroll
-      for (int q = 0; q < 8; ++q) s[q >> 2][q & 3] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q >> 2][q & 3], c, -ref));
-      math.values(s, vr, o);
-      wave_sees_lds();
-      __builtin_amdgcn_sched_barrier(0);
-      if (at.block + 1 == at.blocks) {
-        if (whole) {
-          const float l = math.sum(), inv = 1.0f / l;
-          if (j < rows_of(at)) {
-            const int64_t row = first_head(at) + j;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              float x[kVec];
-#pragma unroll
-              for (int e = 0; e < kVec; ++e) x[e] = o[e][r];
-              put_out<T, kVec>(reinterpret_cast<T*>(a.out) + row * D + kVec * (4 * g + r), x, inv);
-            }
-            if (a.lse != nullptr && g == 0) a.lse[row] = log_sum(m_run, l);
-          }
-        } else {
-          keep(0);
-          cut.has_first = 1;
         }
-        start();
-        whole = true;
-      } else if (todo == 1) {
-        keep(1);
-        cut.has_last = 1;
-        cut.through = !whole;
-        cut.row = at.row, cut.head = at.head, cut.tile = at.tile;
-        cut.rest = at.blocks - 1 - at.block;
+      };
+      f32x4 o[kVec];
+      float m_run;
+      auto start = [&]() __attribute__((always_inline)) {    // with the queries asked for last
+        math.reset();
+        m_run = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+      };
+      // column kVec (4 g + r) + e of row j
+      auto keep = [&](int last) __attribute__((always_inline)) {
+        constexpr int kStore = kVec < 4 ? kVec : 4;
+        typedef float fvec __attribute__((ext_vector_type(kStore)));
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int e = 0; e < kVec; e += kStore) {
+            fvec v;
+#pragma unroll
+            for (int i = 0; i < kStore; ++i) v[i] = o[e + i][r];
+            *reinterpret_cast<fvec*>(sh.o(last, wave, j) + kVec * (4 * g + r) + e) = v;
+          }
+        const float l = math.sum();
+        if (g == 0) {
+          sh.m[last][wave][j] = m_run;
+          sh.l[last][wave][j] = l;
+        }
+      };
+      const float c = a.scale_log2e;
+
+      bool whole = at.block == 0;                            // the present row began in this stretch
+      int64_t left = end - begin;
+      At nx = at;
+      load_k(at, pid);
+      load_v(at, pid, v_even);
+      start();
+      if (left > 1) line.next(nx);
+      line.pages_of(nx, pid);
+      // One block: its V has been asked for a turn ago, and the next block's K and V are asked for before anything is done with it.
+      // (Loads are never skipped: behind a branch the compiler could not count those in flight.  The last turn's nobody uses.)
+      auto turn = [&](typename M::vvec (&vr)[8], typename M::vvec (&v_next)[8], int64_t todo) __attribute__((always_inline)) {
+        stage.put(k_lds);
+        if (nx.block == 0) ask(nx);                          // (ahead of all that is asked for below, so waited for with none of it)
+        load_k(nx, pid);
+        load_v(nx, pid, v_next);
+        wave_sees_lds();
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};     // keys 16 kt + 4 g + r of the block
+        math.template scores<StageK<kRowB, kBlockPages>>(k_lds, s);
+        // (behind the fragments: the scalar unit's loads and those from LDS are waited for together)
+        __builtin_amdgcn_sched_barrier(0);
+        At nn = nx;
+        if (todo > 2) line.next(nn);
+        line.pages_of(nn, pid);
+        if ((uint32_t)(at.block + 1) * kBlockKeys > (uint32_t)at.len) {   // slots at or past the length may hold anything
+          asm volatile("");                                  // (a branch, not selects on every block's path)
+          const int seen = at.len - at.block * kBlockKeys - 4 * g;
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            if (16 * (q >> 2) + (q & 3) >= seen) {
+              s[q >> 2][q & 3] = -INFINITY;
+              vr[q] = typename M::vvec{};
+            }
+        }
+        const float mx = max_over_groups(max8(s[0], s[1])) * c;
+        if (__builtin_amdgcn_ballot_w64(mx > m_run + kRescaleSlack) != 0) {
+          const float m_new = fmaxf(m_run, mx);
+          const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+          m_run = m_new;
+          math.rescale(alpha);
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) o[e] *= alpha;
+        }
+        const float ref = fmaxf(m_run, kNoKeyYet);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) s[q >> 2][q & 3] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q >> 2][q & 3], c, -ref));
+        math.values(s, vr, o);
+        wave_sees_lds();
+        __builtin_amdgcn_sched_barrier(0);
+        if (at.block + 1 == at.blocks) {
+          if (whole) {
+            const float l = math.sum(), inv = 1.0f / l;
+            if (j < rows_of(at)) {
+              const int64_t row = first_head(at) + j;
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                float x[kVec];
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) x[e] = o[e][r];
+                put_out<T, kVec>(reinterpret_cast<T*>(a.out) + row * D + kVec * (4 * g + r), x, inv);
+              }
+              if (a.lse != nullptr && g == 0) a.lse[row] = log_sum(m_run, l);
+            }
+          } else {
+            keep(0);
+            cut.has_first = 1;
+          }
+          start();
+          whole = true;
+        } else if (todo == 1) {
+          keep(1);
+          cut.has_last = 1;
+          cut.through = !whole;
+          cut.row = at.row, cut.head = at.head, cut.tile = at.tile;
+          cut.rest = at.blocks - 1 - at.block;
+        }
+        at = nx;
+        nx = nn;
+      };
+      // (In pairs: with a way out between the two the compiler moves V from one set of registers to the other, and waits for it.)
+      for (; left > 1; left -= 2) {
+        turn(v_even, v_odd, left);
+        turn(v_odd, v_even, left - 1);
       }
-      at = nx;
-      nx = nn;
+      if (left > 0) turn(v_even, v_odd, left);
     };
-    // (In pairs: with a way out between the two the compiler moves V from one set of registers to the other, and waits for it.)
-    for (; left > 1; left -= 2) {
-      turn(v_even, v_odd, left);
-      turn(v_odd, v_even, left - 1);
+    // (The empty statements keep the compiler from making one of what the two have in common, which costs the hint or the registers.)
+    if (once) {
+      asm volatile("; past the caches");
+      walk(Int<1>{});
+      asm volatile("; past the caches");
+    } else {
+      asm volatile("; through the caches");
+      walk(Int<0>{});
+      asm volatile("; through the caches");
     }
-    if (left > 0) turn(v_even, v_odd, left);
   }
   if (lane == 0) {
     sh.cut[wave] = cut;
@@ -642,11 +664,10 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_join_kernel(const Dec
 template <typename T, int D>
 void enqueue(const DecodeArgs& args, hipStream_t stream) {
   if (args.by_row) {
-    attn_decode_kernel<T, D, true, false><<<args.batch * args.Hkv * args.tiles, kWaves * 64, 0, stream>>>(args);
+    attn_decode_kernel<T, D, true><<<args.batch * args.Hkv * args.tiles, kWaves * 64, 0, stream>>>(args);
     return;
   }
-  if (args.tiles == 1) attn_decode_kernel<T, D, false, true><<<kDecodeWgs, kWaves * 64, 0, stream>>>(args);
-  else attn_decode_kernel<T, D, false, false><<<kDecodeWgs, kWaves * 64, 0, stream>>>(args);
+  attn_decode_kernel<T, D, false><<<kDecodeWgs, kWaves * 64, 0, stream>>>(args);
   if (args.G <= kRows / 2) attn_decode_join_kernel<T, D, kRows / 2><<<kDecodeWgs, kWaves * 64, 0, stream>>>(args);
   else attn_decode_join_kernel<T, D, kRows><<<kDecodeWgs, kWaves * 64, 0, stream>>>(args);
 }

@@ -181,6 +181,28 @@ def test_rows_that_share_pages():
     c.check()
 
 
+@pytest.mark.parametrize("dtype,dim", KINDS)
+@pytest.mark.parametrize("heads,rows,length", [((8, 1), 3, 9000), ((12, 2), 150, 700), ((40, 1), 70, 350)])
+def test_shared_pages_give_the_bits_of_copies(dtype, dim, heads, rows, length):
+    """Rows on the same full pages, last pages of their own, some rows empty, against the same rows with a copy of every page."""
+    lens = [0 if r % 7 == 3 else length - r % 5 for r in range(rows)]
+    c = Call(dtype, heads, dim, lens, seed=rows, nan=False)
+    full = min(n for n in lens if n) // PAGE
+    whole = c.table[0, :full].long()
+    for r, n in enumerate(lens):
+        if n:
+            c.k[c.table[r, :full].long()], c.v[c.table[r, :full].long()] = c.k[whole], c.v[whole]
+    c.run()
+    apart = c.out.clone(), c.lse.clone()
+    for r, n in enumerate(lens):
+        if n:
+            c.table[r, :full] = c.table[0, :full]
+    c.out.fill_(math.nan)
+    c.run()
+    assert torch.equal(apart[0], c.out) and torch.equal(apart[1], c.lse)
+    c.check()
+
+
 def test_pages_past_32_bits_of_bytes():
     """A pool of 4.6 GB whose last pages are used."""
     c = Call("bf16", (8, 8), 128, [1000, 35], seed=8, nan=False)
