@@ -397,12 +397,15 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeAr
       if (left > 1) line.next(nx);
       line.pages_of(nx, pid);
       // One block: its V has been asked for a turn ago, and the next block's K and V are asked for before anything is done with it.
-      // (Loads are never skipped: behind a branch the compiler could not count those in flight.  The last turn's nobody uses.)
-      auto turn = [&](typename M::vvec (&vr)[8], typename M::vvec (&v_next)[8], int64_t todo) __attribute__((always_inline)) {
+      // (Loads are not skipped by a branch, behind which the compiler could not count those in flight: the last turn is code of its own.)
+      auto turn = [&](auto at_end, typename M::vvec (&vr)[8], typename M::vvec (&v_next)[8], int64_t todo) __attribute__((always_inline)) {
+        constexpr bool kLast = decltype(at_end)::value != 0;
         stage.put(k_lds);
-        if (nx.block == 0) ask(nx);                          // (ahead of all that is asked for below, so waited for with none of it)
-        load_k(nx, pid);
-        load_v(nx, pid, v_next);
+        if (!kLast) {
+          if (nx.block == 0) ask(nx);                        // (ahead of all that is asked for below, so waited for with none of it)
+          load_k(nx, pid);
+          load_v(nx, pid, v_next);
+        }
         wave_sees_lds();
         __builtin_amdgcn_sched_barrier(0);
         f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};     // keys 16 kt + 4 g + r of the block
@@ -410,8 +413,10 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeAr
         // (behind the fragments: the scalar unit's loads and those from LDS are waited for together)
         __builtin_amdgcn_sched_barrier(0);
         At nn = nx;
-        if (todo > 2) line.next(nn);
-        line.pages_of(nn, pid);
+        if (!kLast) {
+          if (todo > 2) line.next(nn);
+          line.pages_of(nn, pid);
+        }
         if ((uint32_t)(at.block + 1) * kBlockKeys > (uint32_t)at.len) {   // slots at or past the length may hold anything
           asm volatile("");                                  // (a branch, not selects on every block's path)
           const int seen = at.len - at.block * kBlockKeys - 4 * g;
@@ -455,24 +460,28 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeAr
             keep(0);
             cut.has_first = 1;
           }
-          start();
+          if (!kLast) start();
           whole = true;
-        } else if (todo == 1) {
+        } else if (kLast) {
           keep(1);
           cut.has_last = 1;
           cut.through = !whole;
           cut.row = at.row, cut.head = at.head, cut.tile = at.tile;
           cut.rest = at.blocks - 1 - at.block;
         }
-        at = nx;
-        nx = nn;
+        if (!kLast) at = nx, nx = nn;
       };
       // (In pairs: with a way out between the two the compiler moves V from one set of registers to the other, and waits for it.)
-      for (; left > 1; left -= 2) {
-        turn(v_even, v_odd, left);
-        turn(v_odd, v_even, left - 1);
+      for (; left > 2; left -= 2) {
+        turn(Int<0>{}, v_even, v_odd, left);
+        turn(Int<0>{}, v_odd, v_even, left - 1);
       }
-      if (left > 0) turn(v_even, v_odd, left);
+      if (left == 2) {
+        turn(Int<0>{}, v_even, v_odd, 2);
+        turn(Int<1>{}, v_odd, v_even, 1);
+      } else {
+        turn(Int<1>{}, v_even, v_odd, 1);
+      }
     };
     // (The empty statements keep the compiler from making one of what the two have in common, which costs the hint or the registers.)
     if (once) {
