@@ -7,15 +7,13 @@
 // bytes whatever the lengths are.  The keys of every (row, KV head) are cut into blocks of 32, all blocks of the batch stand in one
 // line (row by row, head by head), and each of the 256 x 8 waves takes an equal stretch of the line.  Where its stretch begins
 // a wave finds from the lengths (all of them look them over), so no host plan is made and a captured launch follows the lengths as
-// they grow.  131071 keys of 64/8 heads: 537 MB in 86 us and 5 us for what is joined behind, 5.9 TB/s of the 6.7 that reading alone
-// reaches; 48 rows of 120 to 8000 tokens 66 us (5.6); 128 rows of 20 to 2500 tokens, head_dim 64, 31 us (4.4: the first blocks of all
-// waves arrive after 6 us, the join takes 4).
+// they grow.  131071 keys of 64/8 heads: 537 MB (as counted, too) in 82.7 us, 6.5 TB/s of the 6.7 that reading alone reaches, and 5.6
+// for what is joined behind; 48 rows of 120 to 8000 tokens 62.5 and 4.5 us; 128 rows of 20 to 2500 tokens, head_dim 64, 27 and 4.
 //
 //   * A wave walks its stretch by itself: no barrier in the loop (one a block, to keep a workgroup's waves together, gains nothing).
-//     The next block's K and V are on their way to registers while
-//     this one is used, across the ends of heads and rows too; K is turned into fragments in the wave's own corner of LDS, V
-//     needs no turning (attn_narrow.hip has the layout; the products are the same: S^T = K Q^T, O^T += V^T P^T, the rows of the
-//     tile being the query heads of the KV head).
+//     The next block's K and V are on their way to registers while this one is used, across the ends of heads and rows too; K is
+//     turned into fragments in the wave's own corner of LDS, V needs no turning (attn_narrow.hip has the layout; the products are
+//     the same: S^T = K Q^T, O^T += V^T P^T, the rows of the tile being the query heads of the KV head).
 //   * A softmax runs in one pass with a running reference and sum in fp32.  bf16: p enters P V as two bf16 values, its rounding
 //     and what that left out, so that the output is rounded once (p rounded to 8 bits alone would cost as much again as the output's
 //     own rounding; the matrix units wait for memory anyway).
@@ -591,7 +589,6 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_kernel(const DecodeAr
 template <typename T, int D, int ROWS>
 __global__ __launch_bounds__(kWaves * 64) void attn_decode_join_kernel(const DecodeArgs a) {
   constexpr int kStride = D + 4, kLoads = ROWS * D / 256;  // 16-byte loads of a lane for a part: element 256 k + 4 lane of its rows
-  constexpr int kAtOnce = kLoads > 4 ? 2 : 4;              // parts whose loads are in flight together
   __shared__ __attribute__((aligned(16))) float outs[kWaves][ROWS][kStride];
   __shared__ float tops[kWaves][ROWS], sums[kWaves][ROWS];
   const DecodeMeta meta = a.meta[blockIdx.x];
@@ -605,40 +602,45 @@ __global__ __launch_bounds__(kWaves * 64) void attn_decode_join_kernel(const Dec
     l[k] = 0.f;
     x[k] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  for (int base = wave; base <= meta.more; base += kWaves * kAtOnce) {
-    f32x4 v[kAtOnce][kLoads];
-    float2 ml[kAtOnce][kLoads];
-#pragma unroll
-    for (int n = 0; n < kAtOnce; ++n) {
-      int i = base + n * kWaves;
-      i = i <= meta.more ? i : base;                       // (behind the last: one again, for nothing)
-      const int64_t part = (((int64_t)blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * kRows;
-#pragma unroll
-      for (int k = 0; k < kLoads; ++k) {
-        const int at = 256 * k + 4 * lane;
-        v[n][k] = *reinterpret_cast<const f32x4*>(a.o_parts + part * D + at);
-        ml[n][k] = a.ml_parts[part + at / D];
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < kLoads; ++k) {
-      float most = top[k];
-#pragma unroll
-      for (int n = 0; n < kAtOnce; ++n) most = fmaxf(most, ml[n][k].x);
-      const float ref = most == -INFINITY ? 0.f : most;    // (every score so far is -inf or NaN)
-      const float before = __builtin_amdgcn_exp2f(top[k] - ref);
-      l[k] *= before;
-      x[k] *= before;
-      top[k] = most;
+  auto gather = [&](auto many) __attribute__((always_inline)) {
+    constexpr int kAtOnce = decltype(many)::value;         // parts whose loads are in flight together
+    for (int base = wave; base <= meta.more; base += kWaves * kAtOnce) {
+      f32x4 v[kAtOnce][kLoads];
+      float2 ml[kAtOnce][kLoads];
 #pragma unroll
       for (int n = 0; n < kAtOnce; ++n) {
-        if (base + n * kWaves > meta.more) break;
-        const float weight = __builtin_amdgcn_exp2f(ml[n][k].x - ref);
-        l[k] += weight * ml[n][k].y;
-        x[k] += weight * v[n][k];
+        int i = base + n * kWaves;
+        i = i <= meta.more ? i : base;                       // (behind the last: one again, for nothing)
+        const int64_t part = (((int64_t)blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * kRows;
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+          const int at = 256 * k + 4 * lane;
+          v[n][k] = *reinterpret_cast<const f32x4*>(a.o_parts + part * D + at);
+          ml[n][k] = a.ml_parts[part + at / D];
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kLoads; ++k) {
+        float most = top[k];
+#pragma unroll
+        for (int n = 0; n < kAtOnce; ++n) most = fmaxf(most, ml[n][k].x);
+        const float ref = most == -INFINITY ? 0.f : most;    // (every score so far is -inf or NaN)
+        const float before = __builtin_amdgcn_exp2f(top[k] - ref);
+        l[k] *= before;
+        x[k] *= before;
+        top[k] = most;
+#pragma unroll
+        for (int n = 0; n < kAtOnce; ++n) {
+          if (base + n * kWaves > meta.more) break;
+          const float weight = __builtin_amdgcn_exp2f(ml[n][k].x - ref);
+          l[k] += weight * ml[n][k].y;
+          x[k] += weight * v[n][k];
+        }
       }
     }
-  }
+  };
+  // (At most one part a wave: 48 uneven rows 65.7 -> 64.7 us against asking for it four times; eight at once, 33 parts: 87.9 -> 89.5.)
+  if (meta.more < kWaves) gather(Int<1>{}); else gather(Int<(kLoads > 4 ? 2 : 4)>{});
 #pragma unroll
   for (int k = 0; k < kLoads; ++k) {
     const int at = 256 * k + 4 * lane, row = at / D;
