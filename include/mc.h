@@ -432,7 +432,8 @@ mc_status mc_kv_rope_append_decode(const mc_attn_params* p, const mc_rope_params
  *
  * Slots at or past a row's length are never used as values (they may hold NaN).  fp32 accumulation and softmax; output rounded
  * once, to nearest even.  The same lengths and inputs give the same bits.  batch * Hq > 2^26, or tables so wide that all rows' blocks
- * of 32 keys times Hq exceed 2^51, is MC_ERR_RANGE; batch == 0 enqueues nothing.  Nothing is allocated, uploaded or waited for; the call can be captured.
+ * of 32 keys times Hq exceed 2^51, is MC_ERR_RANGE; batch == 0 enqueues nothing.  Nothing is allocated, uploaded or waited for; the
+ * call can be captured.
  */
 size_t mc_decode_attn_workspace_bytes(const mc_attn_params* p, int32_t batch);
 mc_status mc_decode_attn_paged(const mc_attn_params* p, const void* q, const void* k_pool, const void* v_pool,
