@@ -464,7 +464,8 @@ size_t mc_kv_pages_workspace_bytes(int64_t num_pages, int32_t rows);
  *
  *   src_rows, dst_rows  dev  int32 [n], n <= rows; a dst row has to be empty and to be listed once (else MC_PAGES_BAD_ROW)
  *   moves               dev  int32 [n][2]: report[0] moves, the rest { -1, -1 }
- *   report              { moves, flags, free pages left, pages wanted }; where flags has SHORT or BAD_ROW nothing was changed, no move
+ *   report              { moves, flags, free pages left, pages wanted }; where flags has SHORT or BAD_ROW nothing was changed, no move;
+ *                       BAD_ID: some source names a page outside the pool (its counts are left, and mc_kv_copy_pages passes such a move over)
  *   n == 0 enqueues nothing.
  */
 mc_status mc_kv_pages_fork(int32_t* ref_counts, int64_t num_pages, int32_t* block_tables, int32_t max_pages_per_req, int32_t page_size,

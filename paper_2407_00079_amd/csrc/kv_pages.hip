@@ -165,9 +165,11 @@ __global__ __launch_bounds__(kThreads) void pages_give_kernel(const PagesArgs a)
         a.ref_counts[page] = 1;
         if (kFork) {
           const int at = len / a.page_size;
+          const int from = a.block_tables[(int64_t)a.list[lo] * a.max_pages + at];
           a.block_tables[(int64_t)a.dst_list[lo] * a.max_pages + at] = page;
-          a.moves[2 * (int64_t)rank] = a.block_tables[(int64_t)a.list[lo] * a.max_pages + at];
+          a.moves[2 * (int64_t)rank] = from;
           a.moves[2 * (int64_t)rank + 1] = page;
+          if (from < 0 || from >= a.num_pages) atomicOr(a.report + 1, MC_PAGES_BAD_ID);
         } else {
           a.block_tables[(int64_t)lo * a.max_pages + pages_of(len, a.page_size) + (rank - a.wanted_before[lo])] = page;
         }
@@ -342,9 +344,11 @@ __global__ __launch_bounds__(kThreads) void pages_give_alone_kernel(const PagesA
       a.ref_counts[page] = 1;
       if (kFork) {
         const int at = lens[lo] / a.page_size;
+        const int from = a.block_tables[(int64_t)a.list[lo] * a.max_pages + at];
         a.block_tables[(int64_t)a.dst_list[lo] * a.max_pages + at] = page;
-        a.moves[2 * rank] = a.block_tables[(int64_t)a.list[lo] * a.max_pages + at];
+        a.moves[2 * rank] = from;
         a.moves[2 * rank + 1] = page;
+        if (from < 0 || from >= a.num_pages) bad_id = 1;
       } else {
         a.block_tables[(int64_t)lo * a.max_pages + pages_of(lens[lo], a.page_size) + (rank - wanted_before[lo])] = page;
       }

@@ -47,6 +47,7 @@ class State:
                     flags |= BAD_ID
             if n % self.page:
                 j, page = n // self.page, free.pop(0)
+                flags |= 0 if self.inside(before.tables[s][j]) else BAD_ID
                 self.tables[d][j] = page
                 self.counts[page] = 1
                 moves.append([before.tables[s][j], page])

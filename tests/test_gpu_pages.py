@@ -130,6 +130,27 @@ def test_what_is_not_valid_is_refused_on_the_device():
     assert Device(bad).fork([0], [1])[1][:2] == [1, BAD_ID]
 
 
+@pytest.mark.parametrize("pages,wide", [(40, 4), (20000, 2000)])
+def test_pages_that_are_none(pages, wide):
+    """Entries outside the pool, among full pages and as a row's last page: reported, never followed, in either form of the kernels."""
+    tables = [[-5] * wide for _ in range(6)]
+    tables[0][:3], tables[1][:3], tables[2][:2] = [3, pages, 5], [7, 8, 2 ** 31 - 1], [-1, 9]
+    counts = [0] * pages
+    for page in (3, 5, 7, 8, 9):
+        counts[page] = 1
+    state = State(counts, tables, 16, [48, 40, 32, 0, 0, 0])
+    assert Device(copy.deepcopy(state)).fork([0, 1, 2], [3, 4, 5])[1] == [1, BAD_ID, pages - 6, 1]
+    d = Device(copy.deepcopy(state))
+    moves, report = d.fork([1], [5])
+    assert report[:2] == [1, BAD_ID] and moves.tolist() == [[2 ** 31 - 1, 0]]
+    pool = (torch.arange(pages * 16, device=DEV) % 251).to(torch.uint8)
+    before = pool.clone()
+    B.mc_kv_copy_pages([pool], [pool], pages, 16, moves, d.report[:1])
+    assert torch.equal(pool, before)
+    assert Device(copy.deepcopy(state)).free([0, 1, 2])[:2] == [5, BAD_ID]
+    assert Device(copy.deepcopy(state)).grow([1, 0, 0, 20, 0, 0])[:2] == [3, 0]
+
+
 def test_nothing_to_do():
     d = Device(random_state(np.random.default_rng(1), 50, 4, 5, 16, 0.5))
     empty = torch.empty(0, dtype=torch.int32, device=DEV)
