@@ -643,6 +643,16 @@ def _dtypes() -> dict:
     return _DTYPES
 
 
+def _type(params):
+    """torch's type of a call's tensors; parameters that have none are refused as the library does."""
+    if _params(params) is None:
+        raise McError(MC_ERR_NULL, "params")
+    dtype = (_DTYPES or _dtypes()).get(params.dtype)
+    if dtype is None:
+        raise McError(MC_ERR_UNSUPPORTED, f"dtype {params.dtype}")
+    return dtype
+
+
 def _misfit_by_python(device: int, dtype, *tensors) -> int:
     """What csrc/pycall.cpp does, for an interpreter it was not built for."""
     for i, (t, least) in enumerate(zip(tensors[::2], tensors[1::2])):
@@ -698,7 +708,7 @@ def _table(block_tables, rows: int) -> int:
 
 def _rope_tensors(params, q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, tokens: int):
     """Looks the tensors of a rotation call over: (device, strides or None where all of them are dense)."""
-    dtype = (_DTYPES or _dtypes())[params.dtype]
+    dtype = _type(params)
     device, Hq, Hkv, D = q.get_device(), params.num_q_heads, params.num_kv_heads, params.head_dim
     a, b, c = (_row_stride(device, dtype, q, tokens, Hq, D), _row_stride(device, dtype, k, tokens, Hkv, D),
                _row_stride(device, dtype, v, tokens, Hkv, D))
@@ -730,7 +740,7 @@ def mc_kv_rope_append_paged(params: McAttnParams, rope: McRopeParams, q, k, v, q
     n = len(prefix_lens)
     if len(new_lens) != n:
         raise ValueError(f"{n} prefix lengths and {len(new_lens)} new lengths")
-    device, strides = _rope_tensors(_params(params), q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, sum(new_lens))
+    device, strides = _rope_tensors(params, q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, sum(new_lens))
     wide = _table(block_tables, n)
     _dense("block_tables", device, _torch.int32, block_tables, 0)
     _here(device, workspace)
@@ -742,7 +752,7 @@ def mc_kv_rope_append_paged(params: McAttnParams, rope: McRopeParams, q, k, v, q
 def mc_kv_rope_append_run(params: McAttnParams, plan: McAttnPlan, rope: McRopeParams, q, k, v, q_norm, k_norm, q_out, k_pool, v_pool,
                           block_tables, workspace, stream=None) -> None:
     """mc_kv_rope_append_paged for a prepared batch."""
-    device, strides = _rope_tensors(_params(params), q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, _plan(plan).total_new_tokens)
+    device, strides = _rope_tensors(params, q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, _plan(plan).total_new_tokens)
     wide = _table(block_tables, plan.batch)
     _dense("block_tables", device, _torch.int32, block_tables, 0)
     _here(device, workspace)
@@ -754,7 +764,7 @@ def mc_kv_rope_append_decode(params: McAttnParams, rope: McRopeParams, q, k, v, 
                              seq_lens, stream=None) -> None:
     """The same for one new token a row, at position ``seq_lens[r] - 1``; ``seq_lens``: int32 device tensor."""
     n = seq_lens.numel()
-    device, strides = _rope_tensors(_params(params), q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, n)
+    device, strides = _rope_tensors(params, q, k, v, q_norm, k_norm, q_out, k_pool, v_pool, n)
     wide = _table(block_tables, n)
     _dense("seq_lens block_tables", device, _torch.int32, seq_lens, n, block_tables, 0)
     _here(device, None)
@@ -768,7 +778,7 @@ def mc_decode_attn_workspace_bytes(params: McAttnParams, batch: int) -> int:
 
 def mc_decode_attn_paged(params: McAttnParams, q, k_pool, v_pool, block_tables, seq_lens, out, lse, workspace, stream=None) -> None:
     """Enqueue attention of one new token a row: q, out [rows, heads, head_dim], ``seq_lens`` int32 device tensor [rows]."""
-    dtype = (_DTYPES or _dtypes())[_params(params).dtype]
+    dtype = _type(params)
     n, heads = seq_lens.numel(), params.num_q_heads
     wide = _table(block_tables, n)
     device, size, pool = q.get_device(), n * heads * params.head_dim, _pool_size(params)

@@ -124,3 +124,17 @@ def test_by_python_as_by_the_native_caller():
             _mccall.misfit(*bad)
     with pytest.raises(TypeError):
         _mccall.row_stride(0, bf16, good, 4, 8)
+
+
+def test_parameters_without_a_type():
+    """Refused with the library's statuses by the wrappers, too, which look at the tensors first."""
+    x, ids = torch.zeros((1, 8, 128), dtype=torch.bfloat16), torch.zeros((1, 1), dtype=torch.int32)
+    p = B.attn_params(8, 8, 128, 16, 1, "bf16")
+    p.dtype = 5
+    for params, status in ((p, B.MC_ERR_UNSUPPORTED), (None, B.MC_ERR_NULL)):
+        with pytest.raises(B.McError) as e:
+            B.mc_decode_attn_paged(params, x, x, x, ids, ids[0], x, None, None)
+        assert e.value.status == status
+        with pytest.raises(B.McError) as e:
+            B.mc_kv_rope_append_decode(params, B.rope_params(128, B.MC_ROPE_HALF), x, x, x, None, None, x, x, x, ids, ids[0])
+        assert e.value.status == status
