@@ -508,8 +508,10 @@ mc_status mc_kv_pages_compact(const int32_t* ref_counts, int64_t num_pages, int3
 /*
  * Tables and counts follow moves: entries that name a move's source name its destination afterwards, which takes over the count.
  *
- *   moves  dev  int32 [n][2], sources ascending, as mc_kv_pages_compact lists them (no page may be in two moves)
- *   count  dev  int32: how many of the n are moves (report of the call that listed them), or NULL: all
+ *   moves  dev  int32 [n][2], sources ascending, as mc_kv_pages_compact lists them (no page may be in two moves); unused entries
+ *               { -1, -1 } behind the moves are passed over
+ *   count  dev  int32: how many of the n are looked at (report of the call that listed them), or NULL: all
+ * A row that is longer than its table has a whole one; an entry outside the pool, or of a row past its length, stays as it is.
  */
 mc_status mc_kv_pages_remap(int32_t* ref_counts, int64_t num_pages, int32_t* block_tables, int32_t max_pages_per_req, int32_t page_size,
                             const int32_t* seq_lens, int32_t rows, const int32_t* moves, const int32_t* count, int32_t n,

@@ -839,7 +839,7 @@ def mc_kv_pages_compact(ref_counts, moves, report, workspace, stream=None) -> No
 
 
 def mc_kv_pages_remap(ref_counts, block_tables, page_size: int, seq_lens, moves, count=None, stream=None) -> None:
-    """Enqueue tables and counts following ``moves`` [n, 2], of which ``count[0]`` are moves (None: all)."""
+    """Enqueue tables and counts following ``moves`` [n, 2], of which ``count[0]`` are looked at (None: all; unused ones of -1 are passed over)."""
     n = moves.shape[0]
     if count is None:
         state = _state(ref_counts, block_tables, page_size, seq_lens, None, "moves", moves, 2 * n)

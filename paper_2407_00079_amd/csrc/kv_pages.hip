@@ -440,7 +440,8 @@ __global__ __launch_bounds__(kThreads) void pages_compact_alone_kernel(const Pag
   }
 }
 
-// Table entries and counts follow the moves (sources ascending, as a compaction lists them).
+// Table entries and counts follow the moves (sources ascending, as a compaction lists them, unused entries of -1 behind them: without a
+// sign those are the largest, so the whole list is in order).
 __global__ __launch_bounds__(256) void pages_remap_kernel(const PagesArgs a, const int32_t* __restrict__ count, int entry_blocks) {
   int n = count != nullptr ? *count : a.n;
   n = n < 0 ? 0 : n < a.n ? n : a.n;
@@ -455,16 +456,16 @@ __global__ __launch_bounds__(256) void pages_remap_kernel(const PagesArgs a, con
     return;
   }
   const int64_t entries = (int64_t)a.rows * a.max_pages;
-  const int lowest = a.moves[0];
+  const uint32_t lowest = (uint32_t)a.moves[0];
   for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < entries; at += (int64_t)entry_blocks * 256) {
     const int row = (int)((uint32_t)at / (uint32_t)a.max_pages), j = (int)((uint32_t)at - (uint32_t)row * a.max_pages);
     if ((int64_t)j * a.page_size >= a.seq_lens[row]) continue;
     const int page = a.block_tables[at];
-    if (page < lowest) continue;
+    if (page < 0 || page >= a.num_pages || (uint32_t)page < lowest) continue;
     int lo = 0, hi = n - 1;
     while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (a.moves[2 * (int64_t)mid] <= page) lo = mid; else hi = mid - 1;
+      const int mid = (int)(((int64_t)lo + hi + 1) >> 1);
+      if ((uint32_t)a.moves[2 * (int64_t)mid] <= (uint32_t)page) lo = mid; else hi = mid - 1;
     }
     const int dst = a.moves[2 * (int64_t)lo + 1];
     if (a.moves[2 * (int64_t)lo] == page && dst >= 0 && dst < a.num_pages) a.block_tables[at] = dst;
