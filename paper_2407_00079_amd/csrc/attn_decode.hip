@@ -14,8 +14,8 @@
 //     The next block's K and V are on their way to registers while this one is used, across the ends of heads and rows too; K is
 //     turned into fragments in the wave's own corner of LDS, V needs no turning (attn_narrow.hip has the layout; the products are
 //     the same: S^T = K Q^T, O^T += V^T P^T, the rows of the tile being the query heads of the KV head).
-//   * A softmax runs in one pass with a running reference and sum in fp32.  bf16: p enters P V as two bf16 values, its rounding
-//     and what that left out, so that the output is rounded once (p rounded to 8 bits alone would cost as much again as the output's
+//   * A softmax runs in one pass with a running reference and sum in fp32.  bf16: p enters P V as two bf16 values, its first 8 bits
+//     and what they leave out, so that the output is rounded once (p rounded to 8 bits alone would cost as much again as the output's
 //     own rounding; the matrix units wait for memory anyway).
 //   * A (row, head) that lies within one stretch is finished by its wave.  One that is cut leaves partial results: those of a
 //     workgroup's waves meet in LDS, those of several workgroups - two a workgroup at most, before its first and behind its last
@@ -204,17 +204,22 @@ struct Math<__bf16, D> {
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) s[kt] = mma(Stage::template fragment<bf16x8>(lds, kt, st), qf[st], s[kt]);
   }
+  // p is cut after its first 8 bits, not rounded, so that the rest is never negative, and the rest is 2^-100 at least (or p: some p is
+  // 1 or more), so that it is positive wherever p is: an infinity in V is multiplied by two positive numbers.  2^-16 of p is lost.
   __device__ __forceinline__ void values(const f32x4 (&p)[2], const vvec (&vr)[8], f32x4 (&o)[kVec]) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
     typedef __attribute__((__vector_size__(4))) __bf16 bf16x2;
+    constexpr uint16_t kLeast = (127 - 100) << 7;            // 2^-100 in bf16 (nothing here has a sign: the bits are in the values' order)
     u32x4 hi, lo;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const f32x2 pp = {p[k >> 1][(k & 1) * 2], p[k >> 1][(k & 1) * 2 + 1]};
-      const bf16x2 top = __builtin_convertvector(pp, bf16x2);
-      hi[k] = __builtin_bit_cast(uint32_t, top);
-      const f32x2 rest = {pp[0] - __builtin_bit_cast(float, hi[k] << 16), pp[1] - __builtin_bit_cast(float, hi[k] & 0xffff0000u)};
-      lo[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2));
+      const float a = p[k >> 1][(k & 1) * 2], b = p[k >> 1][(k & 1) * 2 + 1];
+      hi[k] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060302u);
+      const f32x2 rest = {a - __builtin_bit_cast(float, hi[k] << 16), b - __builtin_bit_cast(float, hi[k] & 0xffff0000u)};
+      const u16x2 rounded = __builtin_bit_cast(u16x2, __builtin_convertvector(rest, bf16x2));
+      const u16x2 least = __builtin_elementwise_min(__builtin_bit_cast(u16x2, hi[k]), u16x2{kLeast, kLeast});
+      lo[k] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(rounded, least));
     }
     const bf16x8 ph = __builtin_bit_cast(bf16x8, hi), pl = __builtin_bit_cast(bf16x8, lo);
     l = mma(ones, ph, l);
