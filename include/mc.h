@@ -453,7 +453,7 @@ mc_status mc_decode_attn_paged(const mc_attn_params* p, const void* q, const voi
  */
 #define MC_PAGES_SHORT 1    /* fewer free pages than wanted: nothing was changed */
 #define MC_PAGES_BAD_ROW 2  /* a row or length that the call cannot take; fork and grow changed nothing then */
-#define MC_PAGES_BAD_ID 4   /* a table entry outside the pool, or (free) of a page that was free already: left as it was */
+#define MC_PAGES_BAD_ID 4   /* a table entry outside the pool, or (fork, free) of a page that was free already: left as it was */
 /* Workspace of fork, grow (rows: the table's) and compact (rows 0); 0 for arguments they would refuse. */
 size_t mc_kv_pages_workspace_bytes(int64_t num_pages, int32_t rows);
 
@@ -465,7 +465,8 @@ size_t mc_kv_pages_workspace_bytes(int64_t num_pages, int32_t rows);
  *   src_rows, dst_rows  dev  int32 [n], n <= rows; a dst row has to be empty and to be listed once (else MC_PAGES_BAD_ROW)
  *   moves               dev  int32 [n][2]: report[0] moves, the rest { -1, -1 }
  *   report              { moves, flags, free pages left, pages wanted }; where flags has SHORT or BAD_ROW nothing was changed, no move;
- *                       BAD_ID: some source names a page outside the pool (its counts are left, and mc_kv_copy_pages passes such a move over)
+ *                       BAD_ID: some source names a page outside the pool or a free one.  Its entry is copied as it is, no count of a
+ *                       free page goes up, and its move, whose source is the page outside or -1, is passed over by mc_kv_copy_pages
  *   n == 0 enqueues nothing.
  */
 mc_status mc_kv_pages_fork(int32_t* ref_counts, int64_t num_pages, int32_t* block_tables, int32_t max_pages_per_req, int32_t page_size,

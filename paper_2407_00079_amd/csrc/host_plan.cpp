@@ -1063,7 +1063,8 @@ PagesLayout pages_layout(int64_t num_pages, int32_t rows) {
   lay.lens_off = lay.wanted_off + 4 * n;
   lay.claims_off = lay.lens_off + 4 * n;
   lay.head_off = lay.claims_off + 4 * n;
-  lay.total = lay.head_off + sizeof(PagesHead);
+  lay.map_off = lay.head_off + sizeof(PagesHead);
+  lay.total = lay.map_off + chunks * kPagesMarks;
   return lay;
 }
 

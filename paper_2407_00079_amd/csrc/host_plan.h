@@ -184,7 +184,7 @@ mc_status check_pages(const int32_t* ref_counts, int64_t num_pages, const int32_
                       int32_t page_size, const int32_t* seq_lens, int32_t rows);
 // Where such a call's arrays lie in its workspace; n: rows and entries of a list at most.
 struct PagesLayout {
-  size_t wanted_off, lens_off, claims_off, head_off, total;
+  size_t wanted_off, lens_off, claims_off, head_off, map_off, total;
 };
 PagesLayout pages_layout(int64_t num_pages, int32_t rows);
 

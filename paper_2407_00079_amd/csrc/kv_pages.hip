@@ -15,7 +15,7 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 1024, kWavesHere = kThreads / 64, kPer = kPagesChunk / kThreads;
-static_assert(kPagesChunk % kThreads == 0, "a thread looks at whole pages of a chunk");
+static_assert(kPagesChunk % kThreads == 0 && kPer <= 8 && kThreads == kPagesMarks, "a thread looks at whole pages of a chunk, and has a byte of marks");
 
 // exclusive prefix of x over the workgroup, and the sum of all; every thread calls it
 __device__ __forceinline__ int scan(int x, int* all, int (&room)[kWavesHere]) {
@@ -74,7 +74,10 @@ __device__ __forceinline__ Wish wish_of(const PagesArgs& a, int i) {
   return {pages_of(len + add, a.page_size) - pages_of(len, a.page_size), len, false};
 }
 
-// Workgroups of chunks count free pages; the last one adds up the wishes (n of them; none for a compaction).
+// Whether a page of the pool was free before a fork: of the launch before, since its own launch gives pages out.
+__device__ __forceinline__ bool was_free(const PagesArgs& a, int page) { return a.free_map[page / kPer] >> (page % kPer) & 1; }
+
+// Workgroups of chunks count free pages (and mark them, for a fork); the last one adds up the wishes (n of them; none for a compaction).
 template <bool kFork>
 __global__ __launch_bounds__(kThreads) void pages_count_kernel(const PagesArgs a) {
   __shared__ int room[kWavesHere];
@@ -83,6 +86,12 @@ __global__ __launch_bounds__(kThreads) void pages_count_kernel(const PagesArgs a
     int all;
     scan(free_of(a, blockIdx.x, is_free), &all, room);
     if (threadIdx.x == 0) a.free_before[blockIdx.x] = all;
+    if (kFork) {
+      int marks = 0;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) marks |= is_free[e] << e;
+      a.free_map[(int64_t)blockIdx.x * kThreads + threadIdx.x] = (uint8_t)marks;
+    }
     return;
   }
   if (kFork) {
@@ -166,10 +175,11 @@ __global__ __launch_bounds__(kThreads) void pages_give_kernel(const PagesArgs a)
         if (kFork) {
           const int at = len / a.page_size;
           const int from = a.block_tables[(int64_t)a.list[lo] * a.max_pages + at];
+          const bool inside = from >= 0 && from < a.num_pages, none = inside && was_free(a, from);
           a.block_tables[(int64_t)a.dst_list[lo] * a.max_pages + at] = page;
-          a.moves[2 * (int64_t)rank] = from;
+          a.moves[2 * (int64_t)rank] = none ? -1 : from;
           a.moves[2 * (int64_t)rank + 1] = page;
-          if (from < 0 || from >= a.num_pages) atomicOr(a.report + 1, MC_PAGES_BAD_ID);
+          if (!inside || none) atomicOr(a.report + 1, MC_PAGES_BAD_ID);
         } else {
           a.block_tables[(int64_t)lo * a.max_pages + pages_of(len, a.page_size) + (rank - a.wanted_before[lo])] = page;
         }
@@ -192,7 +202,8 @@ __global__ __launch_bounds__(kThreads) void pages_give_kernel(const PagesArgs a)
     for (int j = threadIdx.x; j < len / a.page_size; j += kThreads) {
       const int page = a.block_tables[(int64_t)src * a.max_pages + j];
       a.block_tables[(int64_t)dst * a.max_pages + j] = page;
-      if (page >= 0 && page < a.num_pages) atomicAdd(a.ref_counts + page, 1);
+      // (a free page keeps its count: another workgroup may be giving it out)
+      if (page >= 0 && page < a.num_pages && !was_free(a, page)) atomicAdd(a.ref_counts + page, 1);
       else atomicOr(a.report + 1, MC_PAGES_BAD_ID);
     }
   }
@@ -345,10 +356,11 @@ __global__ __launch_bounds__(kThreads) void pages_give_alone_kernel(const PagesA
       if (kFork) {
         const int at = lens[lo] / a.page_size;
         const int from = a.block_tables[(int64_t)a.list[lo] * a.max_pages + at];
+        const bool inside = from >= 0 && from < a.num_pages, none = inside && map.is_free(from);
         a.block_tables[(int64_t)a.dst_list[lo] * a.max_pages + at] = page;
-        a.moves[2 * rank] = from;
+        a.moves[2 * rank] = none ? -1 : from;
         a.moves[2 * rank + 1] = page;
-        if (from < 0 || from >= a.num_pages) bad_id = 1;
+        if (!inside || none) bad_id = 1;
       } else {
         a.block_tables[(int64_t)lo * a.max_pages + pages_of(lens[lo], a.page_size) + (rank - wanted_before[lo])] = page;
       }
@@ -360,7 +372,7 @@ __global__ __launch_bounds__(kThreads) void pages_give_alone_kernel(const PagesA
         for (int j = t % 64; j < lens[i] / a.page_size; j += 64) {
           const int page = a.block_tables[(int64_t)src * a.max_pages + j];
           a.block_tables[(int64_t)dst * a.max_pages + j] = page;
-          if (page >= 0 && page < a.num_pages) atomicAdd(a.ref_counts + page, 1);
+          if (page >= 0 && page < a.num_pages && !map.is_free(page)) atomicAdd(a.ref_counts + page, 1);
           else bad_id = 1;
         }
       }

@@ -214,6 +214,7 @@ mc::PagesArgs pages_args(int32_t* ref_counts, int64_t num_pages, int32_t* block_
   a.lens = reinterpret_cast<int32_t*>(ws + lay.lens_off);
   a.claims = reinterpret_cast<int32_t*>(ws + lay.claims_off);
   a.head = reinterpret_cast<mc::PagesHead*>(ws + lay.head_off);
+  a.free_map = reinterpret_cast<uint8_t*>(ws + lay.map_off);
   return a;
 }
 

@@ -122,6 +122,7 @@ struct PagesArgs {
   int32_t max_pages, page_size, rows, n, chunks;
   // in the workspace
   int32_t *free_before;              // free pages of each chunk
+  uint8_t *free_map;                 // (fork) kPagesMarks bytes a chunk, a bit a page: it was free
   int32_t *wanted_before, *lens, *claims;
   PagesHead* head;
 };
