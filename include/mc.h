@@ -448,6 +448,7 @@ mc_status mc_decode_attn_paged(const mc_attn_params* p, const void* q, const voi
  *   seq_lens      int32 [rows]                      tokens of the row; 0: the row is empty
  *   report        int32 [4]                         what the call did: { pages, flags, free pages, pages wanted }, as said below
  *
+ * Pages, rows and rows to free: 2^30 - 1 at most, a table's entries and twice its columns' tokens 2^31 - 1 (MC_ERR_RANGE).
  * Pages are given out lowest first, so the same state gives the same tables.  Calls on one state are ordered by the caller (one
  * stream, or events).  A row, length or page id that is not valid is never followed; the flags say so:
  */

@@ -1047,8 +1047,8 @@ bool decode_by_row(int64_t items, int32_t max_pages) {
 mc_status check_pages(const int32_t* ref_counts, int64_t num_pages, const int32_t* block_tables, int32_t max_pages_per_req,
                       int32_t page_size, const int32_t* seq_lens, int32_t rows) {
   if (num_pages <= 0 || rows < 0 || max_pages_per_req < 0 || page_size <= 0) return MC_ERR_SHAPE;
-  // (twice the pages, and a table's tokens, have to fit 32 bits)
-  if (num_pages > INT32_MAX / 2 || (int64_t)rows * max_pages_per_req > INT32_MAX || (int64_t)max_pages_per_req * page_size > INT32_MAX / 2)
+  // (twice the pages, the rows and a loop's step past them, and a table's tokens, have to fit 32 bits)
+  if (num_pages > kPagesMost || rows > kPagesMost || (int64_t)rows * max_pages_per_req > INT32_MAX || (int64_t)max_pages_per_req * page_size > INT32_MAX / 2)
     return MC_ERR_RANGE;
   if (rows == 0) return MC_OK;
   if (ref_counts == nullptr || block_tables == nullptr || seq_lens == nullptr) return MC_ERR_NULL;

@@ -535,7 +535,7 @@ hipError_t launch_pages_give(bool fork, const PagesArgs& args, hipStream_t strea
 
 hipError_t launch_pages_free(const PagesArgs& args, hipStream_t stream) {
   (void)hipGetLastError();
-  if ((int64_t)args.n * args.max_pages <= kAloneEntries) {
+  if (args.n <= kAloneEntries && (int64_t)args.n * args.max_pages <= kAloneEntries) {
     pages_free_alone_kernel<<<1, kThreads, 0, stream>>>(args);
     return hipGetLastError();
   }

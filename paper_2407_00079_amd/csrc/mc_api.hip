@@ -809,7 +809,7 @@ mc_status mc_decode_attn_paged(const mc_attn_params* p, const void* q, const voi
 }
 
 size_t mc_kv_pages_workspace_bytes(int64_t num_pages, int32_t rows) {
-  return num_pages <= 0 || num_pages > INT32_MAX / 2 || rows < 0 ? 0 : pages_layout(num_pages, rows).total;
+  return num_pages <= 0 || num_pages > mc::kPagesMost || rows < 0 || rows > mc::kPagesMost ? 0 : pages_layout(num_pages, rows).total;
 }
 
 mc_status mc_kv_pages_fork(int32_t* ref_counts, int64_t num_pages, int32_t* block_tables, int32_t max_pages_per_req, int32_t page_size,
@@ -847,6 +847,7 @@ mc_status mc_kv_pages_free(int32_t* ref_counts, int64_t num_pages, const int32_t
   const mc_status st = check_pages(ref_counts, num_pages, block_tables, max_pages_per_req, page_size, seq_lens, rows);
   if (st != MC_OK) return st;
   if (n < 0) return MC_ERR_SHAPE;
+  if (n > mc::kPagesMost) return MC_ERR_RANGE;
   if (n == 0 || rows == 0) return MC_OK;
   if (free_rows == nullptr || report == nullptr) return MC_ERR_NULL;
   if (!aligned4(free_rows) || !aligned4(report)) return MC_ERR_ALIGN;
@@ -859,7 +860,7 @@ mc_status mc_kv_pages_free(int32_t* ref_counts, int64_t num_pages, const int32_t
 mc_status mc_kv_pages_compact(const int32_t* ref_counts, int64_t num_pages, int32_t max_moves, int32_t* moves, int32_t* report,
                               void* workspace, size_t workspace_bytes, void* hip_stream) {
   if (num_pages <= 0 || max_moves < 0) return MC_ERR_SHAPE;
-  if (num_pages > INT32_MAX / 2) return MC_ERR_RANGE;
+  if (num_pages > mc::kPagesMost) return MC_ERR_RANGE;
   if (max_moves == 0) return MC_OK;
   if (ref_counts == nullptr || moves == nullptr || report == nullptr) return MC_ERR_NULL;
   if (!aligned4(ref_counts) || !aligned4(moves) || !aligned4(report) || !aligned16(workspace)) return MC_ERR_ALIGN;

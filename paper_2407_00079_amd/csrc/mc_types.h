@@ -105,6 +105,7 @@ constexpr int decode_wave_of(int64_t total, int64_t x, int waves) { return (int)
 // Page bookkeeping (kv_pages.hip): pages whose free ones one workgroup counts and gives out
 constexpr int kPagesChunk = 4096;
 constexpr int kPagesMarks = 1024;            // bytes of marks a chunk: one a thread, a bit for each of its pages
+constexpr int32_t kPagesMost = INT32_MAX / 2;  // pages, rows and rows to free of a call
 struct PagesHead {
   int32_t wanted, refused;
 };
