@@ -686,7 +686,9 @@ def _dense(names: str, device: int, dtype, *tensors) -> None:
 
 
 def _here(device: int, workspace) -> None:
-    """The tensors' device has to be the current one (streams and launches are its own), and the workspace has to lie there."""
+    """The tensors' device has to be a GPU and the current one (streams and launches are its own), and the workspace has to lie there."""
+    if device < 0:                                         # (before torch has been asked for a GPU, there is no current one to compare with)
+        raise ValueError("tensors in host memory, but tensors on the GPU wanted")
     current = _device() if _device is not None else _torch.cuda.current_device() if _torch.cuda.is_initialized() else device
     if device != current:
         raise ValueError(f"tensors on device {device}, but the current device is {current}")
