@@ -405,8 +405,8 @@ mc_status mc_kv_rope_append_run(const mc_attn_params* p, const mc_attn_plan* pla
  * while the lengths grow.
  *
  *   q, k, v   dev  one token a row: [batch, Hq, D], [batch, Hkv, D] twice
- *   seq_lens  dev  int32 [batch]: the row's length with its new token, which stands at position seq_lens[r] - 1.  A row whose length
- *                  is not in [1, max_pages_per_req * 16] (a padding row: 0) is left out: its q_out and the pools stay as they are
+ *   seq_lens  dev  int32 [batch]: the row's length with its new token, which is written to position seq_lens[r] - 1 whatever
+ *                  stands there (lengths behind a growth that was refused: see mc_kv_pages_grow).  A row whose length is not in [1, max_pages_per_req * 16] (a padding row: 0) is left out: its q_out and the pools stay as they are
  * Nothing is allocated, uploaded or waited for; the call can be captured.
  */
 mc_status mc_kv_rope_append_decode(const mc_attn_params* p, const mc_rope_params* rope, const void* q, const void* k, const void* v,
@@ -476,7 +476,10 @@ mc_status mc_kv_pages_fork(int32_t* ref_counts, int64_t num_pages, int32_t* bloc
 
 /*
  * Row r gets add[r] more tokens (none where add[r] <= 0): its length grows, and the pages that takes are the lowest free ones in row
- * order.  All or nothing: a row that would outgrow its table (or whose length is not valid) is MC_PAGES_BAD_ROW.
+ * order.  All or nothing: a row that would outgrow its table (or whose length is not valid) is MC_PAGES_BAD_ROW.  Where it is refused
+ * (report[1] != 0) all lengths stay as they are, so a step enqueued behind it may not go by them: mc_kv_rope_append_decode would write
+ * each row's last token over, in a page that other rows may share.  Look at the report first, or give the step a copy of the
+ * lengths that is 0 wherever report[1] is not.  (A row of length 0 grows like any other: add is 0 for rows that are to stay empty.)
  *
  *   add     dev  int32 [rows]
  *   report  { pages given, flags, free pages left, pages wanted }
@@ -525,6 +528,7 @@ mc_status mc_kv_pages_remap(int32_t* ref_counts, int64_t num_pages, int32_t* blo
  *
  *   k_pools, v_pools  HOST  [n_layers] device addresses of num_pages * page_bytes each, 16-byte aligned
  *   moves, count      as in mc_kv_pages_remap, in any order
+ * The launch is made for n, whatever count is: up to about 60 us where a long list holds no moves.
  * n_layers > MC_MAX_COPY_LAYERS is MC_ERR_RANGE; page_bytes has to be a multiple of 16.
  */
 #define MC_MAX_COPY_LAYERS 128
