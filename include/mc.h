@@ -406,7 +406,8 @@ mc_status mc_kv_rope_append_run(const mc_attn_params* p, const mc_attn_plan* pla
  *
  *   q, k, v   dev  one token a row: [batch, Hq, D], [batch, Hkv, D] twice
  *   seq_lens  dev  int32 [batch]: the row's length with its new token, which is written to position seq_lens[r] - 1 whatever
- *                  stands there (lengths behind a growth that was refused: see mc_kv_pages_grow).  A row whose length is not in [1, max_pages_per_req * 16] (a padding row: 0) is left out: its q_out and the pools stay as they are
+ *                  stands there (lengths behind a growth that was refused: see mc_kv_pages_grow).  A row whose length is not in
+ *                  [1, max_pages_per_req * 16] (a padding row: 0) is left out: its q_out and the pools stay as they are
  * Nothing is allocated, uploaded or waited for; the call can be captured.
  */
 mc_status mc_kv_rope_append_decode(const mc_attn_params* p, const mc_rope_params* rope, const void* q, const void* k, const void* v,
@@ -446,7 +447,8 @@ mc_status mc_decode_attn_paged(const mc_attn_params* p, const void* q, const voi
  *   ref_counts    int32 [num_pages]                 how many table entries name the page; 0: the page is free
  *   block_tables  int32 [rows, max_pages_per_req]   a row's entries 0 .. ceil(len / page_size) - 1 are its pages
  *   seq_lens      int32 [rows]                      tokens of the row; 0: the row is empty
- *   report        int32 [4]                         what the call did: { pages, flags, free pages, pages wanted }, as said below
+ *   report        int32 [4]                         what the call did: { pages, flags, free pages, pages wanted }, as said below;
+ *                                                   a call that enqueues nothing leaves it as it is
  *
  * Pages, rows and rows to free: 2^30 - 1 at most, a table's entries and twice its columns' tokens 2^31 - 1 (MC_ERR_RANGE).
  * Pages are given out lowest first, so the same state gives the same tables.  Calls on one state are ordered by the caller (one
@@ -483,6 +485,7 @@ mc_status mc_kv_pages_fork(int32_t* ref_counts, int64_t num_pages, int32_t* bloc
  *
  *   add     dev  int32 [rows]
  *   report  { pages given, flags, free pages left, pages wanted }
+ *   rows == 0 enqueues nothing.
  */
 mc_status mc_kv_pages_grow(int32_t* ref_counts, int64_t num_pages, int32_t* block_tables, int32_t max_pages_per_req, int32_t page_size,
                            int32_t* seq_lens, int32_t rows, const int32_t* add, int32_t* report, void* workspace, size_t workspace_bytes,
@@ -492,8 +495,10 @@ mc_status mc_kv_pages_grow(int32_t* ref_counts, int64_t num_pages, int32_t* bloc
  * The listed rows become empty and their pages' counts go down; a row listed twice, or empty, is freed once, or not at all.  Their
  * table entries stay as they are.
  *
- *   free_rows  dev  int32 [n]; a row outside the table is passed over (MC_PAGES_BAD_ROW), as is a length that is not valid
+ *   free_rows  dev  int32 [n]; a row outside the table is passed over (MC_PAGES_BAD_ROW).  A row whose length is not valid becomes
+ *              empty, too (MC_PAGES_BAD_ROW), but which pages are its own cannot be told: no count goes down
  *   report     { pages that became free, flags, 0, 0 }
+ *   n == 0 or rows == 0 enqueues nothing.
  */
 mc_status mc_kv_pages_free(int32_t* ref_counts, int64_t num_pages, const int32_t* block_tables, int32_t max_pages_per_req,
                            int32_t page_size, int32_t* seq_lens, int32_t rows, const int32_t* free_rows, int32_t n, int32_t* report,
@@ -506,6 +511,7 @@ mc_status mc_kv_pages_free(int32_t* ref_counts, int64_t num_pages, const int32_t
  *   max_moves  at most so many moves are listed, the lowest sources first (a bounded step: later calls go on)
  *   moves      dev  int32 [max_moves][2]: { source, destination } by ascending source, then { -1, -1 }
  *   report     { moves listed, 0, free pages, moves it takes in all }
+ *   max_moves == 0 enqueues nothing.
  */
 mc_status mc_kv_pages_compact(const int32_t* ref_counts, int64_t num_pages, int32_t max_moves, int32_t* moves, int32_t* report,
                               void* workspace, size_t workspace_bytes, void* hip_stream);
