@@ -27,8 +27,9 @@
 namespace mc {
 namespace {
 
-constexpr int kRows = 16;              // query heads of a tile
-constexpr int kBlockKeys = 32, kBlockPages = kBlockKeys / kPageTokens;
+constexpr int kRows = kDecodeRows, kBlockKeys = kDecodeBlockKeys, kBlockPages = kBlockKeys / kPageTokens;
+static_assert(kRows == 16 && kBlockKeys == 32, "a tile is a matrix instruction's 16 query heads, a block its 32 keys of P V");
+static_assert(kWaves == kDecodeWaves, "the host bounds the line by the waves of a launch");
 
 template <int N>
 struct Int {

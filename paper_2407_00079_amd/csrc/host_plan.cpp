@@ -1030,7 +1030,7 @@ DecodeLayout decode_layout(const mc_attn_params* p) {
 }
 
 bool decode_fits(const mc_attn_params* p, int32_t batch, int32_t max_pages) {
-  static_assert(kDecodeWgs * 8 == 1 << 11, "the waves of a launch");
+  static_assert(kDecodeWgs * kDecodeWaves == 1 << 11, "the waves of a launch");
   if ((int64_t)batch * p->num_q_heads > 1 << 26) return false;
   const int64_t blocks = (int64_t)batch * (max_pages / (kDecodeBlockKeys / 16) + 1);       // at most, of one head
   return blocks <= ((int64_t)1 << 51) / p->num_q_heads;      // (a tile of query heads has one at least)

@@ -168,7 +168,6 @@ bool auto_layout(const mc_attn_params* p, const int32_t* prefix_lens, const int3
 // any request.
 bool hash_in_one_launch(int64_t max_blocks, int64_t max_tokens);
 
-// arguments of a page copy (pack / unpack and their relatives): a, b source pair, c, d destination pair
 // Where the parts of a decode call lie in its workspace.
 struct DecodeLayout {
   size_t ml_off, meta_off, total;
@@ -194,6 +193,7 @@ mc_status check_rope(const mc_attn_params* p, const mc_rope_params* rope, const 
 mc_status rope_init(mc_rope_params* rope, int32_t rotary_dim, double base, int32_t scaling, double factor, double low, double high,
                     double original_len);
 
+// arguments of a page copy (pack / unpack and their relatives): a, b source pair, c, d destination pair
 mc_status check_copy(const void* a, const void* b, int64_t num_pages, int64_t page_bytes, const int32_t* ids,
                      int64_t n, const void* c, const void* d);
 

@@ -125,9 +125,9 @@ __global__ __launch_bounds__(kThreads) void pages_count_kernel(const PagesArgs a
   }
 }
 
-// What every workgroup of a second launch knows: free pages in all, before its chunk, and before `upto` (a page).
+// What every workgroup of a second launch knows: free pages in all, and before its chunk.
 struct Free {
-  int all, before, below;
+  int all, before;
 };
 __device__ __forceinline__ Free free_pages(const PagesArgs& a, int chunk, int (&room)[kWavesHere]) {
   int all = 0, before = 0;
@@ -136,7 +136,7 @@ __device__ __forceinline__ Free free_pages(const PagesArgs& a, int chunk, int (&
     all += n;
     before += c < chunk ? n : 0;
   }
-  Free f = {0, 0, 0};
+  Free f = {0, 0};
   scan(all, &f.all, room);
   scan(before, &f.before, room);
   return f;
@@ -288,7 +288,7 @@ __global__ __launch_bounds__(kThreads) void pages_compact_kernel(const PagesArgs
 }
 
 // Small states, one launch: one workgroup finds the free pages of the whole pool (a bit a page in LDS, and how many lie before each
-// word) and does what the two launches above do.  Four rows forked, grown and freed, with the copy, and a clone of the tables
+// word; a thread asks for the counts of 16 pages at once) and does what the two launches above do.  Four rows forked, grown and freed, with the copy, and a clone of the tables
 // 44.6 us a pass, so 30.3; a step of 48 moves in a pool of 4096 pages 32.5, so 27.5.
 constexpr int kAlonePages = 16384, kAloneRounds = kAlonePages / kThreads, kAloneWords = kAlonePages / 64;
 struct FreeMap {
@@ -510,8 +510,9 @@ __global__ __launch_bounds__(kCopyThreads) void pages_copy_kernel(const LayerPoo
 }  // namespace
 
 // One workgroup or several (us, alone / in two launches, a pool of 16384 pages): 4 rows of 64 pages forked 8.0 / 9.3 and freed 2.9 /
-// 4.1, 16 rows of 256 pages 13.2 / 10.2 and 8.4 / 4.6: at most so many table entries.  Growth of 64 rows 7.3 / 10.6, a compaction
-// 6.5 / 8.2 (4096 pages: 4.3 / 7.7).
+// 4.1, 16 rows of 256 pages 13.2 / 10.2 and 8.4 / 4.6: at most so many table entries.  64 rows grown by a page each 7.8 / 11.7, by a
+// token 7.5 / 6.4, a compaction 6.4 / 8.2 (4096 pages: 6.3 / 11.2, 5.9 / 6.3, 4.5 / 8.0).  Pools of more than kAlonePages would need more
+// counts a thread: four times as many cost 4.8 us at any size, and 24576 pages 13.5 / 11.9, 13.3 / 6.8, 12.5 / 8.4 then.
 constexpr int64_t kAloneEntries = 1 << 10;
 
 hipError_t launch_pages_give(bool fork, const PagesArgs& args, hipStream_t stream) {

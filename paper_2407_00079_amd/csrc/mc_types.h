@@ -87,6 +87,7 @@ constexpr int kXcds = 8;
 // Decode attention (attn_decode.hip): `total` blocks of keys in one line, shared out over waves in equal stretches.  total is at most
 // 2^51 (decode_fits), so its product with the waves, 2^11, fits.
 constexpr int kDecodeWgs = 256;              // one a compute unit
+constexpr int kDecodeWaves = 8;              // of each
 constexpr int kDecodeRows = 16;              // query heads of a tile
 constexpr int kDecodeBlockKeys = 32;
 struct DecodeMeta {
