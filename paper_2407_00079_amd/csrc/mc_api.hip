@@ -190,7 +190,7 @@ mc::RopeArgs rope_args(const mc_attn_params* p, const mc_rope_params* rope, cons
   a.k_stride = strides != nullptr ? strides[1] * elem : p->num_kv_heads * row;
   a.v_stride = strides != nullptr ? strides[2] * elem : p->num_kv_heads * row;
   a.total_tokens = (int32_t)tokens;
-  // exact for dividends x with x * rows < 2^32: a workgroup divides less than its own 160 rows plus one token's (check_rope_buffers)
+  // exact for dividends x with x * rows < 2^32: a workgroup divides less than its own 64 rows plus one token's (check_rope_buffers)
   a.rows_inverse = (uint32_t)((((uint64_t)1 << 32) + rows - 1) / rows);
   a.Hq = p->num_q_heads, a.Hkv = p->num_kv_heads, a.max_pages = max_pages;
   a.rotary = rope->rotary_dim, a.layout = rope->layout;

@@ -17,8 +17,9 @@
 // are: loads go out first, and under their latency the tokens of the rows are looked up and their angles computed, once a
 // token and pair, into LDS.
 //
-// What bounds it: HBM.  8192 tokens of 64/8 heads, 335 MB read and written: 60.5 us, 5.55 TB/s where a plain copy reaches 6.05; 19505
-// tokens of 32/4 heads in 16 requests 69 us (5.8).  64 single tokens: 3.7 us, a launch and two memory latencies.
+// What bounds it: HBM.  8192 tokens of 64/8 heads, 335 MB read and written: 56.1 us, 5.98 TB/s where a plain copy reaches 6.05; 19505
+// tokens of 32/4 heads in 16 requests 65.6 us (6.09).  64 single tokens of 64/8 heads, with norms: 4.6 us in a trace, a launch and two
+// memory latencies (3.8 a call where a graph has one behind the other).
 #include "mc_internal.h"
 
 namespace mc {
@@ -142,7 +143,8 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(const RopeArgs a,
   const int slot = threadIdx.x / kLanes, gran = threadIdx.x % kLanes;
 
   // (Every lane loads, those without a row of their own the last one: behind a branch each load would be waited for by itself.)
-  // Many rows pass the caches by (8192 tokens of 64/8 heads 66.9 -> 60.7 us, loads alone 65.9); few are read again at once, by attention.
+  // Many rows pass the caches by (8192 tokens of 64/8 heads 66.9 -> 60.7 us, loads alone 65.9; five rows a lane group then); few are read
+  // again at once, by attention.
   auto take = [](const char* at) __attribute__((always_inline)) {
     const u32x4* const v = reinterpret_cast<const u32x4*>(at);
     return U == 1 ? *v : __builtin_nontemporal_load(v);
@@ -249,14 +251,13 @@ void enqueue(const RopeArgs& args, const Source& source, hipStream_t stream) {
   constexpr int kSlots = kThreads / (D / Granule<T>::kElems);
   const int rows = args.Hq + 2 * args.Hkv;
   auto grid = [&](int u) { return (unsigned)(((int64_t)args.total_tokens * rows + kSlots * u - 1) / (kSlots * u)); };
-  // Few rows: one a lane group, so that they spread over the chip.  Else several, whose loads are in flight together: as many as
-  // make a workgroup's rows whole tokens or a token's rows whole workgroups, where 3 to 5 do.  us, one / several: 64/8 heads, 64
-  // tokens 3.7 / 6.4, 400 5.9 / 7.5, 512 7.5 / 7.6, 1024 12.5 / 10.5; 8/1 heads, 64 tokens 3.4 / 7.0, 4096 7.8 / 8.6.
-  auto even = [&](int u) { return rows % (kSlots * u) == 0 || kSlots * u % rows == 0; };
-  if (grid(4) < 3 * 256) rope_append_kernel<T, D, 1><<<grid(1), kThreads, 0, stream>>>(args, source);
-  else if (even(5)) rope_append_kernel<T, D, 5><<<grid(5), kThreads, 0, stream>>>(args, source);
-  else if (even(3) && !even(4)) rope_append_kernel<T, D, 3><<<grid(3), kThreads, 0, stream>>>(args, source);
-  else rope_append_kernel<T, D, 4><<<grid(4), kThreads, 0, stream>>>(args, source);
+  // Few rows: one a lane group, so that they spread over the chip.  Else two, whose loads are in flight together, from two workgroups a
+  // compute unit on.  us a call in a graph, with norms, 1 / 2 / 3 / 4 / 5 rows: 64/8 heads, 64 tokens 3.8 / 4.3 / 5.2 / 5.8 / 6.5, 128 4.8 / 5.0 /
+  // 5.7 / 6.4 / 7.1, 256 5.8 / 5.5 / 6.2 / 6.9 / 7.4, 1024 14.6 / 11.0 / 10.8 / 10.5 / 10.8, 2048 25.3 / 18.6 / 19.7 / 20.8 / 20.7, 8192 81.7 / 58.4 /
+  // 60.3 / 62.6 / 65.1; 8/1 heads, 1024 tokens 5.0 / 5.2 / 6.3 / 7.0 / 7.8, 2048 6.1 / 5.8 / 6.8 / 7.6 / 8.1; 32/8 heads of 64, 8192 tokens 26.3 / 21.0 /
+  // 21.5 / 22.8 / 23.4, in fp32 45.0 / 36.3 / 38.4 / 39.1 / 40.1.
+  if (grid(2) < 2 * 256) rope_append_kernel<T, D, 1><<<grid(1), kThreads, 0, stream>>>(args, source);
+  else rope_append_kernel<T, D, 2><<<grid(2), kThreads, 0, stream>>>(args, source);
 }
 template <typename Source>
 hipError_t launch(int dtype, int head_dim, const RopeArgs& args, const Source& source, hipStream_t stream) {
