@@ -434,7 +434,8 @@ mc_status mc_kv_rope_append_decode(const mc_attn_params* p, const mc_rope_params
  * Slots at or past a row's length are never used as values (they may hold NaN).  fp32 accumulation and softmax; output rounded
  * once, to nearest even; what is not finite gives what the definition gives (a probability below fp32's range is 0).  The same lengths and inputs give the same bits.  batch * Hq > 2^26, or tables so wide that all rows' blocks
  * of 32 keys times Hq exceed 2^51, is MC_ERR_RANGE; batch == 0 enqueues nothing.  Nothing is allocated, uploaded or waited for; the
- * call can be captured.
+ * call can be captured.  Rows that begin with the same page and stand within 32 rows of each other read it through the caches, others'
+ * K and V pass them by (which costs time where far rows share pages, and changes no result).
  */
 size_t mc_decode_attn_workspace_bytes(const mc_attn_params* p, int32_t batch);
 mc_status mc_decode_attn_paged(const mc_attn_params* p, const void* q, const void* k_pool, const void* v_pool,
@@ -457,7 +458,8 @@ mc_status mc_decode_attn_paged(const mc_attn_params* p, const void* q, const voi
 #define MC_PAGES_SHORT 1    /* fewer free pages than wanted: nothing was changed */
 #define MC_PAGES_BAD_ROW 2  /* a row or length that the call cannot take; fork and grow changed nothing then */
 #define MC_PAGES_BAD_ID 4   /* a table entry outside the pool, or (fork, free) of a page that was free already: left as it was */
-/* Workspace of fork, grow (rows: the table's) and compact (rows 0); 0 for arguments they would refuse. */
+/* Workspace of fork, grow (rows: the table's) and compact (rows 0); 0 for arguments they would refuse.  16-byte aligned, of any contents;
+ * calls that may overlap, and captured graphs that may, need one each. */
 size_t mc_kv_pages_workspace_bytes(int64_t num_pages, int32_t rows);
 
 /*

@@ -7,8 +7,8 @@
 // bytes whatever the lengths are.  The keys of every (row, KV head) are cut into blocks of 32, all blocks of the batch stand in one
 // line (row by row, head by head), and each of the 256 x 8 waves takes an equal stretch of the line.  Where its stretch begins
 // a wave finds from the lengths (all of them look them over), so no host plan is made and a captured launch follows the lengths as
-// they grow.  131071 keys of 64/8 heads: 537 MB (as counted, too) in 82.7 us, 6.5 TB/s of the 6.7 that reading alone reaches, and 5.6
-// for what is joined behind; 48 rows of 120 to 8000 tokens 62.5 and 4.5 us; 128 rows of 20 to 2500 tokens, head_dim 64, 27 and 4.
+// they grow.  131071 keys of 64/8 heads: 537 MB (as counted, too) in 82.4 us, 6.5 TB/s of the 6.7 that reading alone reaches, and 5.5
+// for what is joined behind; 48 rows of 120 to 8000 tokens 62.8 and 4.7 us; 128 rows of 20 to 2500 tokens, head_dim 64, 26.7 and 4.6.
 //
 //   * A wave walks its stretch by itself: no barrier in the loop (one a block, to keep a workgroup's waves together, gains nothing).
 //     The next block's K and V are on their way to registers while this one is used, across the ends of heads and rows too; K is

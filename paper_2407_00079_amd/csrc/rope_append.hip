@@ -18,7 +18,7 @@
 // token and pair, into LDS.
 //
 // What bounds it: HBM.  8192 tokens of 64/8 heads, 335 MB read and written: 56.1 us, 5.98 TB/s where a plain copy reaches 6.05; 19505
-// tokens of 32/4 heads in 16 requests 65.6 us (6.09).  64 single tokens of 64/8 heads, with norms: 4.6 us in a trace, a launch and two
+// tokens of 32/4 heads in 16 requests 65.6 us (6.09).  64 single tokens of 64/8 heads, with norms: 4.6 to 5.1 us in a trace, a launch and two
 // memory latencies (3.8 a call where a graph has one behind the other).
 #include "mc_internal.h"
 
