@@ -683,6 +683,149 @@ mc_status mc_prefix_match(const uint64_t* keys, const int64_t* key_offsets, int3
                           int32_t* prefix_len, int32_t* best_len, int32_t* best_inst, void* workspace,
                           size_t workspace_bytes, void* hip_stream);
 
+/*
+ * A cache of latent vectors.  A token leaves one row of R + P numbers in a layer's cache instead of K and V of every KV head: a latent
+ * vector c of R numbers that the keys and values of all heads are made from, and a key part r of P numbers, rotated by the token's
+ * position, that all heads share.  With a layer's weights A_h and B_h (head_dim x R each) head h has, of token j,
+ *
+ *   K_h(j) = [A_h c(j), r(j)]   (head_dim + P numbers),      V_h(j) = B_h c(j)   (head_dim numbers)
+ *
+ * and attention can be written in two ways:
+ *
+ *   expanded   mc_latent_expand_paged makes A_h c and B_h c of whole requests, mc_latent_prefill_attn_paged attends to them.  For prompts:
+ *              2 (2 head_dim + P) operations a head, query and key
+ *   absorbed   A_h goes into the query (A_h^T q_h has R numbers) and B_h behind the attention: mc_latent_decode_attn_paged attends to the cache rows
+ *              themselves.  For new tokens: a key is R + P numbers whatever the number of heads
+ *
+ *   pool  dev  [num_pages, page_size, R + P]   a layer's cache: row j of a request is pool[block_tables[r][j / 16]][j % 16][:] = [c(j), r(j)]
+ *
+ * Block tables, lengths and the care of pages (mc_kv_pages_*) are those of the other cache; the calls that move pages take two pools at a time
+ * (mc_kv_copy_pages, mc_kv_pack_layer and their relatives): give them two layers' pools.
+ */
+typedef struct {
+  int32_t num_heads;    /* H: 1 .. 1024 */
+  int32_t latent_dim;   /* R: 512 or 256 */
+  int32_t rope_dim;     /* P: 64 */
+  int32_t head_dim;     /* of the expanded form, keys without their rotated part and values alike: 128 or 64 */
+  int32_t page_size;    /* 16 */
+  int32_t dtype;        /* MC_DTYPE_BF16 */
+  int64_t num_pages;    /* N pages in a pool */
+  float softmax_scale;  /* 0 selects 1 / sqrt(head_dim + rope_dim), in both forms */
+} mc_latent_params;
+#define MC_LATENT_MAX_HEADS 1024
+#define MC_LATENT_MAX_TOKENS 16
+
+/* Bytes of device workspace of mc_latent_append_paged and mc_latent_expand_paged (a table of the requests).  0 for batch < 0. */
+size_t mc_latent_workspace_bytes(int32_t batch);
+
+/*
+ * New tokens' projections become cache rows, in one pass:
+ *
+ *   c' = c * rsqrt(mean(c^2) + norm_eps) * norm        (norm NULL: c' = c),      r' = r rotated,      pool row of the token = [c', r']
+ *   q_out = the P rotated columns of every head's query
+ *
+ * with the rotation of mc_kv_rope_append_paged (rope->rotary_dim has to be P) by the token's position P_r + i.  fp32 between the load and the one
+ * rounding; angles in 64 bits.
+ *
+ *   q        dev   [total_new_tokens, H, P]    what is rotated of the queries: columns of a wider tensor, as a rule
+ *   kv       dev   [total_new_tokens, R + P]   c and r of a token
+ *   strides  host  int64 [5], in elements: q from token to token and from head to head, kv from token to token, q_out from token to token and
+ *                  from head to head; NULL: all of them dense.  Multiples of 8, none negative; rows of q_out may not overlap each other
+ *   norm     dev   [R], or NULL
+ *   q_out    dev   [total_new_tokens, H, P], such as the last columns of what an attention call takes as q; may be q itself with q's strides, may not
+ *                  overlap the inputs otherwise
+ *   pool     dev   written in place; other slots keep their bytes
+ *   block_tables, max_pages_per_req, prefix_lens, new_lens, batch  as in mc_kv_append_paged
+ *   workspace  dev  >= mc_latent_workspace_bytes(batch), 16-byte aligned
+ *
+ * More than 64 requests are uploaded (no stream capture then).  Two requests whose block tables name the same page for positions both write:
+ * undefined which wins.
+ */
+mc_status mc_latent_append_paged(const mc_latent_params* p, const mc_rope_params* rope, const void* q, const void* kv,
+                                 const int64_t* strides, const void* norm, void* q_out, void* pool, const int32_t* block_tables,
+                                 int32_t max_pages_per_req, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch,
+                                 void* workspace, size_t workspace_bytes, void* hip_stream);
+/*
+ * The same for `tokens` new tokens a row (1 .. MC_LATENT_MAX_TOKENS: a step of decoding, or drafted tokens with it), lengths in DEVICE memory: token t of
+ * row r stands at position seq_lens[r] - tokens + t.  Tokens before position 0, and all tokens of a row whose length is not in
+ * [1, max_pages_per_req * 16] (a padding row: 0), are left out: their q_out and the pool stay as they are.  What mc_kv_rope_append_decode says of
+ * lengths behind a growth that was refused holds here, too.  Nothing is allocated, uploaded or waited for; the call can be captured.
+ *
+ *   q, kv, q_out  dev  [batch * tokens, ...], a row's tokens together
+ *   seq_lens      dev  int32 [batch]: the row's length with its new tokens
+ */
+mc_status mc_latent_append_decode(const mc_latent_params* p, const mc_rope_params* rope, const void* q, const void* kv,
+                                  const int64_t* strides, const void* norm, void* q_out, void* pool, const int32_t* block_tables,
+                                  int32_t max_pages_per_req, const int32_t* seq_lens, int32_t batch, int32_t tokens, void* hip_stream);
+
+/*
+ * Attention of `tokens` new tokens a row in the absorbed form, lengths in DEVICE memory.  Token t of row r sees the n = seq_lens[r] - tokens + t + 1 keys up
+ * to its own:
+ *
+ *   x(j)       = scale * q[r,t,h,:] . pool row j        (R + P numbers)
+ *   out[r,t,h] = sum_{j < n} softmax_j(x(j)) * c(j)     (R numbers)
+ *   lse[r,t,h] = log sum_{j < n} exp(x(j))              (natural log)
+ *
+ *   q            dev  [batch, tokens, H, R + P]: A_h^T q_h, then the rotated columns
+ *   pool, block_tables, seq_lens  as above; the new tokens' rows are in their slots
+ *   out          dev  [batch, tokens, H, R], every row written: 0 where n <= 0 or the row's length is not in [1, max_pages_per_req * 16]
+ *   lse          dev  [batch, tokens, H] fp32, or NULL; -inf there
+ *   workspace    dev  >= mc_latent_decode_attn_workspace_bytes(...) (the same for every length), 16-byte aligned; calls that may overlap, and captured
+ *                     graphs that may, need one each
+ *
+ * Slots at or past what a token sees are never used as values (they may hold NaN).  Products on the matrix cores, fp32 accumulation and softmax;
+ * probabilities are rounded to bf16 before they meet c, as in the bf16 prefill attention.  A key that a token sees and whose score is NaN or +inf
+ * makes the token's row NaN.  The same lengths and inputs give the same bits.  Nothing is allocated, uploaded or waited for; the call can be captured.
+ * batch * tokens * H > 2^26 or batch * max_pages_per_req > 2^31 - 1 is MC_ERR_RANGE; batch == 0 enqueues nothing.
+ */
+size_t mc_latent_decode_attn_workspace_bytes(const mc_latent_params* p, int32_t batch, int32_t tokens);
+mc_status mc_latent_decode_attn_paged(const mc_latent_params* p, const void* q, const void* pool, const int32_t* block_tables,
+                                      int32_t max_pages_per_req, const int32_t* seq_lens, int32_t batch, int32_t tokens, void* out,
+                                      float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Keys and values of all heads from the cache rows of whole requests (one layer):
+ *
+ *   kv[t, h, :] = [A_h c(t), B_h c(t)],      requests back to back, lens[r] tokens of request r
+ *
+ *   weight  dev   [H * 2 * head_dim, R]: of each head the head_dim rows of A_h, then those of B_h
+ *   lens    host  [batch], >= 0: tokens of each request, reused and new ones alike
+ *   kv      dev   [sum of lens, H, 2 * head_dim], dense, every row written; rounded to nearest even from fp32 sums
+ *   workspace  dev  >= mc_latent_workspace_bytes(batch), 16-byte aligned
+ *
+ * More than 64 requests are uploaded (no stream capture then).  No tokens at all: nothing is enqueued.
+ */
+mc_status mc_latent_expand_paged(const mc_latent_params* p, const void* weight, const void* pool, const int32_t* block_tables,
+                                 int32_t max_pages_per_req, const int32_t* lens, int32_t batch, void* kv, void* workspace,
+                                 size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Chunked-prefill attention in the expanded form: as mc_prefill_attn_paged, with every head's own keys and values in memory and the shared key part
+ * in the pages.
+ *
+ *   x(j)     = scale * (q[i,h,:D] . k[j,h,:] + q[i,h,D:] . r(j)),      D = head_dim, j <= P_r + i
+ *   out[i,h] = sum_j softmax_j(x(j)) * v[j,h,:],      lse[i,h] = log sum_j exp(x(j))
+ *
+ *   q        dev   [total_new_tokens, H, D + P] dense, requests back to back
+ *   k, v     dev   [sum of P_r + C_r, H, D]: the keys and values of all of a request's tokens, requests (those without new tokens, too) back to back
+ *   strides  host  int64 [4], in elements: k from token to token and from head to head, v likewise; NULL: those of mc_latent_expand_paged's output
+ *                  (2 D H and 2 D).  Multiples of 8, none negative, from token to token at most 2^26
+ *   pool, block_tables  for r(j)
+ *   prefix_lens, new_lens  host [batch], as in mc_prefill_attn_paged
+ *   out      dev   [total_new_tokens, H, D] dense, every row written
+ *   lse      dev   [total_new_tokens, H] fp32, or NULL
+ *   workspace  dev  >= mc_latent_prefill_attn_workspace_bytes(...) for the same lengths, 16-byte aligned
+ *
+ * A key that a row does not see is never used as a value for it (its k, v and r may hold NaN).  Products on the matrix cores, fp32
+ * accumulation and softmax; probabilities rounded to bf16 before they meet v.  More than 64 requests are uploaded (no stream capture then).
+ * No new tokens: nothing is enqueued.
+ */
+size_t mc_latent_prefill_attn_workspace_bytes(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch);
+mc_status mc_latent_prefill_attn_paged(const mc_latent_params* p, const void* q, const void* k, const void* v, const int64_t* strides,
+                                       const void* pool, const int32_t* block_tables, int32_t max_pages_per_req,
+                                       const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, void* out, float* lse,
+                                       void* workspace, size_t workspace_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

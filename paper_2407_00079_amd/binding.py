@@ -30,12 +30,15 @@ EXPORTS = ("mc_status_string", "mc_prefill_attn_workspace_bytes", "mc_prefill_at
            "mc_prefill_attn_paged_noalloc", "mc_rope_init", "mc_kv_rope_append_paged", "mc_kv_rope_append_run",
            "mc_kv_rope_append_decode", "mc_decode_attn_workspace_bytes", "mc_decode_attn_paged",
            "mc_kv_pages_workspace_bytes", "mc_kv_pages_fork", "mc_kv_pages_grow", "mc_kv_pages_free", "mc_kv_pages_compact",
-           "mc_kv_pages_remap", "mc_kv_copy_pages")
+           "mc_kv_pages_remap", "mc_kv_copy_pages", "mc_latent_workspace_bytes", "mc_latent_append_paged", "mc_latent_append_decode",
+           "mc_latent_decode_attn_workspace_bytes", "mc_latent_decode_attn_paged", "mc_latent_expand_paged",
+           "mc_latent_prefill_attn_workspace_bytes", "mc_latent_prefill_attn_paged")
 MC_PAGES_SHORT, MC_PAGES_BAD_ROW, MC_PAGES_BAD_ID = 1, 2, 4
 MC_MAX_COPY_LAYERS = 128
 MC_ROPE_HALF, MC_ROPE_PAIRS = 0, 1
 MC_ROPE_PLAIN, MC_ROPE_LINEAR, MC_ROPE_BASE, MC_ROPE_BY_PARTS = 0, 1, 2, 3
 MC_MAX_KV_SPLITS = 256
+MC_LATENT_MAX_HEADS, MC_LATENT_MAX_TOKENS = 1024, 16
 
 
 class McAttnParams(ctypes.Structure):
@@ -43,6 +46,11 @@ class McAttnParams(ctypes.Structure):
                 ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
                 ("num_pages", ctypes.c_int64), ("dtype", ctypes.c_int32),
                 ("softmax_scale", ctypes.c_float)]
+
+
+class McLatentParams(ctypes.Structure):
+    _fields_ = [("num_heads", ctypes.c_int32), ("latent_dim", ctypes.c_int32), ("rope_dim", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("dtype", ctypes.c_int32), ("num_pages", ctypes.c_int64), ("softmax_scale", ctypes.c_float)]
 
 
 class McAttnPlan(ctypes.Structure):
@@ -163,6 +171,16 @@ def lib():
         l.mc_kv_pages_compact.argtypes = [vp, i64, i32, vp, vp, vp, sz, vp]
         l.mc_kv_copy_pages.restype = ctypes.c_int
         l.mc_kv_copy_pages.argtypes = [vp, vp, i32, i64, i64, vp, vp, i32, vp]
+        lp = ctypes.POINTER(McLatentParams)
+        for f, args in ((l.mc_latent_workspace_bytes, [i32]), (l.mc_latent_decode_attn_workspace_bytes, [lp, i32, i32]),
+                        (l.mc_latent_prefill_attn_workspace_bytes, [lp, vp, vp, i32])):
+            f.restype, f.argtypes = sz, args
+        for f, args in ((l.mc_latent_append_paged, [lp, rp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, i32, vp, sz, vp]),
+                        (l.mc_latent_append_decode, [lp, rp, vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, i32, vp]),
+                        (l.mc_latent_decode_attn_paged, [lp, vp, vp, vp, i32, vp, i32, i32, vp, vp, vp, sz, vp]),
+                        (l.mc_latent_expand_paged, [lp, vp, vp, vp, i32, vp, i32, vp, vp, sz, vp]),
+                        (l.mc_latent_prefill_attn_paged, [lp, vp, vp, vp, vp, vp, vp, i32, vp, vp, i32, vp, vp, vp, sz, vp])):
+            f.restype, f.argtypes = ctypes.c_int, args
         try:
             from . import _mccall
         except ModuleNotFoundError:                        # none was built for this Python
@@ -223,11 +241,19 @@ _CACHE_KINDS = {
     "mc_kv_pages_remap": "pipiipippii",
     "mc_kv_copy_pages": "QQiiippii",
 }
-_ALL_KINDS = {**_KINDS, **_CACHE_KINDS}
+# ... and of those on a cache of latent vectors.
+_LATENT_KINDS = {
+    "mc_latent_append_paged": "ssppsppppiIIipii",
+    "mc_latent_append_decode": "ssppsppppipiii",
+    "mc_latent_decode_attn_paged": "spppipiipppii",
+    "mc_latent_expand_paged": "spppiIippii",
+    "mc_latent_prefill_attn_paged": "spppsppiIIipppii",
+}
+_ALL_KINDS = {**_KINDS, **_CACHE_KINDS, **_LATENT_KINDS}
 
 
 def _enqueue(name: str, *args) -> None:
-    """The library's function ``name`` with arguments as _KINDS and _CACHE_KINDS have them."""
+    """The library's function ``name`` with arguments as _ALL_KINDS has them."""
     if _call is None:
         lib()
     st = _call(_function[name], _ALL_KINDS[name], *args)
@@ -866,3 +892,135 @@ def mc_kv_copy_pages(k_pools, v_pools, num_pages: int, page_bytes: int, moves, c
     layers = len(k_pools)
     _enqueue("mc_kv_copy_pages", _ints("q", [t.data_ptr() for t in k_pools], layers), _ints("q", [t.data_ptr() for t in v_pools], layers),
              layers, num_pages, page_bytes, moves, count, n, _on(stream))
+
+
+# ---- a cache of latent vectors ----
+
+def latent_params(num_heads: int, latent_dim: int, rope_dim: int, head_dim: int, page_size: int, num_pages: int, dtype: str = "bf16",
+                  softmax_scale: float = 0.0) -> McLatentParams:
+    return McLatentParams(num_heads, latent_dim, rope_dim, head_dim, page_size, MC_DTYPE_BF16 if dtype == "bf16" else MC_DTYPE_F32, num_pages,
+                          softmax_scale)
+
+
+def _latent(params):
+    """torch's type of a call's tensors; parameters that have none are refused as the library does."""
+    if params is None:
+        raise McError(MC_ERR_NULL, "params")
+    if not isinstance(params, McLatentParams):
+        raise TypeError(f"McLatentParams wanted, not {type(params).__name__}")
+    if params.dtype != MC_DTYPE_BF16:
+        raise McError(MC_ERR_UNSUPPORTED, f"dtype {params.dtype}")
+    return (_DTYPES or _dtypes())[params.dtype]
+
+
+def _rows_of_heads(name: str, device: int, dtype, t, tokens: int, heads: int, dim: int):
+    """Elements from token to token and from head to head of [tokens, heads, dim] whose rows are dense."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != tokens or shape[1] != heads or shape[2] != dim or stride[2] != 1 or t.dtype is not dtype or \
+            t.get_device() != device:
+        raise ValueError(f"{name}: {dtype} [{tokens}, {heads}, {dim}] with dense rows on device {device} wanted, not {_is(t)}")
+    return stride[0] if tokens > 1 else heads * dim, stride[1] if heads > 1 else dim
+
+
+def _latent_pool(params, device: int, dtype, pool, block_tables, rows: int, workspace) -> int:
+    _dense("pool", device, dtype, pool, params.num_pages * params.page_size * (params.latent_dim + params.rope_dim))
+    wide = _table(block_tables, rows)
+    _dense("block_tables", device, _torch.int32, block_tables, 0)
+    _here(device, workspace)
+    return wide
+
+
+def _latent_new(params, q, kv, norm, q_out, tokens: int):
+    """Looks the tensors of an append over: (device, type, strides)."""
+    dtype = _latent(params)
+    device, H, P, row = q.get_device(), params.num_heads, params.rope_dim, params.latent_dim + params.rope_dim
+    a = _rows_of_heads("q", device, dtype, q, tokens, H, P)
+    b = _row_stride(device, dtype, kv, tokens, 1, row)
+    c = _rows_of_heads("q_out", device, dtype, q_out, tokens, H, P)
+    if b < 0:
+        raise ValueError(f"kv: {dtype} [{tokens}, {row}] with dense rows on device {device} wanted, not {_is(kv)}")
+    if norm is not None:
+        _dense("norm", device, dtype, norm, params.latent_dim)
+    return device, dtype, (ctypes.c_int64 * 5)(*a, b, *c)
+
+
+def mc_latent_workspace_bytes(batch: int) -> int:
+    return int(lib().mc_latent_workspace_bytes(batch))
+
+
+def mc_latent_append_paged(params: McLatentParams, rope: McRopeParams, q, kv, norm, q_out, pool, block_tables, prefix_lens, new_lens,
+                           workspace, stream=None) -> None:
+    """Enqueue norm, rotation and append of the new tokens' rows.
+
+    q, q_out: [tokens, heads, rope_dim] with dense rows (columns of wider tensors); kv: [tokens, latent_dim + rope_dim]; norm: weights or None."""
+    n = len(prefix_lens)
+    if len(new_lens) != n:
+        raise ValueError(f"{n} prefix lengths and {len(new_lens)} new lengths")
+    device, dtype, strides = _latent_new(params, q, kv, norm, q_out, sum(new_lens))
+    wide = _latent_pool(params, device, dtype, pool, block_tables, n, workspace)
+    _enqueue("mc_latent_append_paged", params, _rope(rope), q, kv, strides, norm, q_out, pool, block_tables, wide, _ints("i", prefix_lens, n),
+             _ints("i", new_lens, n), n, workspace, _nbytes(workspace), _on(stream))
+
+
+def mc_latent_append_decode(params: McLatentParams, rope: McRopeParams, q, kv, norm, q_out, pool, block_tables, seq_lens, tokens: int = 1,
+                            stream=None) -> None:
+    """The same for ``tokens`` new tokens a row, the last at position ``seq_lens[r] - 1``; ``seq_lens``: int32 device tensor."""
+    n = seq_lens.numel()
+    device, dtype, strides = _latent_new(params, q, kv, norm, q_out, n * tokens)
+    wide = _latent_pool(params, device, dtype, pool, block_tables, n, None)
+    _dense("seq_lens", device, _torch.int32, seq_lens, n)
+    _enqueue("mc_latent_append_decode", params, _rope(rope), q, kv, strides, norm, q_out, pool, block_tables, wide, seq_lens, n, tokens,
+             _on(stream))
+
+
+def mc_latent_decode_attn_workspace_bytes(params: McLatentParams, batch: int, tokens: int = 1) -> int:
+    return int(lib().mc_latent_decode_attn_workspace_bytes(ctypes.byref(params), batch, tokens))
+
+
+def mc_latent_decode_attn_paged(params: McLatentParams, q, pool, block_tables, seq_lens, tokens: int, out, lse, workspace, stream=None) -> None:
+    """Enqueue absorbed attention of ``tokens`` new tokens a row: q [rows * tokens, heads, latent_dim + rope_dim], out [..., latent_dim]."""
+    dtype = _latent(params)
+    n, device = seq_lens.numel(), q.get_device()
+    rows = n * tokens * params.num_heads
+    _dense("q out", device, dtype, q, rows * (params.latent_dim + params.rope_dim), out, rows * params.latent_dim)
+    wide = _latent_pool(params, device, dtype, pool, block_tables, n, workspace)
+    _dense("seq_lens", device, _torch.int32, seq_lens, n)
+    if lse is not None:
+        _dense("lse", device, _torch.float32, lse, rows)
+    _enqueue("mc_latent_decode_attn_paged", params, q, pool, block_tables, wide, seq_lens, n, tokens, out, lse, workspace, _nbytes(workspace),
+             _on(stream))
+
+
+def mc_latent_expand_paged(params: McLatentParams, weight, pool, block_tables, lens, kv, workspace, stream=None) -> None:
+    """Enqueue the keys and values of whole requests: weight [heads * 2 * head_dim, latent_dim], kv [sum of lens, heads, 2 * head_dim]."""
+    dtype = _latent(params)
+    n, device, outs = len(lens), pool.get_device(), params.num_heads * 2 * params.head_dim
+    _dense("weight kv", device, dtype, weight, outs * params.latent_dim, kv, sum(lens) * outs)
+    wide = _latent_pool(params, device, dtype, pool, block_tables, n, workspace)
+    _enqueue("mc_latent_expand_paged", params, weight, pool, block_tables, wide, _ints("i", lens, n), n, kv, workspace, _nbytes(workspace), _on(stream))
+
+
+def mc_latent_prefill_attn_workspace_bytes(params: McLatentParams, prefix_lens, new_lens) -> int:
+    n, a, b = _lens(prefix_lens, new_lens)
+    return int(lib().mc_latent_prefill_attn_workspace_bytes(ctypes.byref(params), a.at, b.at, n))
+
+
+def mc_latent_prefill_attn_paged(params: McLatentParams, q, k, v, pool, block_tables, prefix_lens, new_lens, out, lse, workspace,
+                                 stream=None) -> None:
+    """Enqueue chunked-prefill attention to expanded keys and values.
+
+    q: [new tokens, heads, head_dim + rope_dim], out: [new tokens, heads, head_dim], dense; k, v: [all tokens, heads, head_dim] with dense rows
+    (such as the two halves of what mc_latent_expand_paged makes)."""
+    dtype = _latent(params)
+    n = len(prefix_lens)
+    if len(new_lens) != n:
+        raise ValueError(f"{n} prefix lengths and {len(new_lens)} new lengths")
+    device, H, D, T = q.get_device(), params.num_heads, params.head_dim, sum(new_lens)
+    N = T + sum(prefix_lens)
+    _dense("q out", device, dtype, q, T * H * (D + params.rope_dim), out, T * H * D)
+    strides = (ctypes.c_int64 * 4)(*_rows_of_heads("k", device, dtype, k, N, H, D), *_rows_of_heads("v", device, dtype, v, N, H, D))
+    if lse is not None:
+        _dense("lse", device, _torch.float32, lse, T * H)
+    wide = _latent_pool(params, device, dtype, pool, block_tables, n, workspace)
+    _enqueue("mc_latent_prefill_attn_paged", params, q, k, v, strides, pool, block_tables, wide, _ints("i", prefix_lens, n), _ints("i", new_lens, n), n,
+             out, lse, workspace, _nbytes(workspace), _on(stream))

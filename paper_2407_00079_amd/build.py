@@ -17,9 +17,10 @@ OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmooncake_hip.so")
 # the name says which interpreter it is for: others do not load it
 CALLER = os.path.join(PKG, "_mccall" + sysconfig.get_config_var("EXT_SUFFIX"))
-# host_plan.cpp holds no device code: hipcc compiles it as plain C++
+# host_plan.cpp and latent_plan.cpp hold no device code: hipcc compiles them as plain C++
 SOURCES = ["mc_api.hip", "host_plan.cpp", "attn_prefill.hip", "attn_prefill_bf16.hip", "attn_narrow.hip", "attn_decode.hip", "attn_noalloc.hip", "kv_copy.hip",
-           "prefix_hash.hip", "rope_append.hip", "kv_pages.hip"]
+           "prefix_hash.hip", "rope_append.hip", "kv_pages.hip", "latent_api.hip", "latent_plan.cpp", "latent_append.hip", "latent_decode.hip",
+           "latent_expand.hip", "latent_prefill.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed-fp32 VALU forms are switched off on purpose (device code only)

@@ -31,25 +31,6 @@ constexpr int kRows = kDecodeRows, kBlockKeys = kDecodeBlockKeys, kBlockPages = 
 static_assert(kRows == 16 && kBlockKeys == 32, "a tile is a matrix instruction's 16 query heads, a block its 32 keys of P V");
 static_assert(kWaves == kDecodeWaves, "the host bounds the line by the waves of a launch");
 
-template <int N>
-struct Int {
-  static constexpr int value = N;
-};
-
-// inclusive prefix sum over a wave: within rows of 16 lanes, then what lies in the rows before
-__device__ __forceinline__ int scan(int x) {
-  auto shifted = [](int v, auto ctrl, auto rows) __attribute__((always_inline)) {
-    return __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
-  };
-  x += shifted(x, Int<0x111>{}, Int<0xf>{});                 // row_shr 1, 2, 4, 8
-  x += shifted(x, Int<0x112>{}, Int<0xf>{});
-  x += shifted(x, Int<0x114>{}, Int<0xf>{});
-  x += shifted(x, Int<0x118>{}, Int<0xf>{});
-  x += shifted(x, Int<0x142>{}, Int<0xa>{});                 // row_bcast 15: into rows 1 and 3
-  x += shifted(x, Int<0x143>{}, Int<0xc>{});                 // row_bcast 31: into rows 2 and 3
-  return x;
-}
-
 // What stands at one place of the line.
 struct At {
   int row, head, tile;

@@ -28,6 +28,25 @@ __device__ __forceinline__ float max8(f32x4 a, f32x4 b) {
   return m;
 }
 
+template <int N>
+struct Int {
+  static constexpr int value = N;
+};
+
+// inclusive prefix sum over a wave: within rows of 16 lanes, then what lies in the rows before
+__device__ __forceinline__ int scan(int x) {
+  auto shifted = [](int v, auto ctrl, auto rows) __attribute__((always_inline)) {
+    return __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+  };
+  x += shifted(x, Int<0x111>{}, Int<0xf>{});                 // row_shr 1, 2, 4, 8
+  x += shifted(x, Int<0x112>{}, Int<0xf>{});
+  x += shifted(x, Int<0x114>{}, Int<0xf>{});
+  x += shifted(x, Int<0x118>{}, Int<0xf>{});
+  x += shifted(x, Int<0x142>{}, Int<0xa>{});                 // row_bcast 15: into rows 1 and 3
+  x += shifted(x, Int<0x143>{}, Int<0xc>{});                 // row_bcast 31: into rows 2 and 3
+  return x;
+}
+
 // Between one lane's write of LDS and another lane's read of it, and between that read and the next write of the place: a wave's
 // LDS accesses are carried out in the order they are issued, so nothing has to be waited for, but the compiler, which sees one
 // lane, may not move them past each other.

@@ -1,0 +1,467 @@
+// Absorbed attention over a cache of latent vectors, lengths in device memory:
+//
+//   x(j) = scale q . [c(j), r(j)],      out = sum_j softmax_j(x) c(j),      lse = log sum_j exp(x(j))
+//
+// One cache row serves all heads, as key and as value.  A workgroup has 16, 32 or 64 stacked query rows (row = token * H + head) and walks
+// tiles of 64 keys through LDS, read from memory once a workgroup and from LDS once as keys and once as values by each 16 or 32 rows:
+//
+//   * Four waves a group of rows.  Wave w makes the scores S^T = K Q^T of keys 16 w .. 16 w + 15 of the tile for all rows of its group
+//     (queries stay in registers), the probabilities meet in LDS, and it then adds the tile's share of columns R/4 w .. of the output,
+//     O^T += C^T P^T: every element of the tile is read once for each product, whatever the number of waves.
+//   * A softmax runs in one pass in fp32.  Its reference is one for all four waves and lags behind the largest score by at most 2^8: probabilities
+//     are formed against it before the waves have met, and only where a score outgrew it the waves exchange maxima, scale what they
+//     have and form the tile's probabilities again (flags that all waves of the workgroup read behind the same barrier).
+//   * Keys behind what a row sees get probability 0, and in a row's last tiles elements that are not finite are cleared as they come out of LDS
+//     as values: 0 times whatever an unwritten slot holds stays 0.  (A key that counts and is not finite has made its score so.)
+//   * The tiles of all rows stand in one line, of which each workgroup takes an equal stretch; it finds its place from the lengths.  Rows that a stretch's
+//     end cuts leave partial results in the workspace, and a second kernel joins them in the order of the line.
+#include "attn_narrow_device.h"
+#include "latent_device.h"
+
+namespace mc {
+namespace {
+
+constexpr int kTile = kLatentTileKeys, kTilePages = kTile / kPageTokens;
+static_assert(kTilePages == 4, "a page for each wave of a group");
+
+struct At {
+  int row, block, blocks, len;               // tile `block` of the row's `blocks`
+};
+
+struct Line {
+  const_i32_ptr lens, tables;
+  int batch, max_pages;
+  __device__ __forceinline__ explicit Line(const LatentDecodeArgs& a)
+      : lens((const_i32_ptr)a.seq_lens), tables((const_i32_ptr)a.block_tables), batch(a.batch), max_pages(a.max_pages) {}
+  // a length the table has no room for is a padding row's
+  __device__ __forceinline__ int valid(int len) const { return len > 0 && (len - 1) / kPageTokens < max_pages ? len : 0; }
+  static __device__ __forceinline__ int tiles(int len) { return (int)(((uint32_t)len + kTile - 1) / kTile); }
+  __device__ __forceinline__ void next(At& at) const {
+    if (++at.block < at.blocks) return;
+    at.block = 0;
+    do {
+      ++at.row;
+      at.len = at.row < batch ? valid(lens[at.row]) : 1;
+    } while (at.len == 0);
+    at.blocks = tiles(at.len);
+  }
+  struct Sums {
+    int per, upto, mine, all;                // rows a lane looks over; their tiles, running and its own
+  };
+  __device__ __forceinline__ Sums sums() const {
+    const int lane = threadIdx.x & 63;
+    Sums s = {(batch + 63) / 64, 0, 0, 0};
+    for (int i = 0; i < s.per; ++i) {
+      const int r = lane * s.per + i;
+      s.mine += r < batch ? tiles(valid(lens[r])) : 0;
+    }
+    s.upto = scan(s.mine);
+    s.all = __builtin_amdgcn_readlane(s.upto, 63);
+    return s;
+  }
+  // place x < s.all of the line
+  __device__ __forceinline__ At place(const Sums& s, int x) const {
+    const int lane = threadIdx.x & 63;
+    int k = __popcll(__builtin_amdgcn_ballot_w64(s.upto <= x));
+    At at;
+    at.row = k * s.per;
+    int before = __builtin_amdgcn_readlane(s.upto - s.mine, k);
+    for (;;) {                               // (x lies in one of the lane's rows)
+      const int r = at.row + lane, mine = r < batch ? tiles(valid(lens[r])) : 0, upto = before + scan(mine);
+      k = __popcll(__builtin_amdgcn_ballot_w64(upto <= x));
+      if (k < 64) {
+        at.row += k;
+        before = __builtin_amdgcn_readlane(upto - mine, k);
+        break;
+      }
+      at.row += 64;
+      before = __builtin_amdgcn_readlane(upto, 63);
+    }
+    at.len = valid(lens[at.row]);
+    at.blocks = tiles(at.len);
+    at.block = x - before;
+    return at;
+  }
+  // page `i` of a tile; the table is never read past the row's pages
+  __device__ __forceinline__ int page(const At& at, int i) const {
+    const int lp = at.block * kTilePages + i, last = (at.len - 1) / kPageTokens;
+    return tables[(int64_t)at.row * max_pages + (lp < last ? lp : last)];
+  }
+};
+
+// R: numbers of a latent vector; MT: 16-row tiles of a group of four waves; GROUPS of them
+template <int R, int MT, int GROUPS>
+struct Shape {
+  static constexpr int kCols = R + kLatentRope, kBlocks = kCols / 64, kSteps = kCols / 32;      // blocks of 64 columns, steps of 32
+  static constexpr int kRowB = kCols * 2, kTileB = kTile * kRowB, kBlockB = kTile * 128;
+  static constexpr int kRows = 16 * MT * GROUPS, kAllWaves = 4 * GROUPS;
+  static constexpr int kColTiles = R / 64;                   // 16-column tiles of the output a wave has
+  static constexpr int kPRowB = kTile * 2 + 16;              // 16 rows of a column spread over the banks
+  // A tile in LDS: block by block of 64 columns, in each 64 rows of 128 bytes, the 16-byte granules of row r at their place ^ swizzle(r).  The
+  // 256 bytes of all banks are two rows: reads of one granule of 16 rows, and transposing reads of 32 bytes of rows 0-3 and 8-11
+  // (4-7 and 12-15), meet every bank once.
+  static __device__ __forceinline__ int swizzle(int r) { return (r & 2) | ((r >> 1) & 4) | ((r >> 2) & 1); }
+  struct Shared {
+    char tile[2][kTileB];
+    char p[GROUPS][16 * MT][kPRowB];
+    float most[kAllWaves][MT][16], sum[kAllWaves][MT][16];
+    int outgrown[8];
+  };
+};
+
+template <int R, int MT, int GROUPS>
+__global__ __launch_bounds__(GROUPS * 256) void latent_decode_kernel(const LatentDecodeArgs a) {
+  typedef Shape<R, MT, GROUPS> S;
+  __shared__ __attribute__((aligned(256))) typename S::Shared sh;
+  const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave >> 2, w = wave & 3;
+  const int tile = (int)(blockIdx.x / (uint32_t)a.stretches), stretch = (int)blockIdx.x - tile * a.stretches;
+  const Line line(a);
+  const typename Line::Sums sums = line.sums();
+  const int used = latent_used(sums.all, a.stretches);
+  const int begin = stretch < used ? (int)decode_begin(sums.all, stretch, used) : 0;
+  const int end = stretch < used ? (int)decode_begin(sums.all, stretch + 1, used) : 0;
+  const bool notes = tile == 0 && threadIdx.x == 0, by_row = a.batch <= a.stretches;
+  LatentChain open = {0, 0, 0, 0};
+
+  if (begin < end) {
+    // this lane's query rows
+    int row[MT], back[MT];                                   // stacked row; keys before the row's length that it does not see
+    bool live[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const int r = tile * S::kRows + (group * MT + m) * 16 + j;
+      live[m] = r < a.stacked;
+      row[m] = live[m] ? r : a.stacked - 1;                  // (rows past the last compute it again)
+      back[m] = a.tokens - 1 - row[m] / a.heads;
+    }
+    const uint32_t base = (uint32_t)(uintptr_t)(MC_LDS char*)&sh;
+    uint32_t source[2];                                      // of a lane's 16 bytes of 8 rows by 128 bytes: rows 0-7 and 8-15 of a page
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      source[h] = (uint32_t)((8 * h + lane / 8) * S::kRowB + ((lane % 8) ^ S::swizzle(8 * h + lane / 8)) * 16);
+    auto fetch = [&](int page, int buf) __attribute__((always_inline)) {
+      const char* const from = reinterpret_cast<const char*>(a.pool) + (int64_t)page * (kPageTokens * S::kRowB);
+      const uint32_t to = base + buf * S::kTileB + w * (kPageTokens * 128);
+#pragma unroll
+      for (int b = 0; b < S::kBlocks; ++b) {
+        if constexpr (GROUPS == 1) {
+          dma16(from + b * 128, source[0], to + b * S::kBlockB);
+          dma16(from + b * 128, source[1], to + b * S::kBlockB + 1024);
+        } else {
+          dma16(from + b * 128, group == 0 ? source[0] : source[1], to + b * S::kBlockB + group * 1024);
+        }
+      }
+    };
+    // fragment addresses: as keys (rows 16 w + j), as values (columns R/4 w + 16 t, keys 8 g .. of a half of the tile)
+    const uint32_t k_lane = base + (16 * w + j) * 128 + ((g ^ S::swizzle(j)) << 4);
+    const int r0 = 8 * g + (j >> 2);
+    const uint32_t v_lane = base + (R / 256) * w * S::kBlockB + r0 * 128 + ((((j & 3) >> 1) ^ S::swizzle(r0)) << 4) + ((j & 1) << 3);
+    const uint32_t p_base = base + (uint32_t)__builtin_offsetof(typename S::Shared, p) + group * (16 * MT * S::kPRowB);
+
+    bf16x8 qf[S::kSteps][MT];
+    f32x4 o[S::kColTiles][MT];
+    float ref[MT], l[MT];
+    auto start = [&](const At& at) __attribute__((always_inline)) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const char* const q = reinterpret_cast<const char*>(a.q) + ((int64_t)at.row * a.stacked + row[m]) * S::kRowB;
+#pragma unroll
+        for (int st = 0; st < S::kSteps; ++st) qf[st][m] = *reinterpret_cast<const bf16x8*>(q + st * 64 + g * 16);
+        ref[m] = -INFINITY;
+        l[m] = 0.f;
+#pragma unroll
+        for (int t = 0; t < S::kColTiles; ++t) o[t][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+    };
+    const float c = a.scale_log2e;
+
+    // the tile whose copy is next, and the page of it that this wave copies
+    At nx = line.place(sums, begin);
+    int page = line.page(nx, w), fetched = 0, left = end - begin;
+    auto fetch_next = [&]() __attribute__((always_inline)) {
+      if (fetched == end - begin) return;
+      fetch(page, fetched & 1);
+      if (++fetched == end - begin) return;
+      line.next(nx);
+      page = line.page(nx, w);
+    };
+    int buf = 1;
+    auto one_tile = [&](const At& at, int block, auto tail_tag) __attribute__((always_inline)) {
+      constexpr bool tail = decltype(tail_tag)::value != 0;
+      buf ^= 1;
+      __builtin_amdgcn_s_waitcnt(0x0F70);                    // (vmcnt(0): this wave's share of the tile)
+      __syncthreads();
+      fetch_next();
+
+      // scores of keys 16 w + 4 g + i for row j of each tile of rows
+      f32x4 s[MT];
+#pragma unroll
+      for (int m = 0; m < MT; ++m) s[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+      // (fragments are asked for kAhead steps before they are used, and no earlier: with 64 rows there are no registers for more)
+      constexpr int kAhead = 3;
+      bf16x8 ring[kAhead];
+      auto key = [&](int st) __attribute__((always_inline)) {
+        return *reinterpret_cast<MC_LDS const bf16x8*>((k_lane ^ ((st & 1) << 6)) + buf * S::kTileB + (st >> 1) * S::kBlockB);
+      };
+#pragma unroll
+      for (int st = 0; st < kAhead; ++st) ring[st] = key(st);
+#pragma unroll
+      for (int st = 0; st < S::kSteps; ++st) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) s[m] = mma(ring[st % kAhead], qf[st][m], s[m]);
+        if (st + kAhead < S::kSteps) ring[st % kAhead] = key(st + kAhead);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (tail) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          const int seen = at.len - back[m] - block * kTile - 16 * w - 4 * g;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (i >= seen) s[m][i] = -INFINITY;
+        }
+      }
+      float most[MT];
+      bool over = false;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        most[m] = max_over_groups(larger(larger(s[m][0], s[m][1]), larger(s[m][2], s[m][3]))) * c;
+        over |= most[m] > ref[m] + kRescaleSlack;
+      }
+      const bool outgrown = __builtin_amdgcn_ballot_w64(over) != 0;
+      if (lane == 0) sh.outgrown[wave] = outgrown;
+      float p[MT][4];
+      auto probabilities = [&]() __attribute__((always_inline)) {
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        typedef __attribute__((__vector_size__(4))) __bf16 bf16x2;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          const float from = fmaxf(ref[m], kNoKeyYet);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[m][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][i], c, -from));
+          const uint32_t low = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[m][0], p[m][1]}, bf16x2));
+          const uint32_t high = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[m][2], p[m][3]}, bf16x2));
+          *reinterpret_cast<MC_LDS u32x2*>(p_base + (16 * m + j) * S::kPRowB + (16 * w + 4 * g) * 2) = u32x2{low, high};
+        }
+      };
+      probabilities();
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+        if (g == 0) sh.most[wave][m][j] = most[m];
+      __syncthreads();
+      int any = 0;
+#pragma unroll
+      for (int i = 0; i < S::kAllWaves; ++i) any |= sh.outgrown[i];
+      if (__builtin_amdgcn_readfirstlane(any) != 0) {        // (the same for all waves of the workgroup)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          float top = sh.most[4 * group][m][j];
+#pragma unroll
+          for (int i = 1; i < 4; ++i) top = fmaxf(top, sh.most[4 * group + i][m][j]);
+          const float next = fmaxf(ref[m], top), alpha = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[m] - next);
+          ref[m] = next;
+          l[m] *= alpha;
+#pragma unroll
+          for (int t = 0; t < S::kColTiles; ++t) o[t][m] *= alpha;
+        }
+        probabilities();
+        __syncthreads();
+      }
+#pragma unroll
+      for (int m = 0; m < MT; ++m) l[m] += (p[m][0] + p[m][1]) + (p[m][2] + p[m][3]);      // (before their rounding: lse keeps 32 bits)
+      // output += values of this wave's columns
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        bf16x8 pf[MT];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+          pf[m] = *reinterpret_cast<MC_LDS const bf16x8*>(p_base + (16 * m + j) * S::kPRowB + half * 64 + g * 16);
+        constexpr int kAhead = 2;
+        bf16x8 ring[kAhead];
+        auto value = [&](int t) __attribute__((always_inline)) {
+          const uint32_t at0 = (v_lane ^ ((t & 3) << 5)) + buf * S::kTileB + (t >> 2) * S::kBlockB + half * (32 * 128);
+          const uint32_t at1 = (v_lane ^ ((t & 3) << 5) ^ 16) + buf * S::kTileB + (t >> 2) * S::kBlockB + half * (32 * 128) + 4 * 128;
+          const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((MC_LDS bf16x4*)(uintptr_t)at0);
+          const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((MC_LDS bf16x4*)(uintptr_t)at1);
+          return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+#pragma unroll
+        for (int t = 0; t < kAhead; ++t) ring[t] = value(t);
+#pragma unroll
+        for (int t = 0; t < S::kColTiles; ++t) {
+          bf16x8 vf = ring[t % kAhead];
+          if constexpr (tail) {
+            u32x4 bits = __builtin_bit_cast(u32x4, vf);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) bits[i] = finite_pair(bits[i]);
+            vf = __builtin_bit_cast(bf16x8, bits);
+          }
+#pragma unroll
+          for (int m = 0; m < MT; ++m) o[t][m] = mma(vf, pf[m], o[t][m]);
+          if (t + kAhead < S::kColTiles) ring[t % kAhead] = value(t + kAhead);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    };
+    At at = nx;
+    fetch_next();
+    for (;;) {
+      // the tiles of one row that lie in the stretch: those whose keys all its rows see, then the others
+      start(at);
+      const bool whole = at.block == 0;                      // the row began in this stretch
+      const int stop = at.blocks - at.block <= left ? at.blocks : at.block + left;
+      const int clear = (at.len - (a.tokens - 1)) / kTile;
+      left -= stop - at.block;
+      int block = at.block;
+      for (; block < stop && block < clear; ++block) one_tile(at, block, Int<0>{});
+      for (; block < stop; ++block) one_tile(at, block, Int<1>{});
+
+      // the row's sums over the waves' keys, then its result or its part of one
+      const bool done = stop == at.blocks;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        float all = l[m] + __shfl_xor(l[m], 16, 64);
+        all = sum_with_other_half(all);
+        if (g == 0) sh.sum[wave][m][j] = all;
+      }
+      __syncthreads();
+      const int64_t part0 = (((int64_t)tile * a.stretches + stretch) * 2 + (whole ? 1 : 0)) * S::kRows;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        float all = sh.sum[4 * group][m][j];
+#pragma unroll
+        for (int i = 1; i < 4; ++i) all += sh.sum[4 * group + i][m][j];
+        if (!live[m]) continue;
+        const int col = (R / 4) * w + 4 * g;
+        if (whole && done) {
+          const float inv = all == 0.f ? 0.f : 1.0f / all;             // (a row that sees no key: 0)
+          const int64_t to = (int64_t)at.row * a.stacked + row[m];
+#pragma unroll
+          for (int t = 0; t < S::kColTiles; ++t) {
+            bf16x4 v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = (__bf16)(o[t][m][i] * inv);
+            *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(a.out) + to * R + col + 16 * t) = v;
+          }
+          if (a.lse != nullptr && w == 0 && g == 0) a.lse[to] = (ref[m] + __builtin_amdgcn_logf(all)) * 0.6931471805599453f;
+        } else {
+          const int64_t to = part0 + (group * MT + m) * 16 + j;
+#pragma unroll
+          for (int t = 0; t < S::kColTiles; ++t) *reinterpret_cast<f32x4*>(a.o_parts + to * R + col + 16 * t) = o[t][m];
+          if (w == 0 && g == 0) a.ml_parts[to] = float2{ref[m], all};
+        }
+      }
+      if (whole) {
+        // (the row's last tile stands at.blocks - stop places behind the stretch's last one)
+        const int more = done ? 0 : decode_wave_of(sums.all, (int64_t)end - 1 + (at.blocks - stop), used) - stretch;
+        if (notes && by_row) a.chains[at.row] = LatentChain{at.row, stretch, more, 0};
+        if (more != 0) open = LatentChain{at.row, stretch, more, 0};
+      }
+      if (left == 0) break;
+      at.block = at.blocks - 1;
+      line.next(at);
+    }
+  }
+  if (notes && !by_row) a.chains[stretch] = open;
+
+  // padding rows, shared out over the stretches
+  for (int64_t first = stretch; first < a.batch; first += (int64_t)a.stretches * (GROUPS * 256)) {
+    const int64_t r = first + (int64_t)threadIdx.x * a.stretches;
+    const bool empty = r < a.batch && line.valid(a.seq_lens[r]) == 0;
+    if (empty && tile == 0 && by_row) a.chains[r].more = 0;
+    for (uint64_t some = __builtin_amdgcn_ballot_w64(empty); some != 0; some &= some - 1) {
+      const int64_t out_row = (first + (int64_t)(wave * 64 + __builtin_ctzll(some)) * a.stretches) * a.stacked + tile * S::kRows;
+      const int rows = a.stacked - tile * S::kRows < S::kRows ? a.stacked - tile * S::kRows : S::kRows;
+      u32x4* const to = reinterpret_cast<u32x4*>(reinterpret_cast<__bf16*>(a.out) + out_row * R);
+      for (int i = lane; i < rows * (R / 8); i += 64) to[i] = u32x4{};
+      if (a.lse != nullptr && lane < rows) a.lse[out_row + lane] = -INFINITY;
+    }
+  }
+}
+
+// Rows that several stretches have parts of: a workgroup has 128 columns of one stacked row, whose parts its half waves share out.
+constexpr int kJoinCols = 128, kJoinThreads = 512;
+template <int R>
+__global__ __launch_bounds__(kJoinThreads) void latent_join_kernel(const LatentDecodeArgs a, int tile_rows) {
+  __shared__ float weight[kLatentWgs], tops[kJoinThreads / 64], sums[kJoinThreads / 64];
+  __shared__ __attribute__((aligned(16))) float outs[kJoinThreads / 32][kJoinCols];
+  const LatentChain chain = a.chains[blockIdx.x];
+  if (chain.more == 0) return;
+  const int stacked = blockIdx.y, tile = stacked / tile_rows, in_tile = stacked - tile * tile_rows;
+  auto part = [&](int i) __attribute__((always_inline)) {
+    return (((int64_t)tile * a.stretches + chain.first + i) * 2 + (i == 0 ? 1 : 0)) * tile_rows + in_tile;
+  };
+  const int n = chain.more + 1, t = threadIdx.x, wave = t / 64;
+  const float2 ml = t < n ? a.ml_parts[part(t)] : float2{-INFINITY, 0.f};      // (at most kLatentWgs parts)
+  auto over_wave = [](float x, auto&& join) __attribute__((always_inline)) {
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2) x = join(x, __shfl_xor(x, step, 64));
+    return x;
+  };
+  float top = over_wave(ml.x, [](float x, float y) { return fmaxf(x, y); });
+  if (t % 64 == 0) tops[wave] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kJoinThreads / 64; ++i) top = fmaxf(top, tops[i]);
+  const float from = top == -INFINITY ? 0.f : top;           // (every score is -inf or NaN)
+  const float mine = __builtin_amdgcn_exp2f(ml.x - from);
+  if (t < kLatentWgs) weight[t] = mine;
+  const float share = over_wave(mine * ml.y, [](float x, float y) { return x + y; });
+  if (t % 64 == 0) sums[wave] = share;
+  __syncthreads();
+  float l = 0.f;
+#pragma unroll
+  for (int i = 0; i < kJoinThreads / 64; ++i) l += sums[i];
+  const int slot = t / 32, col = t % 32 * 4;
+  const float* const o = a.o_parts + blockIdx.z * kJoinCols + col;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  constexpr int kAtOnce = 8;
+  for (int i0 = slot; i0 < n; i0 += kAtOnce * (kJoinThreads / 32)) {
+    f32x4 v[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int i = i0 + k * (kJoinThreads / 32);
+      v[k] = *reinterpret_cast<const f32x4*>(o + part(i < n ? i : i0) * R);
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int i = i0 + k * (kJoinThreads / 32);
+      if (i < n) x += weight[i] * v[k];
+    }
+  }
+  *reinterpret_cast<f32x4*>(&outs[slot][col]) = x;
+  __syncthreads();
+  if (t >= kJoinCols / 4) return;
+#pragma unroll
+  for (int i = 1; i < kJoinThreads / 32; ++i) x += *reinterpret_cast<const f32x4*>(&outs[i][col]);
+  const int64_t to = (int64_t)chain.row * a.stacked + stacked;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  bf16x4 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = (__bf16)(x[i] * inv);
+  *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(a.out) + to * R + blockIdx.z * kJoinCols + col) = y;
+  if (a.lse != nullptr && blockIdx.z == 0 && t == 0) a.lse[to] = (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+template <int R>
+hipError_t enqueue(int rows, const LatentDecodeArgs& args, hipStream_t stream) {
+  const int wgs = args.tiles * args.stretches;
+  if (rows == 16) latent_decode_kernel<R, 1, 1><<<wgs, 256, 0, stream>>>(args);
+  else if (rows == 32) latent_decode_kernel<R, 2, 1><<<wgs, 256, 0, stream>>>(args);
+  else if (rows == 64) latent_decode_kernel<R, 2, 2><<<wgs, 512, 0, stream>>>(args);
+  else return hipErrorInvalidValue;
+  latent_join_kernel<R><<<dim3(args.n_chains, args.stacked, R / kJoinCols), kJoinThreads, 0, stream>>>(args, rows);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_latent_decode(int latent_dim, int rows, const LatentDecodeArgs& args, hipStream_t stream) {
+  (void)hipGetLastError();
+  if (latent_dim == 512) return enqueue<512>(rows, args, stream);
+  if (latent_dim == 256) return enqueue<256>(rows, args, stream);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace mc

@@ -1,0 +1,58 @@
+// Host-side half of the calls on a cache of latent vectors: argument validation, request tables and workspace layouts.  Nothing here calls
+// HIP (see host_plan.h).
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+#include "latent_types.h"
+#include "mc.h"
+
+namespace mc {
+namespace host {
+
+mc_status check_latent(const mc_latent_params* p);
+// softmax scale times log2(e)
+float latent_scale_log2e(const mc_latent_params* p);
+
+// Strides of an append (elements; null: dense) in the order of the call.
+struct AppendStrides {
+  int64_t q_token, q_head, kv_token, out_token, out_head;
+};
+mc_status check_latent_rope(const mc_latent_params* p, const mc_rope_params* rope);
+mc_status latent_append_strides(const mc_latent_params* p, const int64_t* strides, int64_t tokens, AppendStrides* out);
+mc_status check_latent_append(const mc_latent_params* p, const void* q, const void* kv, const AppendStrides& s, const void* norm,
+                              const void* q_out, const void* pool, const int32_t* block_tables, int64_t tokens);
+
+// Lengths of a batch with `prefix_lens` null for none before: sign and range checks, sums, most pages of a request that has any new tokens.
+struct LatentLens {
+  int64_t total_new, total_keys;
+  int32_t need_pages, most_keys;             // most_keys: of a request with new tokens
+};
+mc_status check_latent_lens(const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, LatentLens* out);
+
+size_t latent_table_bytes(int32_t batch);
+// The request table; work items: `items_per(chunk)` of each request, one after another.  Returns their number.
+int64_t fill_latent_table(const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, int32_t rows_per_item, LatentReq* to);
+
+// Where the parts of an absorbed attention call lie in its workspace.
+struct LatentDecodeLayout {
+  int32_t rows, tiles, stretches, chains;    // stacked rows of a tile; entries of the list of rows to be joined
+  size_t ml_off, chain_off, total;
+};
+LatentDecodeLayout latent_decode_layout(const mc_latent_params* p, int32_t batch, int32_t tokens);
+
+// Expanded attention: key slices (1: whole rows) and where partial results lie.
+struct LatentPrefillLayout {
+  int32_t kv_splits;
+  int64_t items;                             // (request, tile of query rows)
+  size_t o_off, lse_off, total;
+};
+LatentPrefillLayout latent_prefill_layout(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch,
+                                          const LatentLens& lens);
+struct KeyStrides {
+  int64_t k_token, k_head, v_token, v_head;
+};
+mc_status latent_key_strides(const mc_latent_params* p, const int64_t* strides, KeyStrides* out);
+
+}  // namespace host
+}  // namespace mc

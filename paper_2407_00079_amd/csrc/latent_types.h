@@ -1,0 +1,51 @@
+// Plain data shared by the host code and the kernels of the cache of latent vectors; no HIP types here (see mc_types.h).
+#pragma once
+#include <stdint.h>
+
+#include "mc_types.h"
+
+namespace mc {
+
+constexpr int kLatentRope = 64;              // columns of the shared key part, P
+constexpr int kLatentMostHeads = 1024;
+constexpr int kLatentMostTokens = 16;
+
+// A request of a call with host lengths.
+struct LatentReq {
+  int32_t q_off;                             // its first new token in q and out
+  int32_t k_off;                             // its first token in the expanded keys and values
+  int32_t prefix, chunk;
+  int32_t item_off;                          // its first work item
+};
+// at most kMaxArgEntries requests travel with the launch, behind them entries that no search ends at
+struct LatentReqTable {
+  LatentReq r[kMaxArgEntries];
+};
+
+// Absorbed attention: the keys of all rows in tiles of 64 stand in one line, row by row; `stretches` workgroups for each tile of stacked
+// query rows (row = token * H + head) take equal stretches of it.
+constexpr int kLatentTileKeys = 64;
+constexpr int kLatentWgs = 256;              // one a compute unit
+// stacked query rows of a tile, by how many there are: 16, 32 or 64 (latent_decode.hip says what each measured)
+constexpr int latent_tile_rows(int64_t stacked) { return stacked <= 16 ? 16 : stacked <= 32 ? 32 : 64; }
+constexpr int latent_tiles(int64_t stacked) { return (int)((stacked + latent_tile_rows(stacked) - 1) / latent_tile_rows(stacked)); }
+// workgroups a tile has
+constexpr int latent_stretches(int tiles) { return tiles >= kLatentWgs ? 1 : kLatentWgs / tiles; }
+// tiles of keys a stretch has at least, so that partial results do not outweigh what they are of
+constexpr int kLatentLeastTiles = 2;
+// how many stretches have work (decode_begin says where each begins, decode_wave_of which has a place)
+constexpr int latent_used(int64_t total, int stretches) {
+  const int64_t most = (total + kLatentLeastTiles - 1) / kLatentLeastTiles;
+  return most < stretches ? (int)most : stretches;
+}
+// A row that several stretches have parts of: the first of them, and how many follow.  more == 0: nothing is to be joined.
+struct LatentChain {
+  int32_t row, first, more, pad;
+};
+
+// Expanded attention: query rows and keys of a tile
+constexpr int kLatentRows = 256;
+// Expansion: tokens and outputs of a workgroup's tile
+constexpr int kExpandTokens = 256, kExpandOuts = 256;
+
+}  // namespace mc

@@ -7,6 +7,7 @@
 #include <vector>
 
 #include "host_plan.h"
+#include "latent_internal.h"
 #include "mc_internal.h"
 
 namespace {
@@ -235,6 +236,10 @@ mc_status place_tables(const int64_t* a, size_t n_a, const int64_t* b, size_t n_
 }
 
 }  // namespace
+
+namespace mc {
+mc_status upload_table(void* dst, const void* src, size_t bytes, hipStream_t stream) { return upload(dst, src, bytes, stream); }
+}  // namespace mc
 
 extern "C" {
 

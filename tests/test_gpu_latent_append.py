@@ -1,0 +1,92 @@
+"""Norm, rotation and append to a cache of latent vectors against their definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from latent_util import BF16, DEV, P, PAGE, gen, lens_tensor, params, randn, tables, workspace
+from paper_2407_00079_amd import binding as B
+from rope_util import assert_rounded, turned
+
+pytestmark = pytest.mark.gpu
+
+
+def reference(rope, x, pos):
+    return turned(x, None, pos, list(rope.inv_freq), P, rope.layout == B.MC_ROPE_PAIRS, rope.gain)
+
+
+def check_results(rope, latent, q, kv, norm, q_out, pool, before, table, pos, row_of):
+    """pos < 0: the token is left out (q_out as it was: 7)."""
+    keep = pos >= 0
+    got = q_out.clone()
+    assert bool((got[torch.from_numpy(~keep).to(DEV)] == 7).all())
+    at = torch.from_numpy(keep).to(DEV)
+    want, size = reference(rope, q[at].double().cpu().numpy(), pos[keep])
+    assert_rounded(got[at], want, size, BF16, "q_out")
+    page = table.cpu().numpy()[row_of[keep], pos[keep] // PAGE]
+    slot = pos[keep] % PAGE
+    rows = pool.cpu()[page, slot]
+    x = kv[at].double().cpu().numpy()
+    c = x[:, :latent]
+    if norm is not None:
+        c = c / np.sqrt((c * c).mean(-1, keepdims=True) + rope.norm_eps) * norm.double().cpu().numpy()
+    # the mean of R squares in lanes of 8 and 6 exchanges, halved by the root; the root, its product and the weight's: under 16 units of 2^-24
+    assert_rounded(rows[:, :latent], c, np.abs(c), BF16, "latent part")
+    want, size = reference(rope, x[:, None, latent:], pos[keep])
+    assert_rounded(rows[:, None, latent:], want, size, BF16, "key part")
+    rest = torch.ones(pool.shape[:2], dtype=torch.bool)
+    rest[page, slot] = False
+    assert torch.equal(pool.cpu().view(torch.int16)[rest], before.cpu().view(torch.int16)[rest])
+
+
+def rope_of(layout, gain=1.0):
+    return B.rope_params(P, layout, base=10000.0, gain=gain)
+
+
+@pytest.mark.parametrize("layout", [B.MC_ROPE_HALF, B.MC_ROPE_PAIRS])
+@pytest.mark.parametrize("latent", [512, 256])
+@pytest.mark.parametrize("heads,prefix,new", [(1, [0], [1]), (16, [5, 100000, 17], [40, 3, 0]), (128, [31], [33]), (3, [7] * 80, [2, 0, 1, 5] * 20), (16, [100], [1500])])
+def test_prompts(layout, latent, heads, prefix, new):
+    g = gen(heads + len(prefix))
+    lens = [a + b for a, b in zip(prefix, new)]
+    table, pages = tables(g, lens)
+    T = sum(new)
+    q = randn(g, T, heads, 128 + P)[:, :, 128:]
+    kv, norm = randn(g, T, latent + P + 8)[:, : latent + P], randn(g, latent) if heads != 3 else None
+    q_out = torch.full((T, heads, latent + P), 7.0, dtype=BF16, device=DEV)
+    pool = randn(g, pages, PAGE, latent + P)
+    before, rope = pool.clone(), rope_of(layout, 1.25)
+    B.mc_latent_append_paged(params(heads, latent, 128, pages), rope, q, kv, norm, q_out[:, :, latent:], pool, table, prefix, new,
+                             workspace(B.mc_latent_workspace_bytes(len(lens))))
+    assert bool((q_out[:, :, :latent] == 7).all())
+    row_of = np.repeat(np.arange(len(new)), new)
+    pos = np.concatenate([p + np.arange(c) for p, c in zip(prefix, new)])
+    check_results(rope, latent, q, kv, norm, q_out[:, :, latent:], pool, before, table, pos, row_of)
+
+
+@pytest.mark.parametrize("tokens", [1, 3, 16])
+@pytest.mark.parametrize("latent", [512, 256])
+def test_tokens(tokens, latent):
+    g = gen(tokens)
+    lens = [1, 16, 17, 0, 300, 5, -3, 10 ** 6, 70000]
+    real = [n if 0 < n < 10 ** 6 else 0 for n in lens]
+    table, pages = tables(g, real)
+    heads, T = 10, len(lens) * tokens
+    q, kv, norm = randn(g, T, heads, P), randn(g, T, latent + P), randn(g, latent)
+    q_out = torch.full((T, heads, P), 7.0, dtype=BF16, device=DEV)
+    pool = randn(g, pages, PAGE, latent + P)
+    before, rope = pool.clone(), rope_of(B.MC_ROPE_PAIRS)
+    B.mc_latent_append_decode(params(heads, latent, 128, pages), rope, q, kv, norm, q_out, pool, table, lens_tensor(lens), tokens)
+    row_of = np.repeat(np.arange(len(lens)), tokens)
+    pos = np.concatenate([n - tokens + np.arange(tokens) if n > 0 else np.full(tokens, -1) for n in real])
+    check_results(rope, latent, q, kv, norm, q_out, pool, before, table, pos, row_of)
+
+
+def test_in_place_and_by_head():
+    g = gen(2)
+    table, pages = tables(g, [50])
+    p, rope = params(6, 512, 128, pages), rope_of(B.MC_ROPE_HALF)
+    q, kv, pool = randn(g, 50, 6, P), randn(g, 50, 512 + P), torch.zeros((pages, PAGE, 512 + P), dtype=BF16, device=DEV)
+    ws, out = workspace(B.mc_latent_workspace_bytes(1)), torch.empty((6, 50, P), dtype=BF16, device=DEV)
+    B.mc_latent_append_paged(p, rope, q.transpose(0, 1).contiguous().transpose(0, 1), kv, None, out.transpose(0, 1), pool, table, [0], [50], ws)
+    B.mc_latent_append_paged(p, rope, q, kv, None, q, pool, table, [0], [50], ws)
+    assert torch.equal(q, out.transpose(0, 1))
