@@ -19,6 +19,12 @@ namespace {
 
 constexpr int kTile = 64, kBufs = 3;
 
+// The reference of a row's probabilities stands kLift (log2 units) above the largest score it was last set from, so they are at most 2^-7 then and
+// stay below 2 while later scores outgrow that maximum by less than 8: "some probability reached 2" is bit 14 of a bf16 pattern (set in
+// infinities and NaN, too).  It is raised when a score comes within kRaiseAbove of that, before the test can fire again.
+constexpr float kLift = 7.0f, kRaiseAbove = 0.5f;
+constexpr uint32_t kGuardBits = 0x40004000u;
+
 // Rows of ROW_B bytes (256 or 128) in LDS, 16-byte granules swizzled: as keys for reads of one granule of 16 rows, as values for transposing reads
 // of 32 bytes of 8 rows.  The 256 bytes of all banks are one row or two.
 template <int ROW_B>
@@ -28,14 +34,31 @@ struct Banked {
   static __device__ __forceinline__ int value(int row) { return ((row >> kShift) & (kGran / 2 - 1)) << 1; }
 };
 
+// scores, then probabilities, of a block of 32 keys as a lane holds them: e = 4 kt + r is key 16 kt + 4 g + r, for row j of tile rt
+struct Scores {
+  f32x4 t[2][2];                             // [rt][kt]
+  __device__ __forceinline__ float get(int rt, int e) const { return t[rt][e >> 2][e & 3]; }
+  __device__ __forceinline__ void set(int rt, int e, float v) { t[rt][e >> 2][e & 3] = v; }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i >> 1][i & 1] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+};
+__device__ __forceinline__ uint32_t rounded_pair(float a, float b) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __attribute__((__vector_size__(4))) __bf16 bf16x2;
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+
 template <int D, bool SPLIT, typename Table>
 __global__ __launch_bounds__(512) void latent_prefill_kernel(const LatentPrefillArgs a, const Table table) {
   constexpr int kRowB = D * 2, kSteps = D / 32, kRopeSteps = kLatentRope / 32, kDTiles = D / 16, kQRowB = (D + kLatentRope) * 2;
-  constexpr int kRopeB = kTile * 128, kKeyB = kTile * kRowB, kBufB = 2 * kKeyB + kRopeB;             // keys, their shared part, values
+  constexpr int kKeyB = kTile * kRowB, kRopeB = kTile * 128;
+  constexpr int kRopeBase = kBufs * kKeyB, kValueBase = kRopeBase + kBufs * kRopeB;       // keys of all buffers, their shared parts, values
   typedef Banked<kRowB> Row;
   typedef Banked<128> Rope;
   constexpr int kCopies = kTile / Row::kInCopy / 8;          // of a wave, of keys and of values
-  __shared__ __attribute__((aligned(256))) char smem[kBufs * kBufB];
+  __shared__ __attribute__((aligned(256))) char smem[kBufs * (2 * kKeyB + kRopeB)];
   const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
@@ -66,6 +89,7 @@ __global__ __launch_bounds__(512) void latent_prefill_kernel(const LatentPrefill
     limit[rt] = P + row;
     out_row[rt] = (int64_t)(rq.q_off + row) * a.heads + head;
   }
+  const int wave_limit = P + row0 + wave * 32 + 31;          // no row of the wave sees more
   bf16x8 qf[kSteps + kRopeSteps][2];
 #pragma unroll
   for (int rt = 0; rt < 2; ++rt) {
@@ -82,155 +106,287 @@ __global__ __launch_bounds__(512) void latent_prefill_kernel(const LatentPrefill
   const int last_page = (L - 1) / kPageTokens;
   const uint32_t base = (uint32_t)(uintptr_t)(MC_LDS char*)smem;
   const uint32_t rope_at = (uint32_t)(((wave & 1) * 8 + lane / 8) * (int)rope_row + a.latent_dim * 2 + ((lane % 8 ^ Rope::key(wave * 8 + lane / 8)) << 4));
+  const int first_row = wave * kCopies * Row::kInCopy;       // of this wave in a tile
+  const char *k_src = kbase + ((int64_t)t_lo * kTile + first_row) * a.k_token, *v_src = vbase + ((int64_t)t_lo * kTile + first_row) * a.v_token;
+  uint32_t k_at[kCopies], v_at[kCopies];                     // of this lane's 16 bytes, from there
+#pragma unroll
+  for (int i = 0; i < kCopies; ++i) {
+    const int row = i * Row::kInCopy + lane / Row::kGran;
+    k_at[i] = (uint32_t)(row * (int)a.k_token + ((lane % Row::kGran ^ Row::key(first_row + row)) << 4));
+    v_at[i] = (uint32_t)(row * (int)a.v_token + ((lane % Row::kGran ^ Row::value(first_row + row)) << 4));
+  }
   auto page_of = [&](int tile) __attribute__((always_inline)) {
     const int lp = tile * (kTile / kPageTokens) + (wave >> 1);
     return ids[lp < last_page ? lp : last_page];
   };
   int page = page_of(t_lo);
+  const int64_t k_step = kTile * a.k_token, v_step = kTile * a.v_token;
+  const char* const rope_pool = reinterpret_cast<const char*>(a.pool);
+  const int rope_page = kPageTokens * (int)rope_row;
+  // tiles are fetched one after another
   auto fetch = [&](int tile, int buf) __attribute__((always_inline)) {
-    const uint32_t to = base + buf * kBufB;
+    const uint32_t to = base + buf * kKeyB + first_row * kRowB;
+    if ((tile + 1) * kTile <= L) {
 #pragma unroll
-    for (int i = 0; i < kCopies; ++i) {
-      const int first = (wave * kCopies + i) * Row::kInCopy, row = first + lane / Row::kGran;
-      int key = tile * kTile + row;
-      key = key < L ? key : L - 1;                           // (past the last key: it again, seen by no row)
-      dma16(kbase + key * a.k_token + ((lane % Row::kGran ^ Row::key(row)) << 4), to + first * kRowB);
-      dma16(vbase + key * a.v_token + ((lane % Row::kGran ^ Row::value(row)) << 4), to + kKeyB + kRopeB + first * kRowB);
+      for (int i = 0; i < kCopies; ++i) {
+        dma16(k_src, k_at[i], to + i * 1024);
+        dma16(v_src, v_at[i], to + kValueBase + i * 1024);
+      }
+    } else {                                                 // past the last key: it again, seen by no row
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i) {
+        int past = tile * kTile + first_row + i * Row::kInCopy + lane / Row::kGran - (L - 1);
+        past = past > 0 ? past : 0;
+        dma16(k_src + k_at[i] - past * a.k_token, to + i * 1024);
+        dma16(v_src + v_at[i] - past * a.v_token, to + kValueBase + i * 1024);
+      }
     }
-    dma16(reinterpret_cast<const char*>(a.pool) + page * (kPageTokens * rope_row), rope_at, to + kKeyB + wave * 1024);
+    dma16(rope_pool + (int64_t)page * rope_page, rope_at, base + kRopeBase + buf * kRopeB + wave * 1024);
+    k_src += k_step;
+    v_src += v_step;
     page = page_of(tile + 1);
   };
-  constexpr int kInFlight = 2 * kCopies + 1;
 
+  // ---- fragments.  K fragment u of a block: key tile u % 2, step u / 2; V fragment dt: columns 16 dt ..
+  constexpr int kK = 2 * (kSteps + kRopeSteps), kV = kDTiles, kUses = kK + kV;
   const uint32_t k_lane = base + j * kRowB + ((g ^ Row::key(j)) << 4);
-  const uint32_t r_lane = base + kKeyB + j * 128 + ((g ^ Rope::key(j)) << 4);
+  const uint32_t r_lane = base + kRopeBase + j * 128 + ((g ^ Rope::key(j)) << 4);
   const int v_row = 4 * g + (j >> 2);
-  const uint32_t v_lane = base + kKeyB + kRopeB + v_row * kRowB + (Row::value(v_row) << 4) + (((j & 3) >> 1) << 4) + ((j & 1) << 3);
+  const uint32_t v_lane = base + kValueBase + v_row * kRowB + (Row::value(v_row) << 4) + (((j & 3) >> 1) << 4) + ((j & 1) << 3);
+  uint32_t kx[kSteps], rx[kRopeSteps], vx[kDTiles];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) kx[i] = k_lane ^ (uint32_t)(i << 6);
+#pragma unroll
+  for (int i = 0; i < kRopeSteps; ++i) rx[i] = r_lane ^ (uint32_t)(i << 6);
+#pragma unroll
+  for (int i = 0; i < kDTiles; ++i) vx[i] = v_lane ^ (uint32_t)(i << 5);
+  auto load_k = [&](int buf, int kb, int u) __attribute__((always_inline)) {
+    const int st = u >> 1, row = kb * 32 + (u & 1) * 16;
+    const uint32_t at = st < kSteps ? kx[st < kSteps ? st : 0] + buf * kKeyB + row * kRowB : rx[st < kSteps ? 0 : st - kSteps] + buf * kRopeB + row * 128;
+    return *reinterpret_cast<MC_LDS const bf16x8*>(at);
+  };
+  auto load_v = [&](int buf, int kb, int dt) __attribute__((always_inline)) {
+    const uint32_t at = vx[dt] + buf * kKeyB + kb * 32 * kRowB;
+    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((MC_LDS bf16x4*)(uintptr_t)at);
+    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((MC_LDS bf16x4*)(uintptr_t)(at + 16 * kRowB));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
 
   f32x4 o[kDTiles][2];
-  float m_run[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  float m[2] = {-INFINITY, -INFINITY}, m_ref[2] = {kNoKeyYet, kNoKeyYet}, l[2] = {0.f, 0.f};         // references, the same but finite, sums
 #pragma unroll
   for (int dt = 0; dt < kDTiles; ++dt)
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt) o[dt][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
   const float c = a.scale_log2e;
 
-  auto block = [&](int tile, int buf, int kb, auto masked_tag) __attribute__((always_inline)) {
-    constexpr bool kMasked = decltype(masked_tag)::value != 0;
-    const int off = buf * kBufB;
-    f32x4 s[2][2];                                           // [row tile][key tile]
+  auto scores_of = [&](int buf, int kb, Scores& s) __attribute__((always_inline)) {
+    s.zero();
 #pragma unroll
-    for (int rt = 0; rt < 2; ++rt)
+    for (int u = 0; u < kK; ++u) {
+      const bf16x8 kf = load_k(buf, kb, u);
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt) s[rt][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int st = 0; st < kSteps + kRopeSteps; ++st)
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
-        const int row = kb * 32 + kt * 16;
-        const uint32_t at = st < kSteps ? (k_lane ^ (st << 6)) + off + row * kRowB : (r_lane ^ ((st - kSteps) << 6)) + off + row * 128;
-        const bf16x8 kf = *reinterpret_cast<MC_LDS const bf16x8*>(at);
-#pragma unroll
-        for (int rt = 0; rt < 2; ++rt) s[rt][kt] = mma(kf, qf[st][rt], s[rt][kt]);
-      }
+      for (int rt = 0; rt < 2; ++rt) s.t[rt][u & 1] = mma(kf, qf[u >> 1][rt], s.t[rt][u & 1]);
+      if (u % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // raise the references if some row outgrew its own
+  auto settle = [&](const Scores& s) __attribute__((always_inline)) {
     float mx[2];
 #pragma unroll
-    for (int rt = 0; rt < 2; ++rt) {
-      if constexpr (kMasked) {
-        const int seen = limit[rt] - tile * kTile - kb * 32 - 4 * g;
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (16 * kt + r > seen) s[rt][kt][r] = -INFINITY;
-      }
-      mx[rt] = max_over_groups(max8(s[rt][0], s[rt][1])) * c;
-    }
-    if (__builtin_amdgcn_ballot_w64(mx[0] > m_run[0] + kRescaleSlack || mx[1] > m_run[1] + kRescaleSlack) != 0) {
+    for (int rt = 0; rt < 2; ++rt) mx[rt] = max_over_groups(max8(s.t[rt][0], s.t[rt][1])) * c;
+    if (__builtin_amdgcn_ballot_w64(mx[0] > m[0] + kRaiseAbove || mx[1] > m[1] + kRaiseAbove) != 0) {
 #pragma unroll
       for (int rt = 0; rt < 2; ++rt) {
-        const float next = fmaxf(m_run[rt], mx[rt]), alpha = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[rt] - next);
-        m_run[rt] = next;
+        const float next = fmaxf(m[rt], mx[rt] + kLift), alpha = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[rt] - next);
+        m[rt] = next;
+        m_ref[rt] = fmaxf(next, kNoKeyYet);
         l[rt] *= alpha;
 #pragma unroll
         for (int dt = 0; dt < kDTiles; ++dt) o[dt][rt] *= alpha;
       }
     }
-    bf16x8 pf[2];
+  };
+  auto probability = [&](Scores& s, int rt, int e, float& sum) __attribute__((always_inline)) {
+    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s.get(rt, e), c, -m_ref[rt]));
+    s.set(rt, e, p);
+    sum += p;                                                // (before its rounding: lse keeps 32 bits)
+  };
+  auto probabilities = [&](Scores& s, int rt, u32x4& w, float& sum) __attribute__((always_inline)) {
+    sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) probability(s, rt, e, sum);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = rounded_pair(s.get(rt, 2 * k), s.get(rt, 2 * k + 1));
+  };
+
+  // ---- one block start to finish, for those that may reach the diagonal
+  auto plain_block = [&](int tile, int buf, int kb) __attribute__((always_inline)) {
+    const int key0 = tile * kTile + kb * 32;
+    if (key0 > wave_limit) return;
+    Scores s;
+    scores_of(buf, kb, s);
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt) {
-      const float from = fmaxf(m_run[rt], kNoKeyYet);
+      const int seen = limit[rt] - key0 - 4 * g;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][e >> 2][e & 3], c, -from));
-        l[rt] += p;                                          // (before its rounding: lse keeps 32 bits)
-        pf[rt][e] = (__bf16)p;
-      }
+      for (int e = 0; e < 8; ++e)
+        if (16 * (e >> 2) + (e & 3) > seen) s.set(rt, e, -INFINITY);
+    }
+    settle(s);
+    u32x4 w[2];
+    float sum[2];
+#pragma unroll
+    for (int rt = 0; rt < 2; ++rt) {
+      probabilities(s, rt, w[rt], sum[rt]);
+      l[rt] += sum[rt];
     }
     uint32_t odd = 0;
 #pragma unroll
     for (int dt = 0; dt < kDTiles; ++dt) {
-      const uint32_t at = (v_lane ^ (dt << 5)) + off + kb * 32 * kRowB;
-      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((MC_LDS bf16x4*)(uintptr_t)at);
-      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((MC_LDS bf16x4*)(uintptr_t)(at + 16 * kRowB));
-      bf16x8 vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      if constexpr (kMasked) {
-        u32x4 bits = __builtin_bit_cast(u32x4, vf);
+      u32x4 bits = __builtin_bit_cast(u32x4, load_v(buf, kb, dt));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t clean = finite_pair(bits[i]);
-          odd |= clean ^ bits[i];
-          bits[i] = clean;
-        }
-        vf = __builtin_bit_cast(bf16x8, bits);
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t clean = finite_pair(bits[i]);
+        odd |= clean ^ bits[i];
+        bits[i] = clean;
       }
 #pragma unroll
-      for (int rt = 0; rt < 2; ++rt) o[dt][rt] = mma(vf, pf[rt], o[dt][rt]);
+      for (int rt = 0; rt < 2; ++rt) o[dt][rt] = mma(__builtin_bit_cast(bf16x8, bits), __builtin_bit_cast(bf16x8, w[rt]), o[dt][rt]);
     }
-    if constexpr (kMasked) {
-      if (__builtin_amdgcn_ballot_w64(odd != 0) == 0) return;
-      // V has elements that are not finite: each for the rows that see its key
-      for (int from = 0; from < 4; ++from)                   // keys of lane group `from`
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd != 0) == 0, 1)) return;
+    // V has elements that are not finite: each for the rows that see its key
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+    for (int rt = 0; rt < 2; ++rt)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma nounroll
+        for (int from = 0; from < 4; ++from) {               // keys of lane group `from`
           const int row = kb * 32 + (e >> 2) * 16 + 4 * from + (e & 3);
+          const float p = __shfl(s.get(rt, e), from * 16 + j, 64);
+          if (tile * kTile + row > limit[rt]) continue;
 #pragma unroll
-          for (int rt = 0; rt < 2; ++rt) {
-            const float p = __shfl((float)pf[rt][e], from * 16 + j, 64);
-            if (tile * kTile + row > limit[rt]) continue;
+          for (int dt = 0; dt < kDTiles; ++dt) {
+            const int byte = (16 * dt + 4 * g) * 2;
+            const uint32_t at = base + kValueBase + buf * kKeyB + row * kRowB + (((byte >> 4) ^ Row::value(row)) << 4) + (byte & 8);
+            const u32x2 v = *reinterpret_cast<MC_LDS const u32x2*>(at);
 #pragma unroll
-            for (int dt = 0; dt < kDTiles; ++dt) {
-              const int byte = (16 * dt + 4 * g) * 2;
-              const uint32_t at = base + off + kKeyB + kRopeB + row * kRowB + (((byte >> 4) ^ Row::value(row)) << 4) + (byte & 8);
-              const u32x2 v = *reinterpret_cast<MC_LDS const u32x2*>(at);
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const uint32_t bits = r & 1 ? v[r >> 1] & 0xffff0000u : v[r >> 1] << 16;
-                if ((bits & 0x7f800000u) == 0x7f800000u) o[dt][rt][r] += p * __builtin_bit_cast(float, bits);
-              }
+            for (int r = 0; r < 4; ++r) {
+              const uint32_t bits = r & 1 ? v[r >> 1] & 0xffff0000u : v[r >> 1] << 16;
+              if ((bits & 0x7f800000u) == 0x7f800000u) o[dt][rt][r] += p * __builtin_bit_cast(float, bits);
             }
           }
         }
+  };
+
+  // ---- the loop over tiles that every row sees: a software pipeline over blocks of 32 keys.  Phase A makes the scores of the next block while the
+  //      vector unit turns those of this one, row tile 1, into probabilities; phase B multiplies this block's with V, while the next one's, row
+  //      tile 0, are turned.  One ring of fragments goes through both: use u takes slot u % kRing, which is filled for use u + kRing at once.
+  constexpr int kRing = D == 128 ? 5 : 4;
+  static_assert(kUses % kRing == 0 && kRing <= kV, "a use has the same slot in every block, and phase A reads ahead into its own block's V");
+  bf16x8 ring[kRing];
+  Scores s_cur, s_next;
+  u32x4 w_cur[2], w_next;                                    // probabilities as they are multiplied: of this block, and row tile 0 of the next
+  float sum_cur[2], sum_next;
+  // element x of 8 of row tile rt, its rounding with every second one
+  auto turn = [&](Scores& s, int rt, int x, u32x4& w, float& sum) __attribute__((always_inline)) {
+    probability(s, rt, x, sum);
+    if (x & 1) w[x >> 1] = rounded_pair(s.get(rt, x - 1), s.get(rt, x));
+  };
+  auto phase_a = [&](int buf, int kb, int buf_next, int kb_next) __attribute__((always_inline)) {
+    s_cur = s_next;
+    s_next.zero();
+    w_cur[0] = w_next;
+    sum_cur[0] = sum_next;
+    sum_cur[1] = 0.f;
+#pragma unroll
+    for (int u = 0; u < kK; ++u) {
+      s_next.t[0][u & 1] = mma(ring[u % kRing], qf[u >> 1][0], s_next.t[0][u & 1]);
+      __builtin_amdgcn_sched_barrier(0);
+      if (u < 8) turn(s_cur, 1, u, w_cur[1], sum_cur[1]);
+      __builtin_amdgcn_sched_barrier(0);
+      s_next.t[1][u & 1] = mma(ring[u % kRing], qf[u >> 1][1], s_next.t[1][u & 1]);
+      __builtin_amdgcn_sched_barrier(0);
+      ring[u % kRing] = u + kRing < kK ? load_k(buf_next, kb_next, u + kRing) : load_v(buf, kb, u + kRing - kK);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const uint32_t seen = w_cur[0][0] | w_cur[0][1] | w_cur[0][2] | w_cur[0][3] | w_cur[1][0] | w_cur[1][1] | w_cur[1][2] | w_cur[1][3];
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64((seen & kGuardBits) != 0) != 0, 0)) {
+      // a score outgrew its row's reference (or is not finite): the block again, against its true maxima
+      scores_of(buf, kb, s_cur);
+      settle(s_cur);
+#pragma unroll
+      for (int rt = 0; rt < 2; ++rt) probabilities(s_cur, rt, w_cur[rt], sum_cur[rt]);
+    }
+    l[0] += sum_cur[0];
+    l[1] += sum_cur[1];
+  };
+  // (buf_after, kb_after: the block whose scores come next)
+  auto phase_b = [&](int buf, int kb, int buf_after, int kb_after) __attribute__((always_inline)) {
+    sum_next = 0.f;
+#pragma unroll
+    for (int v = 0; v < kV; ++v) {
+      const int u = kK + v;
+      o[v][0] = mma(ring[u % kRing], __builtin_bit_cast(bf16x8, w_cur[0]), o[v][0]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int x = 8 / kV * v; x < 8 / kV * (v + 1); ++x) turn(s_next, 0, x, w_next, sum_next);
+      __builtin_amdgcn_sched_barrier(0);
+      o[v][1] = mma(ring[u % kRing], __builtin_bit_cast(bf16x8, w_cur[1]), o[v][1]);
+      __builtin_amdgcn_sched_barrier(0);
+      ring[u % kRing] = v + kRing < kV ? load_v(buf, kb, v + kRing) : load_k(buf_after, kb_after, v + kRing - kV);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
 
+  int buf = 0;
+  // Tile `tile` begins: the copies of the next one have landed everywhere (scores run a block ahead), the buffer of the one before is free.
+  auto tile_sync = [&](int tile) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(0x0F70);                      // (vmcnt(0): at most tile + 1 is on its way)
+    __syncthreads();
+    if (tile + 2 < tiles) fetch(tile + 2, buf == 0 ? kBufs - 1 : buf - 1);
+  };
+  int tile = t_lo;
   if (t_lo < tiles) {
     fetch(t_lo, 0);
     if (t_lo + 1 < tiles) fetch(t_lo + 1, 1);
-  }
-  int buf = 0;
-  for (int tile = t_lo; tile < tiles; ++tile) {
-    if (tile + 1 < tiles) __builtin_amdgcn_s_waitcnt(0x0F70 | kInFlight);      // (vmcnt: all but the next tile's copies)
-    else __builtin_amdgcn_s_waitcnt(0x0F70);
+    __builtin_amdgcn_s_waitcnt(0x0F70 | 0);
     __syncthreads();
-    if (tile + 2 < tiles) fetch(tile + 2, buf == 0 ? 2 : buf - 1);
-    if (tile < n_free) {
-      block(tile, buf, 0, Int<0>{});
-      block(tile, buf, 1, Int<0>{});
-    } else {
-      block(tile, buf, 0, Int<1>{});
-      block(tile, buf, 1, Int<1>{});
+  }
+  const int n_plain = n_free < tiles - 1 ? n_free : tiles - 1;
+  if (tile < n_plain) {
+    scores_of(0, 0, s_next);
+    settle(s_next);
+    probabilities(s_next, 0, w_next, sum_next);
+#pragma unroll
+    for (int u = 0; u < kRing; ++u) ring[u] = load_k(0, 1, u);
+    // the two waves of a SIMD run half a step apart: while one's softmax holds the vector unit, the other's products keep the matrix unit busy
+    const bool late = wave >= 4;
+    auto pipelined = [&](auto which) __attribute__((always_inline)) {
+      constexpr int b = decltype(which)::value, bn = (b + 1) % kBufs;
+      buf = b;
+      if (!late) tile_sync(tile);
+      phase_a(b, 0, b, 1);
+      if (late) tile_sync(tile);
+      phase_b(b, 0, bn, 0);
+      phase_a(b, 1, bn, 0);
+      phase_b(b, 1, bn, 1);
+      buf = bn;
+      ++tile;
+    };
+    for (;;) {
+      if (tile >= n_plain) break;
+      pipelined(Int<0>{});
+      if (tile >= n_plain) break;
+      pipelined(Int<1>{});
+      if (tile >= n_plain) break;
+      pipelined(Int<2>{});
     }
+  }
+  for (; tile < tiles; ++tile) {
+    tile_sync(tile);
+    plain_block(tile, buf, 0);
+    plain_block(tile, buf, 1);
     buf = buf == kBufs - 1 ? 0 : buf + 1;
   }
 
@@ -239,7 +395,7 @@ __global__ __launch_bounds__(512) void latent_prefill_kernel(const LatentPrefill
     const float all = sum_with_other_half(l[rt] + __shfl_xor(l[rt], 16, 64));
     if (!live[rt]) continue;
     const bool none = all == 0.f;                            // (a slice of the keys that the row sees nothing of)
-    const float inv = none ? 0.f : 1.0f / all, lse = none ? -INFINITY : (m_run[rt] + __builtin_amdgcn_logf(all)) * 0.6931471805599453f;
+    const float inv = none ? 0.f : 1.0f / all, lse = none ? -INFINITY : (m[rt] + __builtin_amdgcn_logf(all)) * 0.6931471805599453f;
     if constexpr (SPLIT) {
       const int64_t to = slice * a.rows_total + out_row[rt];
 #pragma unroll
