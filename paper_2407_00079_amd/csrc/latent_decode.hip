@@ -89,12 +89,13 @@ struct Line {
   }
 };
 
-// R: numbers of a latent vector; MT: 16-row tiles of a group of four waves; GROUPS of them
-template <int R, int MT, int GROUPS>
+// R: numbers of a latent vector; MT: 16-row tiles of a workgroup, whose four waves are RG groups of rows when they make scores
+template <int R, int MT, int RG>
 struct Shape {
   static constexpr int kCols = R + kLatentRope, kBlocks = kCols / 64, kSteps = kCols / 32;      // blocks of 64 columns, steps of 32
   static constexpr int kRowB = kCols * 2, kTileB = kTile * kRowB, kBlockB = kTile * 128;
-  static constexpr int kRows = 16 * MT * GROUPS, kAllWaves = 4 * GROUPS;
+  static constexpr int kRows = 16 * MT;
+  static constexpr int kKeyGroups = 4 / RG, kRowTiles = MT / RG, kKeyTiles = kTile / 16 / kKeyGroups;      // a wave's share of the scores
   static constexpr int kColTiles = R / 64;                   // 16-column tiles of the output a wave has
   static constexpr int kPRowB = kTile * 2 + 16;              // 16 rows of a column spread over the banks
   // A tile in LDS: block by block of 64 columns, in each 64 rows of 128 bytes, the 16-byte granules of row r at their place ^ swizzle(r).  The
@@ -103,18 +104,19 @@ struct Shape {
   static __device__ __forceinline__ int swizzle(int r) { return (r & 2) | ((r >> 1) & 4) | ((r >> 2) & 1); }
   struct Shared {
     char tile[2][kTileB];
-    char p[GROUPS][16 * MT][kPRowB];
-    float most[kAllWaves][MT][16], sum[kAllWaves][MT][16];
-    int outgrown[8];
+    char p[kRows][kPRowB];
+    float most[MT][kKeyGroups][16], sum[MT][kKeyGroups][16];
+    int outgrown[4];
   };
 };
 
-template <int R, int MT, int GROUPS>
-__global__ __launch_bounds__(GROUPS * 256) void latent_decode_kernel(const LatentDecodeArgs a) {
-  typedef Shape<R, MT, GROUPS> S;
+template <int R, int MT, int RG>
+__global__ __launch_bounds__(256) void latent_decode_kernel(const LatentDecodeArgs a) {
+  typedef Shape<R, MT, RG> S;
+  constexpr int MR = S::kRowTiles, KT = S::kKeyTiles, KG = S::kKeyGroups;
   __shared__ __attribute__((aligned(256))) typename S::Shared sh;
   const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave >> 2, w = wave & 3;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = w % KG, m0 = w / KG * MR;      // its keys' and first rows' place
   const int tile = (int)(blockIdx.x / (uint32_t)a.stretches), stretch = (int)blockIdx.x - tile * a.stretches;
   const Line line(a);
   const typename Line::Sums sums = line.sums();
@@ -125,16 +127,14 @@ __global__ __launch_bounds__(GROUPS * 256) void latent_decode_kernel(const Laten
   LatentChain open = {0, 0, 0, 0};
 
   if (begin < end) {
-    // this lane's query rows
-    int row[MT], back[MT];                                   // stacked row; keys before the row's length that it does not see
-    bool live[MT];
+    // stacked row j of row tile m (rows past the last compute it again), and the keys before a row's length that it does not see
+    auto stacked_row = [&](int m) __attribute__((always_inline)) {
+      const int r = tile * S::kRows + m * 16 + j;
+      return r < a.stacked ? r : a.stacked - 1;
+    };
+    int back[MR];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      const int r = tile * S::kRows + (group * MT + m) * 16 + j;
-      live[m] = r < a.stacked;
-      row[m] = live[m] ? r : a.stacked - 1;                  // (rows past the last compute it again)
-      back[m] = a.tokens - 1 - row[m] / a.heads;
-    }
+    for (int m = 0; m < MR; ++m) back[m] = a.tokens - 1 - stacked_row(m0 + m) / a.heads;
     const uint32_t base = (uint32_t)(uintptr_t)(MC_LDS char*)&sh;
     uint32_t source[2];                                      // of a lane's 16 bytes of 8 rows by 128 bytes: rows 0-7 and 8-15 of a page
 #pragma unroll
@@ -145,31 +145,32 @@ __global__ __launch_bounds__(GROUPS * 256) void latent_decode_kernel(const Laten
       const uint32_t to = base + buf * S::kTileB + w * (kPageTokens * 128);
 #pragma unroll
       for (int b = 0; b < S::kBlocks; ++b) {
-        if constexpr (GROUPS == 1) {
-          dma16(from + b * 128, source[0], to + b * S::kBlockB);
-          dma16(from + b * 128, source[1], to + b * S::kBlockB + 1024);
-        } else {
-          dma16(from + b * 128, group == 0 ? source[0] : source[1], to + b * S::kBlockB + group * 1024);
-        }
+        dma16(from + b * 128, source[0], to + b * S::kBlockB);
+        dma16(from + b * 128, source[1], to + b * S::kBlockB + 1024);
       }
     };
-    // fragment addresses: as keys (rows 16 w + j), as values (columns R/4 w + 16 t, keys 8 g .. of a half of the tile)
-    const uint32_t k_lane = base + (16 * w + j) * 128 + ((g ^ S::swizzle(j)) << 4);
+    // fragment addresses: as keys (rows 16 KT kg + j), as values (columns R/4 w + 16 t, keys 8 g .. of a half of the tile)
+    const uint32_t k_lane = base + (16 * KT * kg + j) * 128 + ((g ^ S::swizzle(j)) << 4);
     const int r0 = 8 * g + (j >> 2);
     const uint32_t v_lane = base + (R / 256) * w * S::kBlockB + r0 * 128 + ((((j & 3) >> 1) ^ S::swizzle(r0)) << 4) + ((j & 1) << 3);
-    const uint32_t p_base = base + (uint32_t)__builtin_offsetof(typename S::Shared, p) + group * (16 * MT * S::kPRowB);
+    const uint32_t p_base = base + (uint32_t)__builtin_offsetof(typename S::Shared, p);
+    const uint32_t p_read = p_base + j * S::kPRowB + g * 16, p_write = p_base + (16 * m0 + j) * S::kPRowB + (16 * KT * kg + 4 * g) * 2;
 
-    bf16x8 qf[S::kSteps][MT];
-    f32x4 o[S::kColTiles][MT];
-    float ref[MT], l[MT];
+    bf16x8 qf[S::kSteps][MR];                                // of the wave's rows of scores
+    f32x4 o[S::kColTiles][MT];                               // of all rows: the wave's columns
+    float ref[MR], ref_all[MT], l[MR];
     auto start = [&](const At& at) __attribute__((always_inline)) {
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const char* const q = reinterpret_cast<const char*>(a.q) + ((int64_t)at.row * a.stacked + row[m]) * S::kRowB;
+      for (int m = 0; m < MR; ++m) {
+        const char* const q = reinterpret_cast<const char*>(a.q) + ((int64_t)at.row * a.stacked + stacked_row(m0 + m)) * S::kRowB;
 #pragma unroll
         for (int st = 0; st < S::kSteps; ++st) qf[st][m] = *reinterpret_cast<const bf16x8*>(q + st * 64 + g * 16);
         ref[m] = -INFINITY;
         l[m] = 0.f;
+      }
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        ref_all[m] = -INFINITY;
 #pragma unroll
         for (int t = 0; t < S::kColTiles; ++t) o[t][m] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
@@ -194,74 +195,96 @@ __global__ __launch_bounds__(GROUPS * 256) void latent_decode_kernel(const Laten
       __syncthreads();
       fetch_next();
 
-      // scores of keys 16 w + 4 g + i for row j of each tile of rows
-      f32x4 s[MT];
+      // scores of keys 16 (KT kg + kt) + 4 g + i for row j of each of the wave's tiles of rows
+      f32x4 s[MR][KT];
 #pragma unroll
-      for (int m = 0; m < MT; ++m) s[m] = f32x4{0.f, 0.f, 0.f, 0.f};
-      // (fragments are asked for kAhead steps before they are used, and no earlier: with 64 rows there are no registers for more)
-      constexpr int kAhead = 3;
-      bf16x8 ring[kAhead];
-      auto key = [&](int st) __attribute__((always_inline)) {
-        return *reinterpret_cast<MC_LDS const bf16x8*>((k_lane ^ ((st & 1) << 6)) + buf * S::kTileB + (st >> 1) * S::kBlockB);
-      };
+      for (int m = 0; m < MR; ++m)
 #pragma unroll
-      for (int st = 0; st < kAhead; ++st) ring[st] = key(st);
+        for (int kt = 0; kt < KT; ++kt) s[m][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      {
+        // (fragments are asked for kAhead uses before theirs, and no earlier: there are not the registers for more)
+        constexpr int kUses = S::kSteps * KT, kAhead = 5;
+        bf16x8 ring[kAhead];
+        auto key = [&](int u) __attribute__((always_inline)) {
+          const int st = u / KT, kt = u % KT;
+          return *reinterpret_cast<MC_LDS const bf16x8*>((k_lane ^ ((st & 1) << 6)) + buf * S::kTileB + (st >> 1) * S::kBlockB + kt * (16 * 128));
+        };
 #pragma unroll
-      for (int st = 0; st < S::kSteps; ++st) {
+        for (int u = 0; u < kAhead; ++u) ring[u] = key(u);
 #pragma unroll
-        for (int m = 0; m < MT; ++m) s[m] = mma(ring[st % kAhead], qf[st][m], s[m]);
-        if (st + kAhead < S::kSteps) ring[st % kAhead] = key(st + kAhead);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int u = 0; u < kUses; ++u) {
+#pragma unroll
+          for (int m = 0; m < MR; ++m) s[m][u % KT] = mma(ring[u % kAhead], qf[u / KT][m], s[m][u % KT]);
+          if (u + kAhead < kUses) ring[u % kAhead] = key(u + kAhead);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
       if constexpr (tail) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          const int seen = at.len - back[m] - block * kTile - 16 * w - 4 * g;
+        for (int m = 0; m < MR; ++m) {
+          const int seen = at.len - back[m] - block * kTile - 16 * KT * kg - 4 * g;
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (i >= seen) s[m][i] = -INFINITY;
+          for (int e = 0; e < 4 * KT; ++e)
+            if (16 * (e >> 2) + (e & 3) >= seen) s[m][e >> 2][e & 3] = -INFINITY;
         }
       }
-      float most[MT];
+      float most[MR];
       bool over = false;
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        most[m] = max_over_groups(larger(larger(s[m][0], s[m][1]), larger(s[m][2], s[m][3]))) * c;
+      for (int m = 0; m < MR; ++m) {
+        float x = s[m][0][0];
+#pragma unroll
+        for (int e = 1; e < 4 * KT; ++e) x = larger(x, s[m][e >> 2][e & 3]);
+        most[m] = max_over_groups(x) * c;
         over |= most[m] > ref[m] + kRescaleSlack;
       }
       const bool outgrown = __builtin_amdgcn_ballot_w64(over) != 0;
-      if (lane == 0) sh.outgrown[wave] = outgrown;
-      float p[MT][4];
+      if (lane == 0) sh.outgrown[w] = outgrown;
+      float sum[MR];
       auto probabilities = [&]() __attribute__((always_inline)) {
         typedef float f32x2 __attribute__((ext_vector_type(2)));
         typedef __attribute__((__vector_size__(4))) __bf16 bf16x2;
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
+        for (int m = 0; m < MR; ++m) {
           const float from = fmaxf(ref[m], kNoKeyYet);
+          sum[m] = 0.f;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) p[m][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][i], c, -from));
-          const uint32_t low = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[m][0], p[m][1]}, bf16x2));
-          const uint32_t high = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[m][2], p[m][3]}, bf16x2));
-          *reinterpret_cast<MC_LDS u32x2*>(p_base + (16 * m + j) * S::kPRowB + (16 * w + 4 * g) * 2) = u32x2{low, high};
+          for (int kt = 0; kt < KT; ++kt) {
+            float p[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][kt][i], c, -from));
+              sum[m] += p[i];                                // (before its rounding: lse keeps 32 bits)
+            }
+            const uint32_t low = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[0], p[1]}, bf16x2));
+            const uint32_t high = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[2], p[3]}, bf16x2));
+            *reinterpret_cast<MC_LDS u32x2*>(p_write + 16 * m * S::kPRowB + kt * 32) = u32x2{low, high};
+          }
         }
       };
       probabilities();
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
-        if (g == 0) sh.most[wave][m][j] = most[m];
+      for (int m = 0; m < MR; ++m)
+        if (g == 0) sh.most[m0 + m][kg][j] = most[m];
       __syncthreads();
-      int any = 0;
+      if (__builtin_amdgcn_readfirstlane(sh.outgrown[0] | sh.outgrown[1] | sh.outgrown[2] | sh.outgrown[3]) != 0) {      // (the same for all waves)
+        auto raised = [&](int m, float from) __attribute__((always_inline)) {
+          float top = from;
 #pragma unroll
-      for (int i = 0; i < S::kAllWaves; ++i) any |= sh.outgrown[i];
-      if (__builtin_amdgcn_readfirstlane(any) != 0) {        // (the same for all waves of the workgroup)
+          for (int i = 0; i < KG; ++i) top = fmaxf(top, sh.most[m][i][j]);
+          return top;
+        };
+        auto factor = [](float from, float to) __attribute__((always_inline)) { return to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(from - to); };
+#pragma unroll
+        for (int m = 0; m < MR; ++m) {
+          const float next = raised(m0 + m, ref[m]);
+          l[m] *= factor(ref[m], next);
+          ref[m] = next;
+        }
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-          float top = sh.most[4 * group][m][j];
-#pragma unroll
-          for (int i = 1; i < 4; ++i) top = fmaxf(top, sh.most[4 * group + i][m][j]);
-          const float next = fmaxf(ref[m], top), alpha = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[m] - next);
-          ref[m] = next;
-          l[m] *= alpha;
+          const float next = raised(m, ref_all[m]), alpha = factor(ref_all[m], next);
+          ref_all[m] = next;
 #pragma unroll
           for (int t = 0; t < S::kColTiles; ++t) o[t][m] *= alpha;
         }
@@ -269,17 +292,13 @@ __global__ __launch_bounds__(GROUPS * 256) void latent_decode_kernel(const Laten
         __syncthreads();
       }
 #pragma unroll
-      for (int m = 0; m < MT; ++m) l[m] += (p[m][0] + p[m][1]) + (p[m][2] + p[m][3]);      // (before their rounding: lse keeps 32 bits)
+      for (int m = 0; m < MR; ++m) l[m] += sum[m];
       // output += values of this wave's columns
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        bf16x8 pf[MT];
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-          pf[m] = *reinterpret_cast<MC_LDS const bf16x8*>(p_base + (16 * m + j) * S::kPRowB + half * 64 + g * 16);
-        constexpr int kAhead = 2;
-        bf16x8 ring[kAhead];
-        auto value = [&](int t) __attribute__((always_inline)) {
+      {
+        constexpr int kUses = 2 * S::kColTiles, kAhead = 3;
+        bf16x8 ring[kAhead], pf[MT];
+        auto value = [&](int u) __attribute__((always_inline)) {
+          const int half = u / S::kColTiles, t = u % S::kColTiles;
           const uint32_t at0 = (v_lane ^ ((t & 3) << 5)) + buf * S::kTileB + (t >> 2) * S::kBlockB + half * (32 * 128);
           const uint32_t at1 = (v_lane ^ ((t & 3) << 5) ^ 16) + buf * S::kTileB + (t >> 2) * S::kBlockB + half * (32 * 128) + 4 * 128;
           const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((MC_LDS bf16x4*)(uintptr_t)at0);
@@ -287,10 +306,15 @@ __global__ __launch_bounds__(GROUPS * 256) void latent_decode_kernel(const Laten
           return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         };
 #pragma unroll
-        for (int t = 0; t < kAhead; ++t) ring[t] = value(t);
+        for (int u = 0; u < kAhead; ++u) ring[u] = value(u);
 #pragma unroll
-        for (int t = 0; t < S::kColTiles; ++t) {
-          bf16x8 vf = ring[t % kAhead];
+        for (int u = 0; u < kUses; ++u) {
+          const int t = u % S::kColTiles;
+          if (t == 0) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m) pf[m] = *reinterpret_cast<MC_LDS const bf16x8*>(p_read + 16 * m * S::kPRowB + u / S::kColTiles * 64);
+          }
+          bf16x8 vf = ring[u % kAhead];
           if constexpr (tail) {
             u32x4 bits = __builtin_bit_cast(u32x4, vf);
 #pragma unroll
@@ -299,7 +323,7 @@ __global__ __launch_bounds__(GROUPS * 256) void latent_decode_kernel(const Laten
           }
 #pragma unroll
           for (int m = 0; m < MT; ++m) o[t][m] = mma(vf, pf[m], o[t][m]);
-          if (t + kAhead < S::kColTiles) ring[t % kAhead] = value(t + kAhead);
+          if (u + kAhead < kUses) ring[u % kAhead] = value(u + kAhead);
           __builtin_amdgcn_sched_barrier(0);
         }
       }
@@ -320,23 +344,23 @@ __global__ __launch_bounds__(GROUPS * 256) void latent_decode_kernel(const Laten
       // the row's sums over the waves' keys, then its result or its part of one
       const bool done = stop == at.blocks;
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        float all = l[m] + __shfl_xor(l[m], 16, 64);
-        all = sum_with_other_half(all);
-        if (g == 0) sh.sum[wave][m][j] = all;
+      for (int m = 0; m < MR; ++m) {
+        const float all = sum_with_other_half(l[m] + __shfl_xor(l[m], 16, 64));
+        if (g == 0) sh.sum[m0 + m][kg][j] = all;
       }
       __syncthreads();
       const int64_t part0 = (((int64_t)tile * a.stretches + stretch) * 2 + (whole ? 1 : 0)) * S::kRows;
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        float all = sh.sum[4 * group][m][j];
+        float all = sh.sum[m][0][j];
 #pragma unroll
-        for (int i = 1; i < 4; ++i) all += sh.sum[4 * group + i][m][j];
-        if (!live[m]) continue;
+        for (int i = 1; i < KG; ++i) all += sh.sum[m][i][j];
+        const int row = tile * S::kRows + m * 16 + j;
+        if (row >= a.stacked) continue;
         const int col = (R / 4) * w + 4 * g;
         if (whole && done) {
           const float inv = all == 0.f ? 0.f : 1.0f / all;             // (a row that sees no key: 0)
-          const int64_t to = (int64_t)at.row * a.stacked + row[m];
+          const int64_t to = (int64_t)at.row * a.stacked + row;
 #pragma unroll
           for (int t = 0; t < S::kColTiles; ++t) {
             bf16x4 v;
@@ -344,12 +368,12 @@ __global__ __launch_bounds__(GROUPS * 256) void latent_decode_kernel(const Laten
             for (int i = 0; i < 4; ++i) v[i] = (__bf16)(o[t][m][i] * inv);
             *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(a.out) + to * R + col + 16 * t) = v;
           }
-          if (a.lse != nullptr && w == 0 && g == 0) a.lse[to] = (ref[m] + __builtin_amdgcn_logf(all)) * 0.6931471805599453f;
+          if (a.lse != nullptr && w == 0 && g == 0) a.lse[to] = (ref_all[m] + __builtin_amdgcn_logf(all)) * 0.6931471805599453f;
         } else {
-          const int64_t to = part0 + (group * MT + m) * 16 + j;
+          const int64_t to = part0 + m * 16 + j;
 #pragma unroll
           for (int t = 0; t < S::kColTiles; ++t) *reinterpret_cast<f32x4*>(a.o_parts + to * R + col + 16 * t) = o[t][m];
-          if (w == 0 && g == 0) a.ml_parts[to] = float2{ref[m], all};
+          if (w == 0 && g == 0) a.ml_parts[to] = float2{ref_all[m], all};
         }
       }
       if (whole) {
@@ -366,12 +390,12 @@ __global__ __launch_bounds__(GROUPS * 256) void latent_decode_kernel(const Laten
   if (notes && !by_row) a.chains[stretch] = open;
 
   // padding rows, shared out over the stretches
-  for (int64_t first = stretch; first < a.batch; first += (int64_t)a.stretches * (GROUPS * 256)) {
+  for (int64_t first = stretch; first < a.batch; first += (int64_t)a.stretches * 256) {
     const int64_t r = first + (int64_t)threadIdx.x * a.stretches;
     const bool empty = r < a.batch && line.valid(a.seq_lens[r]) == 0;
     if (empty && tile == 0 && by_row) a.chains[r].more = 0;
     for (uint64_t some = __builtin_amdgcn_ballot_w64(empty); some != 0; some &= some - 1) {
-      const int64_t out_row = (first + (int64_t)(wave * 64 + __builtin_ctzll(some)) * a.stretches) * a.stacked + tile * S::kRows;
+      const int64_t out_row = (first + (int64_t)(w * 64 + __builtin_ctzll(some)) * a.stretches) * a.stacked + tile * S::kRows;
       const int rows = a.stacked - tile * S::kRows < S::kRows ? a.stacked - tile * S::kRows : S::kRows;
       u32x4* const to = reinterpret_cast<u32x4*>(reinterpret_cast<__bf16*>(a.out) + out_row * R);
       for (int i = lane; i < rows * (R / 8); i += 64) to[i] = u32x4{};
@@ -444,14 +468,72 @@ __global__ __launch_bounds__(kJoinThreads) void latent_join_kernel(const LatentD
   if (a.lse != nullptr && blockIdx.z == 0 && t == 0) a.lse[to] = (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
+// The same for many rows, of few parts each as a rule: a wave has 128 columns of a stacked row, its halves every other part.
+constexpr int kRowJoinThreads = 256;
+template <int R>
+__global__ __launch_bounds__(kRowJoinThreads) void latent_join_rows_kernel(const LatentDecodeArgs a, int tile_rows) {
+  constexpr int kGroups = R / kJoinCols, kRowsOfWg = kRowJoinThreads / 64 / kGroups > 0 ? kRowJoinThreads / 64 / kGroups : 1;
+  static_assert(kRowsOfWg * kGroups * 64 == kRowJoinThreads, "whole rows a workgroup");
+  const LatentChain chain = a.chains[blockIdx.x];
+  if (chain.more == 0) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = (wave % kGroups) * kJoinCols + (lane & 31) * 4;
+  const int stacked = blockIdx.y * kRowsOfWg + wave / kGroups, tile = stacked / tile_rows, in_tile = stacked - tile * tile_rows;
+  if (stacked >= a.stacked) return;
+  auto part = [&](int i) __attribute__((always_inline)) {
+    return (((int64_t)tile * a.stretches + chain.first + i) * 2 + (i == 0 ? 1 : 0)) * tile_rows + in_tile;
+  };
+  const int n = chain.more + 1;
+  float top = -INFINITY;
+  for (int i = lane; i < n; i += 64) top = fmaxf(top, a.ml_parts[part(i)].x);
+#pragma unroll
+  for (int step = 1; step < 64; step *= 2) top = fmaxf(top, __shfl_xor(top, step, 64));
+  const float from = top == -INFINITY ? 0.f : top;           // (every score is -inf or NaN)
+  float l = 0.f;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  constexpr int kAtOnce = 4;
+  for (int i0 = half; i0 < n; i0 += 2 * kAtOnce) {
+    f32x4 v[kAtOnce];
+    float2 ml[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int64_t at = part(i0 + 2 * k < n ? i0 + 2 * k : i0);
+      v[k] = *reinterpret_cast<const f32x4*>(a.o_parts + at * R + col);
+      ml[k] = a.ml_parts[at];
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k)
+      if (i0 + 2 * k < n) {
+        const float weight = __builtin_amdgcn_exp2f(ml[k].x - from);
+        l += weight * ml[k].y;
+        x += weight * v[k];
+      }
+  }
+  l += __shfl_xor(l, 32, 64);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] += __shfl_xor(x[i], 32, 64);
+  if (half != 0) return;
+  const int64_t to = (int64_t)chain.row * a.stacked + stacked;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  bf16x4 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = (__bf16)(x[i] * inv);
+  *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(a.out) + to * R + col) = y;
+  if (a.lse != nullptr && col == 0) a.lse[to] = (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
 template <int R>
 hipError_t enqueue(int rows, const LatentDecodeArgs& args, hipStream_t stream) {
   const int wgs = args.tiles * args.stretches;
   if (rows == 16) latent_decode_kernel<R, 1, 1><<<wgs, 256, 0, stream>>>(args);
   else if (rows == 32) latent_decode_kernel<R, 2, 1><<<wgs, 256, 0, stream>>>(args);
-  else if (rows == 64) latent_decode_kernel<R, 2, 2><<<wgs, 512, 0, stream>>>(args);
+  else if (rows == 64) latent_decode_kernel<R, 4, 2><<<wgs, 256, 0, stream>>>(args);
   else return hipErrorInvalidValue;
-  latent_join_kernel<R><<<dim3(args.n_chains, args.stacked, R / kJoinCols), kJoinThreads, 0, stream>>>(args, rows);
+  if (args.n_chains * args.stacked < 512) {
+    latent_join_kernel<R><<<dim3(args.n_chains, args.stacked, R / kJoinCols), kJoinThreads, 0, stream>>>(args, rows);
+  } else {
+    constexpr int kRowsOfWg = kRowJoinThreads / 64 / (R / kJoinCols);
+    latent_join_rows_kernel<R><<<dim3(args.n_chains, (args.stacked + kRowsOfWg - 1) / kRowsOfWg), kRowJoinThreads, 0, stream>>>(args, rows);
+  }
   return hipGetLastError();
 }
 
