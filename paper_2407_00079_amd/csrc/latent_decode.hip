@@ -22,7 +22,7 @@ namespace mc {
 namespace {
 
 constexpr int kTile = kLatentTileKeys, kTilePages = kTile / kPageTokens;
-static_assert(kTilePages == 4, "a page for each wave of a group");
+static_assert(kTilePages * 2 == kWaves, "half a page for each wave");
 
 struct At {
   int row, block, blocks, len;               // tile `block` of the row's `blocks`
@@ -89,14 +89,14 @@ struct Line {
   }
 };
 
-// R: numbers of a latent vector; MT: 16-row tiles of a workgroup, whose four waves are RG groups of rows when they make scores
-template <int R, int MT, int RG>
+// R: numbers of a latent vector; MT: 16-row tiles of a workgroup.  Scores: a wave has one of them and its share of the keys.
+template <int R, int MT>
 struct Shape {
   static constexpr int kCols = R + kLatentRope, kBlocks = kCols / 64, kSteps = kCols / 32;      // blocks of 64 columns, steps of 32
   static constexpr int kRowB = kCols * 2, kTileB = kTile * kRowB, kBlockB = kTile * 128;
   static constexpr int kRows = 16 * MT;
-  static constexpr int kKeyGroups = 4 / RG, kRowTiles = MT / RG, kKeyTiles = kTile / 16 / kKeyGroups;      // a wave's share of the scores
-  static constexpr int kColTiles = R / 64;                   // 16-column tiles of the output a wave has
+  static constexpr int kKeyGroups = MT == 4 ? 2 : 4, kKeyTiles = kTile / 16 / kKeyGroups, kScoring = MT * kKeyGroups;      // waves that make scores
+  static constexpr int kColTiles = R / 16 / kWaves;   // 16-column tiles of the output a wave has
   static constexpr int kPRowB = kTile * 2 + 16;              // 16 rows of a column spread over the banks
   // A tile in LDS: block by block of 64 columns, in each 64 rows of 128 bytes, the 16-byte granules of row r at their place ^ swizzle(r).  The
   // 256 bytes of all banks are two rows: reads of one granule of 16 rows, and transposing reads of 32 bytes of rows 0-3 and 8-11
@@ -106,17 +106,18 @@ struct Shape {
     char tile[2][kTileB];
     char p[kRows][kPRowB];
     float most[MT][kKeyGroups][16], sum[MT][kKeyGroups][16];
-    int outgrown[4];
+    int outgrown[kWaves];
   };
 };
 
-template <int R, int MT, int RG>
-__global__ __launch_bounds__(256) void latent_decode_kernel(const LatentDecodeArgs a) {
-  typedef Shape<R, MT, RG> S;
-  constexpr int MR = S::kRowTiles, KT = S::kKeyTiles, KG = S::kKeyGroups;
+template <int R, int MT>
+__global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const LatentDecodeArgs a) {
+  typedef Shape<R, MT> S;
+  constexpr int KT = S::kKeyTiles, KG = S::kKeyGroups;
+  constexpr bool kAllScore = S::kScoring == kWaves;
   __shared__ __attribute__((aligned(256))) typename S::Shared sh;
   const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = w % KG, m0 = w / KG * MR;      // its keys' and first rows' place
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = w % KG, mine = w / KG % MT;      // its keys and rows of scores
   const int tile = (int)(blockIdx.x / (uint32_t)a.stretches), stretch = (int)blockIdx.x - tile * a.stretches;
   const Line line(a);
   const typename Line::Sums sums = line.sums();
@@ -132,42 +133,45 @@ __global__ __launch_bounds__(256) void latent_decode_kernel(const LatentDecodeAr
       const int r = tile * S::kRows + m * 16 + j;
       return r < a.stacked ? r : a.stacked - 1;
     };
-    int back[MR];
-#pragma unroll
-    for (int m = 0; m < MR; ++m) back[m] = a.tokens - 1 - stacked_row(m0 + m) / a.heads;
+    const int my_row = stacked_row(mine), back = a.tokens - 1 - my_row / a.heads;
+    const bool scoring = kAllScore || w < S::kScoring;
     const uint32_t base = (uint32_t)(uintptr_t)(MC_LDS char*)&sh;
-    uint32_t source[2];                                      // of a lane's 16 bytes of 8 rows by 128 bytes: rows 0-7 and 8-15 of a page
+    // A copy instruction holds its wave for over 100 cycles: all waves share a tile's, or (16 rows) those that make no scores do them.
+    constexpr int kHalves = kAllScore ? 1 : 2;               // 8 rows by 128 bytes of a page: rows 0-7, 8-15
+    const bool copies = kAllScore || !scoring;
+    const int copy_page = kAllScore ? w >> 1 : w & 3;
+    uint32_t source[kHalves];                                // of a lane's 16 bytes
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      source[h] = (uint32_t)((8 * h + lane / 8) * S::kRowB + ((lane % 8) ^ S::swizzle(8 * h + lane / 8)) * 16);
+    for (int h = 0; h < kHalves; ++h) {
+      const int r = 8 * (kAllScore ? w & 1 : h) + lane / 8;
+      source[h] = (uint32_t)(r * S::kRowB + ((lane % 8) ^ S::swizzle(r)) * 16);
+    }
     auto fetch = [&](int page, int buf) __attribute__((always_inline)) {
       const char* const from = reinterpret_cast<const char*>(a.pool) + (int64_t)page * (kPageTokens * S::kRowB);
-      const uint32_t to = base + buf * S::kTileB + w * (kPageTokens * 128);
+      const uint32_t to = base + buf * S::kTileB + copy_page * (kPageTokens * 128) + (kAllScore ? (w & 1) * 1024 : 0);
 #pragma unroll
-      for (int b = 0; b < S::kBlocks; ++b) {
-        dma16(from + b * 128, source[0], to + b * S::kBlockB);
-        dma16(from + b * 128, source[1], to + b * S::kBlockB + 1024);
-      }
+      for (int b = 0; b < S::kBlocks; ++b)
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) dma16(from + b * 128, source[h], to + b * S::kBlockB + h * 1024);
     };
-    // fragment addresses: as keys (rows 16 KT kg + j), as values (columns R/4 w + 16 t, keys 8 g .. of a half of the tile)
+    // fragment addresses: as keys (rows 16 KT kg + j), as values (columns R/8 w + 16 t, keys 8 g .. of a half of the tile)
     const uint32_t k_lane = base + (16 * KT * kg + j) * 128 + ((g ^ S::swizzle(j)) << 4);
     const int r0 = 8 * g + (j >> 2);
-    const uint32_t v_lane = base + (R / 256) * w * S::kBlockB + r0 * 128 + ((((j & 3) >> 1) ^ S::swizzle(r0)) << 4) + ((j & 1) << 3);
+    const uint32_t v_lane = base + (R / 8 * w / 64) * S::kBlockB + r0 * 128 + (((((j & 3) >> 1) ^ S::swizzle(r0)) ^ (R / 8 * w % 64 / 8)) << 4) + ((j & 1) << 3);
     const uint32_t p_base = base + (uint32_t)__builtin_offsetof(typename S::Shared, p);
-    const uint32_t p_read = p_base + j * S::kPRowB + g * 16, p_write = p_base + (16 * m0 + j) * S::kPRowB + (16 * KT * kg + 4 * g) * 2;
+    const uint32_t p_read = p_base + j * S::kPRowB + g * 16, p_write = p_base + (16 * mine + j) * S::kPRowB + (16 * KT * kg + 4 * g) * 2;
 
-    bf16x8 qf[S::kSteps][MR];                                // of the wave's rows of scores
+    bf16x8 qf[S::kSteps];                                    // of the wave's rows of scores
     f32x4 o[S::kColTiles][MT];                               // of all rows: the wave's columns
-    float ref[MR], ref_all[MT], l[MR];
+    float ref, ref_all[MT], l;
     auto start = [&](const At& at) __attribute__((always_inline)) {
+      if (scoring) {
+        const char* const q = reinterpret_cast<const char*>(a.q) + ((int64_t)at.row * a.stacked + my_row) * S::kRowB;
 #pragma unroll
-      for (int m = 0; m < MR; ++m) {
-        const char* const q = reinterpret_cast<const char*>(a.q) + ((int64_t)at.row * a.stacked + stacked_row(m0 + m)) * S::kRowB;
-#pragma unroll
-        for (int st = 0; st < S::kSteps; ++st) qf[st][m] = *reinterpret_cast<const bf16x8*>(q + st * 64 + g * 16);
-        ref[m] = -INFINITY;
-        l[m] = 0.f;
+        for (int st = 0; st < S::kSteps; ++st) qf[st] = *reinterpret_cast<const bf16x8*>(q + st * 64 + g * 16);
       }
+      ref = -INFINITY;
+      l = 0.f;
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         ref_all[m] = -INFINITY;
@@ -179,13 +183,13 @@ __global__ __launch_bounds__(256) void latent_decode_kernel(const LatentDecodeAr
 
     // the tile whose copy is next, and the page of it that this wave copies
     At nx = line.place(sums, begin);
-    int page = line.page(nx, w), fetched = 0, left = end - begin;
+    int page = line.page(nx, copy_page), fetched = 0, left = end - begin;
     auto fetch_next = [&]() __attribute__((always_inline)) {
       if (fetched == end - begin) return;
-      fetch(page, fetched & 1);
+      if (copies) fetch(page, fetched & 1);
       if (++fetched == end - begin) return;
       line.next(nx);
-      page = line.page(nx, w);
+      page = line.page(nx, copy_page);
     };
     int buf = 1;
     auto one_tile = [&](const At& at, int block, auto tail_tag) __attribute__((always_inline)) {
@@ -195,15 +199,32 @@ __global__ __launch_bounds__(256) void latent_decode_kernel(const LatentDecodeAr
       __syncthreads();
       fetch_next();
 
-      // scores of keys 16 (KT kg + kt) + 4 g + i for row j of each of the wave's tiles of rows
-      f32x4 s[MR][KT];
+      // scores of keys 16 (KT kg + kt) + 4 g + i for row j of the wave's tile of rows
+      f32x4 s[KT];
+      float sum = 0.f;
+      auto probabilities = [&]() __attribute__((always_inline)) {
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        typedef __attribute__((__vector_size__(4))) __bf16 bf16x2;
+        const float from = fmaxf(ref, kNoKeyYet);
+        sum = 0.f;
 #pragma unroll
-      for (int m = 0; m < MR; ++m)
+        for (int kt = 0; kt < KT; ++kt) {
+          float p[4];
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) s[m][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-      {
-        // (fragments are asked for kAhead uses before theirs, and no earlier: there are not the registers for more)
-        constexpr int kUses = S::kSteps * KT, kAhead = 5;
+          for (int i = 0; i < 4; ++i) {
+            p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i], c, -from));
+            sum += p[i];                                     // (before its rounding: lse keeps 32 bits)
+          }
+          const uint32_t low = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[0], p[1]}, bf16x2));
+          const uint32_t high = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[2], p[3]}, bf16x2));
+          *reinterpret_cast<MC_LDS u32x2*>(p_write + kt * 32) = u32x2{low, high};
+        }
+      };
+      if (scoring) {
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) s[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        f32x4 s2 = {0.f, 0.f, 0.f, 0.f};                     // (KT 1: every other step, so that no product waits for the one before)
+        constexpr int kUses = S::kSteps * KT, kAhead = 6;
         bf16x8 ring[kAhead];
         auto key = [&](int u) __attribute__((always_inline)) {
           const int st = u / KT, kt = u % KT;
@@ -213,61 +234,32 @@ __global__ __launch_bounds__(256) void latent_decode_kernel(const LatentDecodeAr
         for (int u = 0; u < kAhead; ++u) ring[u] = key(u);
 #pragma unroll
         for (int u = 0; u < kUses; ++u) {
-#pragma unroll
-          for (int m = 0; m < MR; ++m) s[m][u % KT] = mma(ring[u % kAhead], qf[u / KT][m], s[m][u % KT]);
+          f32x4& to = KT == 1 && (u & 1) ? s2 : s[u % KT];
+          to = mma(ring[u % kAhead], qf[u / KT], to);
           if (u + kAhead < kUses) ring[u % kAhead] = key(u + kAhead);
           __builtin_amdgcn_sched_barrier(0);
         }
-      }
-      if constexpr (tail) {
-#pragma unroll
-        for (int m = 0; m < MR; ++m) {
-          const int seen = at.len - back[m] - block * kTile - 16 * KT * kg - 4 * g;
+        if constexpr (KT == 1) s[0] += s2;
+        if constexpr (tail) {
+          const int seen = at.len - back - block * kTile - 16 * KT * kg - 4 * g;
 #pragma unroll
           for (int e = 0; e < 4 * KT; ++e)
-            if (16 * (e >> 2) + (e & 3) >= seen) s[m][e >> 2][e & 3] = -INFINITY;
+            if (16 * (e >> 2) + (e & 3) >= seen) s[e >> 2][e & 3] = -INFINITY;
         }
+        float most = s[0][0];
+#pragma unroll
+        for (int e = 1; e < 4 * KT; ++e) most = larger(most, s[e >> 2][e & 3]);
+        most = max_over_groups(most) * c;
+        const bool outgrown = __builtin_amdgcn_ballot_w64(most > ref + kRescaleSlack) != 0;
+        if (lane == 0) sh.outgrown[w] = outgrown;
+        probabilities();
+        if (g == 0) sh.most[mine][kg][j] = most;
       }
-      float most[MR];
-      bool over = false;
-#pragma unroll
-      for (int m = 0; m < MR; ++m) {
-        float x = s[m][0][0];
-#pragma unroll
-        for (int e = 1; e < 4 * KT; ++e) x = larger(x, s[m][e >> 2][e & 3]);
-        most[m] = max_over_groups(x) * c;
-        over |= most[m] > ref[m] + kRescaleSlack;
-      }
-      const bool outgrown = __builtin_amdgcn_ballot_w64(over) != 0;
-      if (lane == 0) sh.outgrown[w] = outgrown;
-      float sum[MR];
-      auto probabilities = [&]() __attribute__((always_inline)) {
-        typedef float f32x2 __attribute__((ext_vector_type(2)));
-        typedef __attribute__((__vector_size__(4))) __bf16 bf16x2;
-#pragma unroll
-        for (int m = 0; m < MR; ++m) {
-          const float from = fmaxf(ref[m], kNoKeyYet);
-          sum[m] = 0.f;
-#pragma unroll
-          for (int kt = 0; kt < KT; ++kt) {
-            float p[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][kt][i], c, -from));
-              sum[m] += p[i];                                // (before its rounding: lse keeps 32 bits)
-            }
-            const uint32_t low = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[0], p[1]}, bf16x2));
-            const uint32_t high = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[2], p[3]}, bf16x2));
-            *reinterpret_cast<MC_LDS u32x2*>(p_write + 16 * m * S::kPRowB + kt * 32) = u32x2{low, high};
-          }
-        }
-      };
-      probabilities();
-#pragma unroll
-      for (int m = 0; m < MR; ++m)
-        if (g == 0) sh.most[m0 + m][kg][j] = most[m];
       __syncthreads();
-      if (__builtin_amdgcn_readfirstlane(sh.outgrown[0] | sh.outgrown[1] | sh.outgrown[2] | sh.outgrown[3]) != 0) {      // (the same for all waves)
+      int any = 0;
+#pragma unroll
+      for (int i = 0; i < S::kScoring; ++i) any |= sh.outgrown[i];
+      if (__builtin_amdgcn_readfirstlane(any) != 0) {        // (the same for all waves)
         auto raised = [&](int m, float from) __attribute__((always_inline)) {
           float top = from;
 #pragma unroll
@@ -276,26 +268,24 @@ __global__ __launch_bounds__(256) void latent_decode_kernel(const LatentDecodeAr
         };
         auto factor = [](float from, float to) __attribute__((always_inline)) { return to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(from - to); };
 #pragma unroll
-        for (int m = 0; m < MR; ++m) {
-          const float next = raised(m0 + m, ref[m]);
-          l[m] *= factor(ref[m], next);
-          ref[m] = next;
-        }
-#pragma unroll
         for (int m = 0; m < MT; ++m) {
           const float next = raised(m, ref_all[m]), alpha = factor(ref_all[m], next);
           ref_all[m] = next;
 #pragma unroll
           for (int t = 0; t < S::kColTiles; ++t) o[t][m] *= alpha;
         }
-        probabilities();
+        if (scoring) {
+          const float next = raised(mine, ref);
+          l *= factor(ref, next);
+          ref = next;
+          probabilities();
+        }
         __syncthreads();
       }
-#pragma unroll
-      for (int m = 0; m < MR; ++m) l[m] += sum[m];
+      l += sum;
       // output += values of this wave's columns
       {
-        constexpr int kUses = 2 * S::kColTiles, kAhead = 3;
+        constexpr int kUses = 2 * S::kColTiles, kAhead = kUses < 3 ? kUses : 3;
         bf16x8 ring[kAhead], pf[MT];
         auto value = [&](int u) __attribute__((always_inline)) {
           const int half = u / S::kColTiles, t = u % S::kColTiles;
@@ -343,10 +333,9 @@ __global__ __launch_bounds__(256) void latent_decode_kernel(const LatentDecodeAr
 
       // the row's sums over the waves' keys, then its result or its part of one
       const bool done = stop == at.blocks;
-#pragma unroll
-      for (int m = 0; m < MR; ++m) {
-        const float all = sum_with_other_half(l[m] + __shfl_xor(l[m], 16, 64));
-        if (g == 0) sh.sum[m0 + m][kg][j] = all;
+      if (scoring) {
+        const float all = sum_with_other_half(l + __shfl_xor(l, 16, 64));
+        if (g == 0) sh.sum[mine][kg][j] = all;
       }
       __syncthreads();
       const int64_t part0 = (((int64_t)tile * a.stretches + stretch) * 2 + (whole ? 1 : 0)) * S::kRows;
@@ -357,7 +346,7 @@ __global__ __launch_bounds__(256) void latent_decode_kernel(const LatentDecodeAr
         for (int i = 1; i < KG; ++i) all += sh.sum[m][i][j];
         const int row = tile * S::kRows + m * 16 + j;
         if (row >= a.stacked) continue;
-        const int col = (R / 4) * w + 4 * g;
+        const int col = (R / 8) * w + 4 * g;
         if (whole && done) {
           const float inv = all == 0.f ? 0.f : 1.0f / all;             // (a row that sees no key: 0)
           const int64_t to = (int64_t)at.row * a.stacked + row;
@@ -390,7 +379,7 @@ __global__ __launch_bounds__(256) void latent_decode_kernel(const LatentDecodeAr
   if (notes && !by_row) a.chains[stretch] = open;
 
   // padding rows, shared out over the stretches
-  for (int64_t first = stretch; first < a.batch; first += (int64_t)a.stretches * 256) {
+  for (int64_t first = stretch; first < a.batch; first += (int64_t)a.stretches * (kWaves * 64)) {
     const int64_t r = first + (int64_t)threadIdx.x * a.stretches;
     const bool empty = r < a.batch && line.valid(a.seq_lens[r]) == 0;
     if (empty && tile == 0 && by_row) a.chains[r].more = 0;
@@ -524,9 +513,9 @@ __global__ __launch_bounds__(kRowJoinThreads) void latent_join_rows_kernel(const
 template <int R>
 hipError_t enqueue(int rows, const LatentDecodeArgs& args, hipStream_t stream) {
   const int wgs = args.tiles * args.stretches;
-  if (rows == 16) latent_decode_kernel<R, 1, 1><<<wgs, 256, 0, stream>>>(args);
-  else if (rows == 32) latent_decode_kernel<R, 2, 1><<<wgs, 256, 0, stream>>>(args);
-  else if (rows == 64) latent_decode_kernel<R, 4, 2><<<wgs, 256, 0, stream>>>(args);
+  if (rows == 16) latent_decode_kernel<R, 1><<<wgs, kWaves * 64, 0, stream>>>(args);
+  else if (rows == 32) latent_decode_kernel<R, 2><<<wgs, kWaves * 64, 0, stream>>>(args);
+  else if (rows == 64) latent_decode_kernel<R, 4><<<wgs, kWaves * 64, 0, stream>>>(args);
   else return hipErrorInvalidValue;
   if (args.n_chains * args.stacked < 512) {
     latent_join_kernel<R><<<dim3(args.n_chains, args.stacked, R / kJoinCols), kJoinThreads, 0, stream>>>(args, rows);

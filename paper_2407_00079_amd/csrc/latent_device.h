@@ -11,10 +11,10 @@ static_assert(sizeof(LatentReq) == 20, "five integers");
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// two bf16 of a word, those that are not finite replaced by 0
+// two bf16 of a word, those that are not finite (exponent all ones: one more carries into the sign's place) replaced by 0
 __device__ __forceinline__ uint32_t finite_pair(uint32_t x) {
-  const uint32_t low = (x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu, high = (x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u;
-  return low | high;
+  const uint32_t odd = ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+  return x & ~(odd | (odd - (odd >> 15)));
 }
 
 // The last request whose field FIELD (a running sum) is not past x: 64 entries at a time, the same for all lanes of a wave.  (Of
