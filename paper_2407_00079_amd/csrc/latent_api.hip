@@ -5,22 +5,25 @@
 #include "host_plan.h"
 #include "latent_internal.h"
 #include "latent_plan.h"
-#include "mc_internal.h"
 
 namespace {
 
 using namespace mc::host;
 
-// The request table of a call: in `arg` if it fits, else uploaded to the workspace.  *items: its work items of `rows` rows each.
-mc_status place_latent(const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, int32_t rows, void* workspace, hipStream_t stream,
-                       mc::LatentReqTable* arg, int64_t* items) {
+// The request table of a call: in `arg` if it fits, else uploaded to the workspace.  most_tiles: -1, or how attention's work items are cut.
+mc_status place_latent(const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, int32_t most_tiles, void* workspace, hipStream_t stream,
+                       mc::LatentReqTable* arg) {
+  auto fill = [&](mc::LatentReq* to) {
+    fill_latent_table(prefix_lens, new_lens, batch, to);
+    if (most_tiles >= 0) fill_latent_items(batch, most_tiles, to);
+  };
   if (batch <= mc::kMaxArgEntries) {
-    *items = fill_latent_table(prefix_lens, new_lens, batch, rows, arg->r);
+    fill(arg->r);
     return MC_OK;
   }
   try {
     std::vector<mc::LatentReq> reqs((size_t)batch);
-    *items = fill_latent_table(prefix_lens, new_lens, batch, rows, reqs.data());
+    fill(reqs.data());
     return mc::upload_table(workspace, reqs.data(), sizeof(mc::LatentReq) * reqs.size(), stream);
   } catch (const std::bad_alloc&) {
     return MC_ERR_HIP;
@@ -75,8 +78,7 @@ mc_status mc_latent_append_paged(const mc_latent_params* p, const mc_rope_params
 
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   mc::LatentReqTable arg = {};
-  int64_t items = 0;
-  st = place_latent(prefix_lens, new_lens, batch, 1, workspace, stream, &arg, &items);
+  st = place_latent(prefix_lens, new_lens, batch, -1, workspace, stream, &arg);
   if (st != MC_OK) return st;
   const mc::LatentAppendArgs args = append_args(p, rope, q, kv, s, norm, q_out, pool, block_tables, max_pages_per_req, lens.total_new);
   return mc::launch_latent_append(args, reinterpret_cast<const mc::LatentReq*>(workspace), batch <= mc::kMaxArgEntries ? &arg : nullptr, batch,
@@ -164,8 +166,7 @@ mc_status mc_latent_expand_paged(const mc_latent_params* p, const void* weight, 
 
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   mc::LatentReqTable arg = {};
-  int64_t items = 0;
-  st = place_latent(nullptr, lens, batch, 1, workspace, stream, &arg, &items);
+  st = place_latent(nullptr, lens, batch, -1, workspace, stream, &arg);
   if (st != MC_OK) return st;
   return mc::launch_latent_expand(args, reinterpret_cast<const mc::LatentReq*>(workspace), batch <= mc::kMaxArgEntries ? &arg : nullptr, stream) == hipSuccess
              ? MC_OK
@@ -176,7 +177,7 @@ size_t mc_latent_prefill_attn_workspace_bytes(const mc_latent_params* p, const i
   LatentLens lens;
   if (check_latent(p) != MC_OK || batch < 0 || (batch > 0 && (prefix_lens == nullptr || new_lens == nullptr))) return 0;
   if (check_latent_lens(prefix_lens, new_lens, batch, &lens) != MC_OK) return 0;
-  return latent_prefill_layout(p, prefix_lens, new_lens, batch, lens).total;
+  return latent_prefill_layout(p, prefix_lens, new_lens, batch).total;
 }
 
 mc_status mc_latent_prefill_attn_paged(const mc_latent_params* p, const void* q, const void* k, const void* v, const int64_t* strides,
@@ -201,29 +202,24 @@ mc_status mc_latent_prefill_attn_paged(const mc_latent_params* p, const void* q,
   for (const void* at : {q, k, v, pool, (const void*)out, (const void*)workspace})
     if (!aligned16(at)) return MC_ERR_ALIGN;
   if (!aligned4(block_tables) || !aligned4(lse)) return MC_ERR_ALIGN;
-  const LatentPrefillLayout lay = latent_prefill_layout(p, prefix_lens, new_lens, batch, lens);
-  if ((int64_t)batch * max_pages_per_req > INT32_MAX || lay.items * p->num_heads * lay.kv_splits > INT32_MAX) return MC_ERR_RANGE;
+  const LatentPrefillLayout lay = latent_prefill_layout(p, prefix_lens, new_lens, batch);
+  if ((int64_t)batch * max_pages_per_req > INT32_MAX || lay.items * p->num_heads > INT32_MAX) return MC_ERR_RANGE;
   if (workspace == nullptr || workspace_bytes < lay.total) return MC_ERR_WORKSPACE;
 
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   mc::LatentReqTable arg = {};
-  int64_t items = 0;
-  st = place_latent(prefix_lens, new_lens, batch, mc::kLatentRows, workspace, stream, &arg, &items);
+  st = place_latent(prefix_lens, new_lens, batch, lay.most_tiles, workspace, stream, &arg);
   if (st != MC_OK) return st;
   char* const ws = reinterpret_cast<char*>(workspace);
   mc::LatentPrefillArgs args = {};
   args.q = q, args.k = k, args.v = v, args.pool = pool, args.block_tables = block_tables, args.out = out, args.lse = lse;
   args.o_parts = reinterpret_cast<float*>(ws + lay.o_off);
-  args.lse_parts = reinterpret_cast<float*>(ws + lay.lse_off);
+  args.ml_parts = reinterpret_cast<float2*>(ws + lay.ml_off);
   args.k_token = 2 * s.k_token, args.k_head = 2 * s.k_head, args.v_token = 2 * s.v_token, args.v_head = 2 * s.v_head;
-  args.rows_total = lens.total_new * p->num_heads;
   args.heads = p->num_heads, args.head_dim = p->head_dim, args.latent_dim = p->latent_dim, args.batch = batch, args.max_pages = max_pages_per_req;
-  args.kv_splits = lay.kv_splits, args.items = (int32_t)items;
+  args.most_tiles = lay.most_tiles, args.items = (int32_t)lay.items;
   args.scale_log2e = latent_scale_log2e(p);
-  if (mc::launch_latent_prefill(args, reinterpret_cast<const mc::LatentReq*>(workspace), batch <= mc::kMaxArgEntries ? &arg : nullptr, stream) != hipSuccess)
-    return MC_ERR_HIP;
-  if (lay.kv_splits == 1) return MC_OK;
-  return mc::launch_attn_merge(MC_DTYPE_BF16, p->head_dim, args.o_parts, args.lse_parts, lay.kv_splits, args.rows_total, out, lse, stream) == hipSuccess
+  return mc::launch_latent_prefill(args, reinterpret_cast<const mc::LatentReq*>(workspace), batch <= mc::kMaxArgEntries ? &arg : nullptr, stream) == hipSuccess
              ? MC_OK
              : MC_ERR_HIP;
 }

@@ -59,9 +59,9 @@ __global__ __launch_bounds__(kThreads) void latent_expand_kernel(const LatentExp
       int l = lo, h = hi;
       while (l < h) {
         const int mid = (l + h + 1) >> 1;
-        if (ints[5 * (int64_t)mid + 1] <= tok) l = mid; else h = mid - 1;
+        if (ints[7 * (int64_t)mid + 1] <= tok) l = mid; else h = mid - 1;
       }
-      const int pos = tok - ints[5 * (int64_t)l + 1];
+      const int pos = tok - ints[7 * (int64_t)l + 1];
       const int64_t page = a.block_tables[(int64_t)l * a.max_pages + pos / kPageTokens];
       from[i] = reinterpret_cast<const char*>(a.pool) + (page * kPageTokens + pos % kPageTokens) * kRowB + ((lane % 8 ^ token_swizzle(row)) << 4);
       const int out = out0 + row < a.outs ? row : a.outs - 1 - out0;

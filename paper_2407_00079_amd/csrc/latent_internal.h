@@ -54,10 +54,11 @@ struct LatentPrefillArgs {
   const int32_t* block_tables;
   void* out;
   float* lse;
-  float *o_parts, *lse_parts;                // kv_splits > 1: [kv_splits][rows][head_dim], [kv_splits][rows]
+  float* o_parts;                            // most_tiles > 0: rows of partial results, [rows][heads][head_dim]
+  float2* ml_parts;                          // their references and sums
   int64_t k_token, k_head, v_token, v_head;  // bytes
-  int64_t rows_total;                        // total new tokens * heads
-  int32_t heads, head_dim, latent_dim, batch, max_pages, kv_splits, items;
+  int32_t heads, head_dim, latent_dim, batch, max_pages, items;
+  int32_t most_tiles;                        // key tiles of a piece at most; 0: row tiles are whole
   float scale_log2e;
 };
 hipError_t launch_latent_prefill(const LatentPrefillArgs& args, const LatentReq* reqs, const LatentReqTable* arg, hipStream_t stream);

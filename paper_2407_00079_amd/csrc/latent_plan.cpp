@@ -94,16 +94,31 @@ mc_status check_latent_lens(const int32_t* prefix_lens, const int32_t* new_lens,
 
 size_t latent_table_bytes(int32_t batch) { return ((size_t)batch * sizeof(LatentReq) + 15) & ~(size_t)15; }
 
-int64_t fill_latent_table(const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, int32_t rows_per_item, LatentReq* to) {
-  int64_t q_off = 0, k_off = 0, items = 0;
+void fill_latent_table(const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, LatentReq* to) {
+  int64_t q_off = 0, k_off = 0;
   for (int32_t r = 0; r < batch; ++r) {
     const int32_t before = prefix_lens != nullptr ? prefix_lens[r] : 0;
-    to[r] = {(int32_t)q_off, (int32_t)k_off, before, new_lens[r], (int32_t)items};
+    to[r] = {(int32_t)q_off, (int32_t)k_off, before, new_lens[r], 0, 0, r};
     q_off += new_lens[r];
     k_off += (int64_t)before + new_lens[r];
-    items += ((int64_t)new_lens[r] + rows_per_item - 1) / rows_per_item;
   }
-  return items;
+}
+
+void fill_latent_items(int32_t batch, int32_t most_tiles, LatentReq* reqs) {
+  std::stable_sort(reqs, reqs + batch, [](const LatentReq& a, const LatentReq& b) { return (int64_t)a.prefix + a.chunk > (int64_t)b.prefix + b.chunk; });
+  int64_t items = 0, parts = 0;
+  for (int32_t r = 0; r < batch; ++r) {
+    const int32_t tiles = latent_row_tiles(reqs[r].chunk);
+    reqs[r].item_off = (int32_t)items;
+    reqs[r].part_off = (int32_t)parts;
+    if (most_tiles == 0) items += tiles;
+    else
+      for (int32_t t = 0; t < tiles; ++t) {
+        const int pieces = latent_pieces(latent_key_tiles(reqs[r].prefix, reqs[r].chunk, t), most_tiles);
+        items += pieces;
+        parts += pieces > 1 ? (int64_t)pieces * latent_tile_height(reqs[r].chunk, t) : 0;
+      }
+  }
 }
 
 LatentDecodeLayout latent_decode_layout(const mc_latent_params* p, int32_t batch, int32_t tokens) {
@@ -120,18 +135,66 @@ LatentDecodeLayout latent_decode_layout(const mc_latent_params* p, int32_t batch
   return l;
 }
 
-LatentPrefillLayout latent_prefill_layout(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch,
-                                          const LatentLens& lens) {
+namespace {
+// us of a tile of keys, of a workgroup's beginning and end, and of joining, as measured (latent_prefill.hip)
+struct PrefillTimes {
+  double tile, row, ends, join, part_byte;
+};
+PrefillTimes times_of(const mc_latent_params* p) {
+  return p->head_dim == 128 ? PrefillTimes{0.9, 1.14 / kLatentRows, 5.0, 4.0, 1.0 / 2.0e6} : PrefillTimes{0.8, 0.6 / kLatentRows, 4.0, 4.0, 1.0 / 2.0e6};
+}
+struct PrefillCut {
+  int64_t items, part_rows;
+  int64_t most;                              // key tiles of a piece
+  double us;
+};
+PrefillCut cut_into(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, int32_t most_tiles) {
+  const PrefillTimes t = times_of(p);
+  PrefillCut cut = {0, 0, 0, 0};
+  double all = 0, longest = 0;
+  for (int32_t r = 0; r < batch; ++r)
+    for (int32_t i = 0, n = latent_row_tiles(new_lens[r]); i < n; ++i) {
+      const int keys = latent_key_tiles(prefix_lens[r], new_lens[r], i), pieces = latent_pieces(keys, most_tiles), rows = latent_tile_height(new_lens[r], i);
+      const int each = (keys + pieces - 1) / pieces;
+      cut.items += pieces;
+      cut.part_rows += pieces > 1 ? (int64_t)pieces * rows : 0;
+      cut.most = std::max<int64_t>(cut.most, each);
+      const double tile = t.tile + t.row * rows;
+      all += keys * tile + pieces * t.ends;
+      longest = std::max(longest, each * tile + t.ends);
+    }
+  const double wgs = (double)cut.items * p->num_heads, mean = wgs > 0 ? all * p->num_heads / wgs : 0;
+  // (the last workgroups to start end half a mean one apart)
+  cut.us = std::max(longest, all * p->num_heads / 256 + (wgs > 256 ? 0.5 * mean : 0.0));
+  if (wgs <= 256) cut.us = longest;
+  if (cut.part_rows > 0) cut.us += t.join + (double)cut.part_rows * p->num_heads * p->head_dim * 4 * t.part_byte;
+  return cut;
+}
+}  // namespace
+
+LatentPrefillLayout latent_prefill_layout(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch) {
   LatentPrefillLayout l = {};
-  (void)prefix_lens;
-  for (int32_t r = 0; r < batch; ++r) l.items += ((int64_t)new_lens[r] + kLatentRows - 1) / kLatentRows;
-  // Key slices where whole rows leave compute units idle: as many as fill them twice over, each of 8 tiles of 64 keys at least.
-  const int64_t wgs = l.items * p->num_heads, most = std::max(1, lens.most_keys / (8 * 64));
-  l.kv_splits = wgs == 0 || wgs >= 256 ? 1 : (int32_t)std::min<int64_t>({(512 + wgs - 1) / wgs, most, MC_MAX_KV_SPLITS});
+  for (int32_t r = 0; r < batch; ++r) l.items += latent_row_tiles(new_lens[r]);
+  // From eight rounds of workgroups on, whole row tiles keep the compute units busy to the end.
+  if (l.items * p->num_heads < 8 * 256) {
+    PrefillCut best = cut_into(p, prefix_lens, new_lens, batch, 0);
+    const int64_t longest = best.most;
+    for (const int parts : {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+      const int32_t most = (int32_t)((longest + parts - 1) / parts);
+      if (most < 4) break;
+      const PrefillCut cut = cut_into(p, prefix_lens, new_lens, batch, most);
+      if (cut.us < 0.97 * best.us) {
+        best = cut;
+        l.most_tiles = most;
+      }
+    }
+    l.items = best.items;
+    l.part_rows = best.part_rows;
+  }
   l.o_off = round_up(latent_table_bytes(batch));
-  const size_t rows = l.kv_splits > 1 ? (size_t)l.kv_splits * (size_t)lens.total_new * p->num_heads : 0;
-  l.lse_off = l.o_off + round_up(rows * p->head_dim * sizeof(float));
-  l.total = l.lse_off + round_up(rows * sizeof(float)) + 256;
+  const size_t rows = (size_t)l.part_rows * (size_t)p->num_heads;
+  l.ml_off = l.o_off + round_up(rows * p->head_dim * sizeof(float));
+  l.total = l.ml_off + round_up(rows * 2 * sizeof(float)) + 256;
   return l;
 }
 

@@ -31,8 +31,10 @@ struct LatentLens {
 mc_status check_latent_lens(const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, LatentLens* out);
 
 size_t latent_table_bytes(int32_t batch);
-// The request table; work items: `items_per(chunk)` of each request, one after another.  Returns their number.
-int64_t fill_latent_table(const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, int32_t rows_per_item, LatentReq* to);
+// The request table; and with the work items of expanded attention whose pieces have at most most_tiles key tiles (0: whole), the requests of most
+// keys first, so that what starts last is short.
+void fill_latent_table(const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, LatentReq* to);
+void fill_latent_items(int32_t batch, int32_t most_tiles, LatentReq* reqs);
 
 // Where the parts of an absorbed attention call lie in its workspace.
 struct LatentDecodeLayout {
@@ -41,14 +43,13 @@ struct LatentDecodeLayout {
 };
 LatentDecodeLayout latent_decode_layout(const mc_latent_params* p, int32_t batch, int32_t tokens);
 
-// Expanded attention: key slices (1: whole rows) and where partial results lie.
+// Expanded attention: how row tiles are cut along the keys, and where partial results lie.
 struct LatentPrefillLayout {
-  int32_t kv_splits;
-  int64_t items;                             // (request, tile of query rows)
-  size_t o_off, lse_off, total;
+  int32_t most_tiles;                        // key tiles of a piece at most; 0: nothing is cut
+  int64_t items, part_rows;                  // pieces of row tiles; rows of partial results of each head
+  size_t o_off, ml_off, total;
 };
-LatentPrefillLayout latent_prefill_layout(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch,
-                                          const LatentLens& lens);
+LatentPrefillLayout latent_prefill_layout(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch);
 struct KeyStrides {
   int64_t k_token, k_head, v_token, v_head;
 };

@@ -50,7 +50,36 @@ __device__ __forceinline__ uint32_t rounded_pair(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
-template <int D, bool SPLIT, typename Table>
+// A work item: which piece of which row tile.
+struct Item {
+  int req, row_tile, piece, pieces;
+  int64_t part_row;                          // the row tile's first row of partial results (pieces > 1)
+  LatentReq rq;
+};
+template <bool CUT, typename Table>
+__device__ __forceinline__ Item item_of(const LatentPrefillArgs& a, const Table& table, int item) {
+  Item it;
+  it.req = find_request<4>(table.ints(), table.batch, item);
+  it.rq = request(table, it.req);
+  it.row_tile = latent_row_tiles(it.rq.chunk) - 1;
+  it.part_row = it.rq.part_off;
+  it.pieces = 1;
+  it.piece = item - it.rq.item_off;
+  if constexpr (CUT) {
+    for (;; --it.row_tile) {
+      it.pieces = latent_pieces(latent_key_tiles(it.rq.prefix, it.rq.chunk, it.row_tile), a.most_tiles);
+      if (it.piece < it.pieces) break;
+      it.piece -= it.pieces;
+      if (it.pieces > 1) it.part_row += it.pieces * latent_tile_height(it.rq.chunk, it.row_tile);
+    }
+  } else {
+    it.row_tile -= it.piece;
+    it.piece = 0;
+  }
+  return it;
+}
+
+template <int D, bool CUT, typename Table>
 __global__ __launch_bounds__(512) void latent_prefill_kernel(const LatentPrefillArgs a, const Table table) {
   constexpr int kRowB = D * 2, kSteps = D / 32, kRopeSteps = kLatentRope / 32, kDTiles = D / 16, kQRowB = (D + kLatentRope) * 2;
   constexpr int kKeyB = kTile * kRowB, kRopeB = kTile * 128;
@@ -62,20 +91,13 @@ __global__ __launch_bounds__(512) void latent_prefill_kernel(const LatentPrefill
   const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  // heads fastest (consecutive workgroups land on different XCDs, so an XCD keeps the streams of few heads), then key slices, then row
-  // tiles, of a request from the last one (most keys) down
-  const int head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads, slice = SPLIT ? rest % a.kv_splits : 0, item = SPLIT ? rest / a.kv_splits : rest;
-  const int req = find_request<4>(table.ints(), table.batch, item);
-  const LatentReq rq = request(table, req);
-  const int row_tile = (rq.chunk - 1) / kLatentRows - (item - rq.item_off);
-  const int row0 = row_tile * kLatentRows, P = rq.prefix, L = rq.prefix + rq.chunk;
-  const int last_row = row0 + kLatentRows < rq.chunk ? row0 + kLatentRows - 1 : rq.chunk - 1;
-  int tiles = (P + last_row) / kTile + 1, t_lo = 0;
-  if (SPLIT) {
-    const int per = ((L + kTile - 1) / kTile + a.kv_splits - 1) / a.kv_splits;
-    t_lo = slice * per;
-    tiles = tiles < t_lo + per ? tiles : t_lo + per;
-  }
+  // heads fastest: consecutive workgroups land on different XCDs, so an XCD keeps the streams of few heads
+  const int head = blockIdx.x % a.heads;
+  const Item it = item_of<CUT>(a, table, blockIdx.x / a.heads);
+  const LatentReq rq = it.rq;
+  const int req = rq.row, row0 = it.row_tile * kLatentRows, P = rq.prefix, L = rq.prefix + rq.chunk;
+  int tiles = latent_key_tiles(P, rq.chunk, it.row_tile), t_lo = 0;
+  if (CUT) piece_tiles(tiles, it.piece, it.pieces, &t_lo, &tiles);
   const int n_free = (P + row0 + 1) / kTile;                 // every row sees every key of these tiles
 
   int64_t out_row[2];
@@ -220,18 +242,58 @@ __global__ __launch_bounds__(512) void latent_prefill_kernel(const LatentPrefill
     for (int k = 0; k < 4; ++k) w[k] = rounded_pair(s.get(rt, 2 * k), s.get(rt, 2 * k + 1));
   };
 
-  // ---- one block start to finish, for those that may reach the diagonal
-  auto plain_block = [&](int tile, int buf, int kb) __attribute__((always_inline)) {
+  // ---- one block start to finish, near the diagonal (fragments a few uses ahead: there are not the registers for more)
+  auto plain_block = [&](int tile, int buf, int kb, auto masked) __attribute__((always_inline)) {
+    constexpr bool kMasked = decltype(masked)::value != 0;
     const int key0 = tile * kTile + kb * 32;
-    if (key0 > wave_limit) return;
+    // (addresses made here, not kept for all of the loop)
+    uint32_t k_at = k_lane, r_at = r_lane, v_at = v_lane;
+    asm volatile("" : "+v"(k_at), "+v"(r_at), "+v"(v_at));
+    k_at += buf * kKeyB + kb * 32 * kRowB;
+    r_at += buf * kRopeB + kb * 32 * 128;
+    v_at += buf * kKeyB + kb * 32 * kRowB;
+    auto key = [&](int u) __attribute__((always_inline)) {
+      const int st = u >> 1, row = (u & 1) * 16;
+      const uint32_t at = st < kSteps ? (k_at ^ (st << 6)) + row * kRowB : (r_at ^ ((st - kSteps) << 6)) + row * 128;
+      return *reinterpret_cast<MC_LDS const bf16x8*>(at);
+    };
+    auto value = [&](int dt) __attribute__((always_inline)) {
+      const uint32_t at = v_at ^ (dt << 5);
+      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((MC_LDS bf16x4*)(uintptr_t)at);
+      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((MC_LDS bf16x4*)(uintptr_t)(at + 16 * kRowB));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
     Scores s;
-    scores_of(buf, kb, s);
+    s.zero();
+    {
+      constexpr int kAhead = 6;
+      bf16x8 kf[kAhead];
 #pragma unroll
-    for (int rt = 0; rt < 2; ++rt) {
-      const int seen = limit[rt] - key0 - 4 * g;
+      for (int u = 0; u < kAhead; ++u) kf[u] = key(u);
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (16 * (e >> 2) + (e & 3) > seen) s.set(rt, e, -INFINITY);
+      for (int u = 0; u < kK; ++u) {
+#pragma unroll
+        for (int rt = 0; rt < 2; ++rt) s.t[rt][u & 1] = mma(kf[u % kAhead], qf[u >> 1][rt], s.t[rt][u & 1]);
+        if (u + kAhead < kK) kf[u % kAhead] = key(u + kAhead);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    uint32_t exponents = 0;
+    if constexpr (kMasked) {
+#pragma unroll
+      for (int dt = 0; dt < kDTiles; ++dt) {                 // (all ones, and one more: the bit above)
+        const u32x4 x = __builtin_bit_cast(u32x4, value(dt));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) exponents |= (x[i] & 0x7f807f80u) + 0x00800080u;
+        if (dt % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int rt = 0; rt < 2; ++rt) {
+        const int seen = limit[rt] - key0 - 4 * g;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (16 * (e >> 2) + (e & 3) > seen) s.set(rt, e, -INFINITY);
+      }
     }
     settle(s);
     u32x4 w[2];
@@ -241,42 +303,58 @@ __global__ __launch_bounds__(512) void latent_prefill_kernel(const LatentPrefill
       probabilities(s, rt, w[rt], sum[rt]);
       l[rt] += sum[rt];
     }
-    uint32_t odd = 0;
+    auto values = [&](auto clean) __attribute__((always_inline)) {
+      constexpr int kAhead = 4;
+      bf16x8 vf[kAhead];
 #pragma unroll
-    for (int dt = 0; dt < kDTiles; ++dt) {
-      u32x4 bits = __builtin_bit_cast(u32x4, load_v(buf, kb, dt));
+      for (int dt = 0; dt < kAhead; ++dt) vf[dt] = value(dt);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t clean = finite_pair(bits[i]);
-        odd |= clean ^ bits[i];
-        bits[i] = clean;
+      for (int dt = 0; dt < kDTiles; ++dt) {
+        bf16x8 v = vf[dt % kAhead];
+        if constexpr (decltype(clean)::value != 0) {
+          u32x4 x = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] = finite_pair(x[i]);
+          v = __builtin_bit_cast(bf16x8, x);
+        }
+#pragma unroll
+        for (int rt = 0; rt < 2; ++rt) o[dt][rt] = mma(v, __builtin_bit_cast(bf16x8, w[rt]), o[dt][rt]);
+        if (dt + kAhead < kDTiles) vf[dt % kAhead] = value(dt + kAhead);
+        __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-      for (int rt = 0; rt < 2; ++rt) o[dt][rt] = mma(__builtin_bit_cast(bf16x8, bits), __builtin_bit_cast(bf16x8, w[rt]), o[dt][rt]);
+    };
+    if (!kMasked || __builtin_expect(__builtin_amdgcn_ballot_w64((exponents & 0x80008000u) != 0) == 0, 1)) {
+      values(Int<0>{});
+      return;
     }
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd != 0) == 0, 1)) return;
-    // V has elements that are not finite: each for the rows that see its key
+    values(Int<1>{});
+    // V has elements that are not finite: a row that sees some in a column gets their sum there.  Counted by a product: +inf as 1, -inf as 64, NaN
+    // as 4096 of at most 32 keys, times 1 for keys that the row sees.
+    bf16x8 sees[2];
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt)
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-#pragma nounroll
-        for (int from = 0; from < 4; ++from) {               // keys of lane group `from`
-          const int row = kb * 32 + (e >> 2) * 16 + 4 * from + (e & 3);
-          const float p = __shfl(s.get(rt, e), from * 16 + j, 64);
-          if (tile * kTile + row > limit[rt]) continue;
+      for (int e = 0; e < 8; ++e) sees[rt][e] = 16 * (e >> 2) + (e & 3) <= limit[rt] - key0 - 4 * g ? (__bf16)1.0f : (__bf16)0.0f;
 #pragma unroll
-          for (int dt = 0; dt < kDTiles; ++dt) {
-            const int byte = (16 * dt + 4 * g) * 2;
-            const uint32_t at = base + kValueBase + buf * kKeyB + row * kRowB + (((byte >> 4) ^ Row::value(row)) << 4) + (byte & 8);
-            const u32x2 v = *reinterpret_cast<MC_LDS const u32x2*>(at);
+    for (int dt = 0; dt < kDTiles; ++dt) {
+      const u32x4 x = __builtin_bit_cast(u32x4, value(dt));
+      bf16x8 kind;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const uint32_t bits = r & 1 ? v[r >> 1] & 0xffff0000u : v[r >> 1] << 16;
-              if ((bits & 0x7f800000u) == 0x7f800000u) o[dt][rt][r] += p * __builtin_bit_cast(float, bits);
-            }
-          }
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t bits = e & 1 ? x[e >> 1] >> 16 : x[e >> 1] & 0xffffu;
+        kind[e] = (__bf16)((bits & 0x7f80u) != 0x7f80u ? 0.f : bits == 0x7f80u ? 1.f : bits == 0xff80u ? 64.f : 4096.f);
+      }
+#pragma unroll
+      for (int rt = 0; rt < 2; ++rt) {
+        const f32x4 n = mma(kind, sees[rt], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int k = (int)n[r];
+          o[dt][rt][r] += k == 0 ? 0.f : k < 64 ? INFINITY : k < 4096 && k % 64 == 0 ? -INFINITY : NAN;
         }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
 
   // ---- the loop over tiles that every row sees: a software pipeline over blocks of 32 keys.  Phase A makes the scores of the next block while the
@@ -346,12 +424,17 @@ __global__ __launch_bounds__(512) void latent_prefill_kernel(const LatentPrefill
     __syncthreads();
     if (tile + 2 < tiles) fetch(tile + 2, buf == 0 ? kBufs - 1 : buf - 1);
   };
-  int tile = t_lo;
-  if (t_lo < tiles) {
-    fetch(t_lo, 0);
-    if (t_lo + 1 < tiles) fetch(t_lo + 1, 1);
-    __builtin_amdgcn_s_waitcnt(0x0F70 | 0);
-    __syncthreads();
+  int tile = t_lo;                                           // (every piece has a tile)
+  fetch(t_lo, 0);
+  if (t_lo + 1 < tiles) fetch(t_lo + 1, 1);
+  __builtin_amdgcn_s_waitcnt(0x0F70);
+  __syncthreads();
+  if (row0 + wave * 32 >= rq.chunk) {                        // a wave without rows only copies
+    for (; tile < tiles; ++tile) {
+      tile_sync(tile);
+      buf = buf == kBufs - 1 ? 0 : buf + 1;
+    }
+    return;
   }
   const int n_plain = n_free < tiles - 1 ? n_free : tiles - 1;
   if (tile < n_plain) {
@@ -385,8 +468,13 @@ __global__ __launch_bounds__(512) void latent_prefill_kernel(const LatentPrefill
   }
   for (; tile < tiles; ++tile) {
     tile_sync(tile);
-    plain_block(tile, buf, 0);
-    plain_block(tile, buf, 1);
+#pragma nounroll
+    for (int kb = 0; kb < 2; ++kb) {
+      const int key0 = tile * kTile + kb * 32;
+      if (key0 > wave_limit) continue;                       // (no row of the wave sees any of it)
+      if (key0 + 31 <= wave_limit - 31) plain_block(tile, buf, kb, Int<0>{});
+      else plain_block(tile, buf, kb, Int<1>{});
+    }
     buf = buf == kBufs - 1 ? 0 : buf + 1;
   }
 
@@ -394,37 +482,90 @@ __global__ __launch_bounds__(512) void latent_prefill_kernel(const LatentPrefill
   for (int rt = 0; rt < 2; ++rt) {
     const float all = sum_with_other_half(l[rt] + __shfl_xor(l[rt], 16, 64));
     if (!live[rt]) continue;
-    const bool none = all == 0.f;                            // (a slice of the keys that the row sees nothing of)
-    const float inv = none ? 0.f : 1.0f / all, lse = none ? -INFINITY : (m[rt] + __builtin_amdgcn_logf(all)) * 0.6931471805599453f;
-    if constexpr (SPLIT) {
-      const int64_t to = slice * a.rows_total + out_row[rt];
+    if (CUT && it.pieces > 1) {
+      const int64_t to = (it.part_row + (int64_t)it.piece * latent_tile_height(rq.chunk, it.row_tile) + wave * 32 + rt * 16 + j) * a.heads + head;
 #pragma unroll
-      for (int dt = 0; dt < kDTiles; ++dt) *reinterpret_cast<f32x4*>(a.o_parts + to * D + 16 * dt + 4 * g) = o[dt][rt] * inv;
-      if (g == 0) a.lse_parts[to] = lse;
-    } else {
-#pragma unroll
-      for (int dt = 0; dt < kDTiles; ++dt) {
-        bf16x4 v;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = (__bf16)(o[dt][rt][r] * inv);
-        *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(a.out) + out_row[rt] * D + 16 * dt + 4 * g) = v;
-      }
-      if (a.lse != nullptr && g == 0) a.lse[out_row[rt]] = lse;
+      for (int dt = 0; dt < kDTiles; ++dt) *reinterpret_cast<f32x4*>(a.o_parts + to * D + 16 * dt + 4 * g) = o[dt][rt];
+      if (g == 0) a.ml_parts[to] = float2{m[rt], all};
+      continue;
     }
+    const float inv = 1.0f / all;                            // (a row sees its own key at least)
+#pragma unroll
+    for (int dt = 0; dt < kDTiles; ++dt) {
+      bf16x4 v;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] = (__bf16)(o[dt][rt][r] * inv);
+      *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(a.out) + out_row[rt] * D + 16 * dt + 4 * g) = v;
+    }
+    if (a.lse != nullptr && g == 0) a.lse[out_row[rt]] = (m[rt] + __builtin_amdgcn_logf(all)) * 0.6931471805599453f;
   }
 }
 
+// Row tiles that were cut: a workgroup joins 32 rows of one head, 8 lanes a row.
+constexpr int kJoinRows = 32;
+template <int D, typename Table>
+__global__ __launch_bounds__(kJoinRows * 8) void latent_prefill_join_kernel(const LatentPrefillArgs a, const Table table) {
+  constexpr int kPer = D / 8, kVecs = kPer / 4, kAtOnce = 4;
+  const int head = blockIdx.x % a.heads;
+  const Item it = item_of<true>(a, table, blockIdx.x / a.heads);
+  const int rows = latent_tile_height(it.rq.chunk, it.row_tile), row = blockIdx.y * kJoinRows + threadIdx.x / 8, col = threadIdx.x % 8 * 4;
+  if (it.pieces == 1 || it.piece != 0 || row >= rows) return;
+  auto part = [&](int i) __attribute__((always_inline)) { return (it.part_row + (int64_t)i * rows + row) * a.heads + head; };
+  float top = -INFINITY;
+  for (int i = 0; i < it.pieces; ++i) top = fmaxf(top, a.ml_parts[part(i)].x);
+  const float from = top == -INFINITY ? 0.f : top;           // (every score is -inf or NaN)
+  float l = 0.f;
+  f32x4 x[kVecs];
+#pragma unroll
+  for (int v = 0; v < kVecs; ++v) x[v] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int i0 = 0; i0 < it.pieces; i0 += kAtOnce) {
+    f32x4 o[kAtOnce][kVecs];
+    float2 ml[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int64_t at = part(i0 + k < it.pieces ? i0 + k : i0);
+      ml[k] = a.ml_parts[at];
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v) o[k][v] = *reinterpret_cast<const f32x4*>(a.o_parts + at * D + col + 32 * v);
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k)
+      if (i0 + k < it.pieces) {
+        const float weight = __builtin_amdgcn_exp2f(ml[k].x - from);
+        l += weight * ml[k].y;
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) x[v] += weight * o[k][v];
+      }
+  }
+  const int64_t to = (int64_t)(it.rq.q_off + it.row_tile * kLatentRows + row) * a.heads + head;
+  const float inv = 1.0f / l;
+#pragma unroll
+  for (int v = 0; v < kVecs; ++v) {
+    bf16x4 y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = (__bf16)(x[v][i] * inv);
+    *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(a.out) + to * D + col + 32 * v) = y;
+  }
+  if (a.lse != nullptr && col == 0) a.lse[to] = (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+template <int D, typename Table>
+hipError_t enqueue(const LatentPrefillArgs& args, const Table& table, hipStream_t stream) {
+  const int wgs = args.items * args.heads;
+  if (args.most_tiles == 0) {
+    latent_prefill_kernel<D, false><<<wgs, 512, 0, stream>>>(args, table);
+  } else {
+    latent_prefill_kernel<D, true><<<wgs, 512, 0, stream>>>(args, table);
+    latent_prefill_join_kernel<D><<<dim3(wgs, kLatentRows / kJoinRows), kJoinRows * 8, 0, stream>>>(args, table);
+  }
+  return hipGetLastError();
+}
 template <typename Table>
 hipError_t launch(const LatentPrefillArgs& args, const Table& table, hipStream_t stream) {
   (void)hipGetLastError();
-  const int wgs = args.items * args.heads * args.kv_splits;
-  const bool split = args.kv_splits > 1;
-  if (args.head_dim == 128 && split) latent_prefill_kernel<128, true><<<wgs, 512, 0, stream>>>(args, table);
-  else if (args.head_dim == 128) latent_prefill_kernel<128, false><<<wgs, 512, 0, stream>>>(args, table);
-  else if (args.head_dim == 64 && split) latent_prefill_kernel<64, true><<<wgs, 512, 0, stream>>>(args, table);
-  else if (args.head_dim == 64) latent_prefill_kernel<64, false><<<wgs, 512, 0, stream>>>(args, table);
-  else return hipErrorInvalidValue;
-  return hipGetLastError();
+  if (args.head_dim == 128) return enqueue<128>(args, table, stream);
+  if (args.head_dim == 64) return enqueue<64>(args, table, stream);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace

@@ -16,6 +16,8 @@ struct LatentReq {
   int32_t k_off;                             // its first token in the expanded keys and values
   int32_t prefix, chunk;
   int32_t item_off;                          // its first work item
+  int32_t part_off;                          // its first row of partial results
+  int32_t row;                               // of the block table
 };
 // at most kMaxArgEntries requests travel with the launch, behind them entries that no search ends at
 struct LatentReqTable {
@@ -43,8 +45,18 @@ struct LatentChain {
   int32_t row, first, more, pad;
 };
 
-// Expanded attention: query rows and keys of a tile
+// Expanded attention: query rows of a tile; the key tiles that a row tile sees are cut into equal pieces of at most `most` each (0: one piece).
+// Work items of a request: row tiles from the last one (most keys) down, the pieces of each.
 constexpr int kLatentRows = 256;
+constexpr int latent_key_tiles(int prefix, int chunk, int row_tile) {
+  const int64_t end = (int64_t)(row_tile + 1) * kLatentRows;
+  return (int)((prefix + (end < chunk ? end : chunk) - 1) / kLatentTileKeys) + 1;
+}
+constexpr int latent_pieces(int key_tiles, int most) { return most == 0 ? 1 : (key_tiles + most - 1) / most; }
+constexpr int latent_row_tiles(int chunk) { return (int)(((int64_t)chunk + kLatentRows - 1) / kLatentRows); }
+constexpr int latent_tile_height(int chunk, int row_tile) {
+  return chunk - row_tile * kLatentRows < kLatentRows ? chunk - row_tile * kLatentRows : kLatentRows;
+}
 // Expansion: tokens and outputs of a workgroup's tile
 constexpr int kExpandTokens = 256, kExpandOuts = 256;
 
