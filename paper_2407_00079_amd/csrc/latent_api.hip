@@ -30,6 +30,16 @@ mc_status place_latent(const int32_t* prefix_lens, const int32_t* new_lens, int3
   }
 }
 
+// false: no memory for it
+bool lay_prefill_out(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, LatentPrefillLayout* lay) {
+  try {
+    *lay = latent_prefill_layout(p, prefix_lens, new_lens, batch);
+    return true;
+  } catch (const std::bad_alloc&) {
+    return false;
+  }
+}
+
 mc::LatentAppendArgs append_args(const mc_latent_params* p, const mc_rope_params* rope, const void* q, const void* kv, const AppendStrides& s,
                                  const void* norm, void* q_out, void* pool, const int32_t* block_tables, int32_t max_pages, int64_t tokens) {
   mc::LatentAppendArgs a = {};
@@ -177,7 +187,8 @@ size_t mc_latent_prefill_attn_workspace_bytes(const mc_latent_params* p, const i
   LatentLens lens;
   if (check_latent(p) != MC_OK || batch < 0 || (batch > 0 && (prefix_lens == nullptr || new_lens == nullptr))) return 0;
   if (check_latent_lens(prefix_lens, new_lens, batch, &lens) != MC_OK) return 0;
-  return latent_prefill_layout(p, prefix_lens, new_lens, batch).total;
+  LatentPrefillLayout lay;
+  return lay_prefill_out(p, prefix_lens, new_lens, batch, &lay) ? lay.total : 0;
 }
 
 mc_status mc_latent_prefill_attn_paged(const mc_latent_params* p, const void* q, const void* k, const void* v, const int64_t* strides,
@@ -202,7 +213,8 @@ mc_status mc_latent_prefill_attn_paged(const mc_latent_params* p, const void* q,
   for (const void* at : {q, k, v, pool, (const void*)out, (const void*)workspace})
     if (!aligned16(at)) return MC_ERR_ALIGN;
   if (!aligned4(block_tables) || !aligned4(lse)) return MC_ERR_ALIGN;
-  const LatentPrefillLayout lay = latent_prefill_layout(p, prefix_lens, new_lens, batch);
+  LatentPrefillLayout lay;
+  if (!lay_prefill_out(p, prefix_lens, new_lens, batch, &lay)) return MC_ERR_HIP;
   if ((int64_t)batch * max_pages_per_req > INT32_MAX || lay.items * p->num_heads > INT32_MAX) return MC_ERR_RANGE;
   if (workspace == nullptr || workspace_bytes < lay.total) return MC_ERR_WORKSPACE;
 

@@ -4,6 +4,9 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <functional>
+#include <queue>
+#include <vector>
 
 #include "host_plan.h"
 
@@ -136,37 +139,44 @@ LatentDecodeLayout latent_decode_layout(const mc_latent_params* p, int32_t batch
 }
 
 namespace {
-// us of a tile of keys, of a workgroup's beginning and end, and of joining, as measured (latent_prefill.hip)
+// us of a tile of keys (and of each of a row tile's rows in it), of a workgroup's beginning and end, of joining and of a byte of partial results,
+// as measured: head_dim 128 2.0 and 64 1.5 with 256 rows, 1.4 and 0.9 with 64
 struct PrefillTimes {
   double tile, row, ends, join, part_byte;
 };
 PrefillTimes times_of(const mc_latent_params* p) {
-  return p->head_dim == 128 ? PrefillTimes{0.9, 1.14 / kLatentRows, 5.0, 4.0, 1.0 / 2.0e6} : PrefillTimes{0.8, 0.6 / kLatentRows, 4.0, 4.0, 1.0 / 2.0e6};
+  return p->head_dim == 128 ? PrefillTimes{1.15, 0.9 / kLatentRows, 5.0, 4.0, 0.5e-6} : PrefillTimes{0.75, 0.75 / kLatentRows, 4.0, 4.0, 0.5e-6};
 }
 struct PrefillCut {
   int64_t items, part_rows;
-  int64_t most;                              // key tiles of a piece
-  double us;
+  int32_t longest;                           // key tiles of a row tile
+  double us;                                 // negative: more work items than are worth looking at
 };
-PrefillCut cut_into(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, int32_t most_tiles) {
+// The launch as the compute units that each head has take the work items, in their order, one by one.
+PrefillCut cut_into(const mc_latent_params* p, const std::vector<LatentReq>& reqs, int32_t most_tiles) {
   const PrefillTimes t = times_of(p);
   PrefillCut cut = {0, 0, 0, 0};
-  double all = 0, longest = 0;
-  for (int32_t r = 0; r < batch; ++r)
-    for (int32_t i = 0, n = latent_row_tiles(new_lens[r]); i < n; ++i) {
-      const int keys = latent_key_tiles(prefix_lens[r], new_lens[r], i), pieces = latent_pieces(keys, most_tiles), rows = latent_tile_height(new_lens[r], i);
-      const int each = (keys + pieces - 1) / pieces;
+  const size_t units = (size_t)std::max(1, kLatentWgs / p->num_heads);
+  std::priority_queue<double, std::vector<double>, std::greater<double>> ends;
+  double last = 0;
+  for (const LatentReq& r : reqs)
+    for (int32_t i = latent_row_tiles(r.chunk) - 1; i >= 0; --i) {
+      const int keys = latent_key_tiles(r.prefix, r.chunk, i), pieces = latent_pieces(keys, most_tiles), rows = latent_tile_height(r.chunk, i);
       cut.items += pieces;
       cut.part_rows += pieces > 1 ? (int64_t)pieces * rows : 0;
-      cut.most = std::max<int64_t>(cut.most, each);
-      const double tile = t.tile + t.row * rows;
-      all += keys * tile + pieces * t.ends;
-      longest = std::max(longest, each * tile + t.ends);
+      cut.longest = std::max(cut.longest, keys);
+      if (cut.items > 4 * (int64_t)units) return {0, 0, cut.longest, -1.0};
+      for (int piece = 0; piece < pieces; ++piece) {
+        double from = 0;
+        if (ends.size() == units) {
+          from = ends.top();
+          ends.pop();
+        }
+        ends.push(from + (double)keys / pieces * (t.tile + t.row * rows) + t.ends);
+        last = std::max(last, from + (double)keys / pieces * (t.tile + t.row * rows) + t.ends);
+      }
     }
-  const double wgs = (double)cut.items * p->num_heads, mean = wgs > 0 ? all * p->num_heads / wgs : 0;
-  // (the last workgroups to start end half a mean one apart)
-  cut.us = std::max(longest, all * p->num_heads / 256 + (wgs > 256 ? 0.5 * mean : 0.0));
-  if (wgs <= 256) cut.us = longest;
+  cut.us = last;
   if (cut.part_rows > 0) cut.us += t.join + (double)cut.part_rows * p->num_heads * p->head_dim * 4 * t.part_byte;
   return cut;
 }
@@ -175,21 +185,27 @@ PrefillCut cut_into(const mc_latent_params* p, const int32_t* prefix_lens, const
 LatentPrefillLayout latent_prefill_layout(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch) {
   LatentPrefillLayout l = {};
   for (int32_t r = 0; r < batch; ++r) l.items += latent_row_tiles(new_lens[r]);
-  // From eight rounds of workgroups on, whole row tiles keep the compute units busy to the end.
-  if (l.items * p->num_heads < 8 * 256) {
-    PrefillCut best = cut_into(p, prefix_lens, new_lens, batch, 0);
-    const int64_t longest = best.most;
-    for (const int parts : {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-      const int32_t most = (int32_t)((longest + parts - 1) / parts);
-      if (most < 4) break;
-      const PrefillCut cut = cut_into(p, prefix_lens, new_lens, batch, most);
+  // From four rounds of workgroups on, whole row tiles keep the compute units busy to the end.
+  if (l.items > 0 && l.items * p->num_heads <= 4 * kLatentWgs) {
+    std::vector<LatentReq> reqs((size_t)batch);
+    fill_latent_table(prefix_lens, new_lens, batch, reqs.data());
+    fill_latent_items(batch, 0, reqs.data());
+    PrefillCut best = cut_into(p, reqs, 0);
+    const int32_t longest = best.longest;
+    for (const int parts : {2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64}) {
+      const int32_t most = (longest + parts - 1) / parts;
+      if (best.us < 0 || most < 4) break;
+      const PrefillCut cut = cut_into(p, reqs, most);
+      if (cut.us < 0) break;
       if (cut.us < 0.97 * best.us) {
         best = cut;
         l.most_tiles = most;
       }
     }
-    l.items = best.items;
-    l.part_rows = best.part_rows;
+    if (l.most_tiles > 0) {
+      l.items = best.items;
+      l.part_rows = best.part_rows;
+    }
   }
   l.o_off = round_up(latent_table_bytes(batch));
   const size_t rows = (size_t)l.part_rows * (size_t)p->num_heads;
