@@ -146,13 +146,11 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
       const int r = 8 * (kAllScore ? w & 1 : h) + lane / 8;
       source[h] = (uint32_t)(r * S::kRowB + ((lane % 8) ^ S::swizzle(r)) * 16);
     }
-    auto fetch = [&](int page, int buf) __attribute__((always_inline)) {
+    auto fetch = [&](int page, int buf, int b) __attribute__((always_inline)) {      // (its block b of 64 columns)
       const char* const from = reinterpret_cast<const char*>(a.pool) + (int64_t)page * (kPageTokens * S::kRowB);
       const uint32_t to = base + buf * S::kTileB + copy_page * (kPageTokens * 128) + (kAllScore ? (w & 1) * 1024 : 0);
 #pragma unroll
-      for (int b = 0; b < S::kBlocks; ++b)
-#pragma unroll
-        for (int h = 0; h < kHalves; ++h) dma16(from + b * 128, source[h], to + b * S::kBlockB + h * 1024);
+      for (int h = 0; h < kHalves; ++h) dma16(from + b * 128, source[h], to + b * S::kBlockB + h * 1024);
     };
     // fragment addresses: as keys (rows 16 KT kg + j), as values (columns R/8 w + 16 t, keys 8 g .. of a half of the tile)
     const uint32_t k_lane = base + (16 * KT * kg + j) * 128 + ((g ^ S::swizzle(j)) << 4);
@@ -164,12 +162,13 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
     bf16x8 qf[S::kSteps];                                    // of the wave's rows of scores
     f32x4 o[S::kColTiles][MT];                               // of all rows: the wave's columns
     float ref, ref_all[MT], l;
-    auto start = [&](const At& at) __attribute__((always_inline)) {
-      if (scoring) {
-        const char* const q = reinterpret_cast<const char*>(a.q) + ((int64_t)at.row * a.stacked + my_row) * S::kRowB;
+    auto ask = [&](int of) __attribute__((always_inline)) {  // for the queries of a row, in place of those at hand
+      if (!scoring) return;
+      const char* const q = reinterpret_cast<const char*>(a.q) + ((int64_t)of * a.stacked + my_row) * S::kRowB;
 #pragma unroll
-        for (int st = 0; st < S::kSteps; ++st) qf[st] = *reinterpret_cast<const bf16x8*>(q + st * 64 + g * 16);
-      }
+      for (int st = 0; st < S::kSteps; ++st) qf[st] = *reinterpret_cast<const bf16x8*>(q + st * 64 + g * 16);
+    };
+    auto start = [&]() __attribute__((always_inline)) {
       ref = -INFINITY;
       l = 0.f;
 #pragma unroll
@@ -184,20 +183,23 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
     // the tile whose copy is next, and the page of it that this wave copies
     At nx = line.place(sums, begin);
     int page = line.page(nx, copy_page), fetched = 0, left = end - begin;
-    auto fetch_next = [&]() __attribute__((always_inline)) {
-      if (fetched == end - begin) return;
-      if (copies) fetch(page, fetched & 1);
-      if (++fetched == end - begin) return;
+    auto fetched_one = [&]() __attribute__((always_inline)) {
+      if (++fetched >= end - begin) return;
       line.next(nx);
       page = line.page(nx, copy_page);
     };
     int buf = 1;
-    auto one_tile = [&](const At& at, int block, auto tail_tag) __attribute__((always_inline)) {
+    // last: the row's last tile in the stretch, behind which row `then` follows (negative: none does)
+    auto one_tile = [&](const At& at, int block, bool last, int then, auto tail_tag) __attribute__((always_inline)) {
       constexpr bool tail = decltype(tail_tag)::value != 0;
       buf ^= 1;
       __builtin_amdgcn_s_waitcnt(0x0F70);                    // (vmcnt(0): this wave's share of the tile)
       __syncthreads();
-      fetch_next();
+      const bool more = fetched < end - begin;
+      if (!kAllScore && copies && more) {
+#pragma unroll
+        for (int b = 0; b < S::kBlocks; ++b) fetch(page, buf ^ 1, b);
+      }
 
       // scores of keys 16 (KT kg + kt) + 4 g + i for row j of the wave's tile of rows
       f32x4 s[KT];
@@ -238,7 +240,12 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
           to = mma(ring[u % kAhead], qf[u / KT], to);
           if (u + kAhead < kUses) ring[u % kAhead] = key(u + kAhead);
           __builtin_amdgcn_sched_barrier(0);
+          if (kAllScore && u % (2 * KT) == 0) {              // (a step of 64 columns a copy)
+            if (more) fetch(page, buf ^ 1, u / (2 * KT));
+            __builtin_amdgcn_sched_barrier(0);
+          }
         }
+        if (last && then >= 0) ask(then);
         if constexpr (KT == 1) s[0] += s2;
         if constexpr (tail) {
           const int seen = at.len - back - block * kTile - 16 * KT * kg - 4 * g;
@@ -255,6 +262,7 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
         probabilities();
         if (g == 0) sh.most[mine][kg][j] = most;
       }
+      if (more) fetched_one();
       __syncthreads();
       int any = 0;
 #pragma unroll
@@ -319,17 +327,26 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
       }
     };
     At at = nx;
-    fetch_next();
+    ask(at.row);
+    if (copies) {
+#pragma unroll
+      for (int b = 0; b < S::kBlocks; ++b) fetch(page, 0, b);
+    }
+    fetched_one();
     for (;;) {
       // the tiles of one row that lie in the stretch: those whose keys all its rows see, then the others
-      start(at);
+      start();
       const bool whole = at.block == 0;                      // the row began in this stretch
       const int stop = at.blocks - at.block <= left ? at.blocks : at.block + left;
       const int clear = (at.len - (a.tokens - 1)) / kTile;
       left -= stop - at.block;
+      At behind = at;                                        // the next row
+      behind.block = at.blocks - 1;
+      if (left > 0) line.next(behind);
+      const int then = left > 0 ? behind.row : -1;
       int block = at.block;
-      for (; block < stop && block < clear; ++block) one_tile(at, block, Int<0>{});
-      for (; block < stop; ++block) one_tile(at, block, Int<1>{});
+      for (; block < stop && block < clear; ++block) one_tile(at, block, block + 1 == stop, then, Int<0>{});
+      for (; block < stop; ++block) one_tile(at, block, block + 1 == stop, then, Int<1>{});
 
       // the row's sums over the waves' keys, then its result or its part of one
       const bool done = stop == at.blocks;
@@ -344,10 +361,9 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
         float all = sh.sum[m][0][j];
 #pragma unroll
         for (int i = 1; i < KG; ++i) all += sh.sum[m][i][j];
-        const int row = tile * S::kRows + m * 16 + j;
-        if (row >= a.stacked) continue;
-        const int col = (R / 8) * w + 4 * g;
+        const int row = tile * S::kRows + m * 16 + j, col = (R / 8) * w + 4 * g;
         if (whole && done) {
+          if (row >= a.stacked) continue;
           const float inv = all == 0.f ? 0.f : 1.0f / all;             // (a row that sees no key: 0)
           const int64_t to = (int64_t)at.row * a.stacked + row;
 #pragma unroll
@@ -359,10 +375,11 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
           }
           if (a.lse != nullptr && w == 0 && g == 0) a.lse[to] = (ref_all[m] + __builtin_amdgcn_logf(all)) * 0.6931471805599453f;
         } else {
-          const int64_t to = part0 + m * 16 + j;
+          // (in the order of the registers: 1 KiB of 16 rows by 16 columns at a time)
 #pragma unroll
-          for (int t = 0; t < S::kColTiles; ++t) *reinterpret_cast<f32x4*>(a.o_parts + to * R + col + 16 * t) = o[t][m];
-          if (w == 0 && g == 0) a.ml_parts[to] = float2{ref_all[m], all};
+          for (int t = 0; t < S::kColTiles; ++t)
+            *reinterpret_cast<f32x4*>(a.o_parts + (part0 + m * 16) * R + (w * S::kColTiles + t) * 256 + lane * 4) = o[t][m];
+          if (w == 0 && g == 0) a.ml_parts[part0 + m * 16 + j] = float2{ref_all[m], all};
         }
       }
       if (whole) {
@@ -372,8 +389,7 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
         if (more != 0) open = LatentChain{at.row, stretch, more, 0};
       }
       if (left == 0) break;
-      at.block = at.blocks - 1;
-      line.next(at);
+      at = behind;
     }
   }
   if (notes && !by_row) a.chains[stretch] = open;
@@ -393,121 +409,74 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
   }
 }
 
-// Rows that several stretches have parts of: a workgroup has 128 columns of one stacked row, whose parts its half waves share out.
-constexpr int kJoinCols = 128, kJoinThreads = 512;
-template <int R>
-__global__ __launch_bounds__(kJoinThreads) void latent_join_kernel(const LatentDecodeArgs a, int tile_rows) {
-  __shared__ float weight[kLatentWgs], tops[kJoinThreads / 64], sums[kJoinThreads / 64];
-  __shared__ __attribute__((aligned(16))) float outs[kJoinThreads / 32][kJoinCols];
+// Rows that several stretches have parts of.  A part of 16 stacked rows by 16 columns is 1 KiB, lane by lane as it was computed: a wave joins that
+// of all parts, or (few such pieces, of many parts as a rule) the WAVES waves of a workgroup every WAVES-th each.
+template <int R, int WAVES, bool SHARED>
+__global__ __launch_bounds__(WAVES * 64) void latent_join_kernel(const LatentDecodeArgs a, int tile_rows) {
+  __shared__ f32x4 outs[SHARED ? WAVES : 1][64];
+  __shared__ float2 sums[SHARED ? WAVES : 1][16];
   const LatentChain chain = a.chains[blockIdx.x];
   if (chain.more == 0) return;
-  const int stacked = blockIdx.y, tile = stacked / tile_rows, in_tile = stacked - tile * tile_rows;
-  auto part = [&](int i) __attribute__((always_inline)) {
-    return (((int64_t)tile * a.stretches + chain.first + i) * 2 + (i == 0 ? 1 : 0)) * tile_rows + in_tile;
-  };
-  const int n = chain.more + 1, t = threadIdx.x, wave = t / 64;
-  const float2 ml = t < n ? a.ml_parts[part(t)] : float2{-INFINITY, 0.f};      // (at most kLatentWgs parts)
-  auto over_wave = [](float x, auto&& join) __attribute__((always_inline)) {
-#pragma unroll
-    for (int step = 1; step < 64; step *= 2) x = join(x, __shfl_xor(x, step, 64));
-    return x;
-  };
-  float top = over_wave(ml.x, [](float x, float y) { return fmaxf(x, y); });
-  if (t % 64 == 0) tops[wave] = top;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kJoinThreads / 64; ++i) top = fmaxf(top, tops[i]);
-  const float from = top == -INFINITY ? 0.f : top;           // (every score is -inf or NaN)
-  const float mine = __builtin_amdgcn_exp2f(ml.x - from);
-  if (t < kLatentWgs) weight[t] = mine;
-  const float share = over_wave(mine * ml.y, [](float x, float y) { return x + y; });
-  if (t % 64 == 0) sums[wave] = share;
-  __syncthreads();
-  float l = 0.f;
-#pragma unroll
-  for (int i = 0; i < kJoinThreads / 64; ++i) l += sums[i];
-  const int slot = t / 32, col = t % 32 * 4;
-  const float* const o = a.o_parts + blockIdx.z * kJoinCols + col;
-  f32x4 x = {0.f, 0.f, 0.f, 0.f};
-  constexpr int kAtOnce = 8;
-  for (int i0 = slot; i0 < n; i0 += kAtOnce * (kJoinThreads / 32)) {
-    f32x4 v[kAtOnce];
-#pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      const int i = i0 + k * (kJoinThreads / 32);
-      v[k] = *reinterpret_cast<const f32x4*>(o + part(i < n ? i : i0) * R);
-    }
-#pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      const int i = i0 + k * (kJoinThreads / 32);
-      if (i < n) x += weight[i] * v[k];
-    }
-  }
-  *reinterpret_cast<f32x4*>(&outs[slot][col]) = x;
-  __syncthreads();
-  if (t >= kJoinCols / 4) return;
-#pragma unroll
-  for (int i = 1; i < kJoinThreads / 32; ++i) x += *reinterpret_cast<const f32x4*>(&outs[i][col]);
-  const int64_t to = (int64_t)chain.row * a.stacked + stacked;
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
-  bf16x4 y;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) y[i] = (__bf16)(x[i] * inv);
-  *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(a.out) + to * R + blockIdx.z * kJoinCols + col) = y;
-  if (a.lse != nullptr && blockIdx.z == 0 && t == 0) a.lse[to] = (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-}
-
-// The same for many rows, of few parts each as a rule: a wave has 128 columns of a stacked row, its halves every other part.
-constexpr int kRowJoinThreads = 256;
-template <int R>
-__global__ __launch_bounds__(kRowJoinThreads) void latent_join_rows_kernel(const LatentDecodeArgs a, int tile_rows) {
-  constexpr int kGroups = R / kJoinCols, kRowsOfWg = kRowJoinThreads / 64 / kGroups > 0 ? kRowJoinThreads / 64 / kGroups : 1;
-  static_assert(kRowsOfWg * kGroups * 64 == kRowJoinThreads, "whole rows a workgroup");
-  const LatentChain chain = a.chains[blockIdx.x];
-  if (chain.more == 0) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = (wave % kGroups) * kJoinCols + (lane & 31) * 4;
-  const int stacked = blockIdx.y * kRowsOfWg + wave / kGroups, tile = stacked / tile_rows, in_tile = stacked - tile * tile_rows;
-  if (stacked >= a.stacked) return;
-  auto part = [&](int i) __attribute__((always_inline)) {
-    return (((int64_t)tile * a.stretches + chain.first + i) * 2 + (i == 0 ? 1 : 0)) * tile_rows + in_tile;
-  };
+  const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, wave = threadIdx.x >> 6;
+  const int cols = SHARED ? (int)blockIdx.z : (int)blockIdx.z * WAVES + wave;      // which 16 of them
+  const int row0 = blockIdx.y * 16, tile = row0 / tile_rows, in_tile = row0 - tile * tile_rows;
   const int n = chain.more + 1;
-  float top = -INFINITY;
-  for (int i = lane; i < n; i += 64) top = fmaxf(top, a.ml_parts[part(i)].x);
-#pragma unroll
-  for (int step = 1; step < 64; step *= 2) top = fmaxf(top, __shfl_xor(top, step, 64));
-  const float from = top == -INFINITY ? 0.f : top;           // (every score is -inf or NaN)
-  float l = 0.f;
+  constexpr int kStep = SHARED ? WAVES : 1, kAtOnce = 8;
+  float top = -INFINITY, l = 0.f;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
-  constexpr int kAtOnce = 4;
-  for (int i0 = half; i0 < n; i0 += 2 * kAtOnce) {
+  auto reference = [](float m) __attribute__((always_inline)) { return m == -INFINITY ? 0.f : m; };      // (every score is -inf or NaN)
+  for (int i0 = SHARED ? wave : 0; i0 < n; i0 += kStep * kAtOnce) {
     f32x4 v[kAtOnce];
     float2 ml[kAtOnce];
+    float next = top;
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) {
-      const int64_t at = part(i0 + 2 * k < n ? i0 + 2 * k : i0);
-      v[k] = *reinterpret_cast<const f32x4*>(a.o_parts + at * R + col);
-      ml[k] = a.ml_parts[at];
+      const int i = i0 + kStep * k < n ? i0 + kStep * k : i0;          // (behind the last: one again, for nothing)
+      const int64_t at = (((int64_t)tile * a.stretches + chain.first + i) * 2 + (i == 0 ? 1 : 0)) * tile_rows + in_tile;
+      v[k] = *reinterpret_cast<const f32x4*>(a.o_parts + at * R + cols * 256 + lane * 4);
+      ml[k] = a.ml_parts[at + j];
     }
 #pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) next = fmaxf(next, ml[k].x);
+    const float from = reference(next), before = __builtin_amdgcn_exp2f(top - from);
+    l *= before;
+    x *= before;
+    top = next;
+#pragma unroll
     for (int k = 0; k < kAtOnce; ++k)
-      if (i0 + 2 * k < n) {
+      if (i0 + kStep * k < n) {
         const float weight = __builtin_amdgcn_exp2f(ml[k].x - from);
         l += weight * ml[k].y;
         x += weight * v[k];
       }
   }
-  l += __shfl_xor(l, 32, 64);
+  if constexpr (SHARED) {
+    outs[wave][lane] = x;
+    if (g == 0) sums[wave][j] = float2{top, l};
+    __syncthreads();
+    if (wave != 0) return;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] += __shfl_xor(x[i], 32, 64);
-  if (half != 0) return;
+    for (int i = 1; i < WAVES; ++i) top = fmaxf(top, sums[i][j].x);
+    const float from = reference(top);
+    l = 0.f;
+    x = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) {
+      const float2 ml = sums[i][j];
+      const float weight = __builtin_amdgcn_exp2f(ml.x - from);
+      l += weight * ml.y;
+      x += weight * outs[i][lane];
+    }
+  }
+  const int stacked = row0 + j;
+  if (stacked >= a.stacked) return;
   const int64_t to = (int64_t)chain.row * a.stacked + stacked;
   const float inv = l == 0.f ? 0.f : 1.0f / l;
   bf16x4 y;
 #pragma unroll
   for (int i = 0; i < 4; ++i) y[i] = (__bf16)(x[i] * inv);
-  *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(a.out) + to * R + col) = y;
-  if (a.lse != nullptr && col == 0) a.lse[to] = (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(a.out) + to * R + cols * 16 + 4 * g) = y;
+  if (a.lse != nullptr && cols == 0 && g == 0) a.lse[to] = (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
 template <int R>
@@ -517,12 +486,9 @@ hipError_t enqueue(int rows, const LatentDecodeArgs& args, hipStream_t stream) {
   else if (rows == 32) latent_decode_kernel<R, 2><<<wgs, kWaves * 64, 0, stream>>>(args);
   else if (rows == 64) latent_decode_kernel<R, 4><<<wgs, kWaves * 64, 0, stream>>>(args);
   else return hipErrorInvalidValue;
-  if (args.n_chains * args.stacked < 512) {
-    latent_join_kernel<R><<<dim3(args.n_chains, args.stacked, R / kJoinCols), kJoinThreads, 0, stream>>>(args, rows);
-  } else {
-    constexpr int kRowsOfWg = kRowJoinThreads / 64 / (R / kJoinCols);
-    latent_join_rows_kernel<R><<<dim3(args.n_chains, (args.stacked + kRowsOfWg - 1) / kRowsOfWg), kRowJoinThreads, 0, stream>>>(args, rows);
-  }
+  const int pieces = (args.stacked + 15) / 16;
+  if (args.n_chains * pieces < 32) latent_join_kernel<R, 16, true><<<dim3(args.n_chains, pieces, R / 16), 16 * 64, 0, stream>>>(args, rows);
+  else latent_join_kernel<R, 4, false><<<dim3(args.n_chains, pieces, R / 16 / 4), 4 * 64, 0, stream>>>(args, rows);
   return hipGetLastError();
 }
 
