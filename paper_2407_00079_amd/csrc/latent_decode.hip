@@ -11,8 +11,8 @@
 //   * A softmax runs in one pass in fp32.  Its reference is one for all four waves and lags behind the largest score by at most 2^8: probabilities
 //     are formed against it before the waves have met, and only where a score outgrew it the waves exchange maxima, scale what they
 //     have and form the tile's probabilities again (flags that all waves of the workgroup read behind the same barrier).
-//   * Keys behind what a row sees get probability 0, and in a row's last tiles elements that are not finite are cleared as they come out of LDS
-//     as values: 0 times whatever an unwritten slot holds stays 0.  (A key that counts and is not finite has made its score so.)
+//   * Keys behind what a row sees get probability 0, and what is not finite in a row's last tiles is cleared, once it has been used as keys, before
+//     it is used as values: 0 times whatever an unwritten slot holds stays 0.  (A key that counts and is not finite has made its score so.)
 //   * The tiles of all rows stand in one line, of which each workgroup takes an equal stretch; it finds its place from the lengths.  Rows that a stretch's
 //     end cuts leave partial results in the workspace, and a second kernel joins them in the order of the line.
 #include "attn_narrow_device.h"
@@ -190,8 +190,10 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
     };
     int buf = 1;
     // last: the row's last tile in the stretch, behind which row `then` follows (negative: none does)
-    auto one_tile = [&](const At& at, int block, bool last, int then, auto tail_tag) __attribute__((always_inline)) {
-      constexpr bool tail = decltype(tail_tag)::value != 0;
+    // (one piece of code for all tiles: a launch begins with an empty instruction cache, and a second one for the last tiles cost 3 us)
+    auto one_tile = [&](const At& at, int block, bool last, int then) __attribute__((always_inline)) {
+      const int unseen = at.len - (a.tokens - 1) - block * kTile;      // the first key of the tile that not all rows see
+      const bool tail = unseen < kTile;
       buf ^= 1;
       __builtin_amdgcn_s_waitcnt(0x0F70);                    // (vmcnt(0): this wave's share of the tile)
       __syncthreads();
@@ -247,7 +249,8 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
         }
         if (last && then >= 0) ask(then);
         if constexpr (KT == 1) s[0] += s2;
-        if constexpr (tail) {
+        if (tail) {
+          asm volatile("");                                  // (a branch, not selects on every tile's path)
           const int seen = at.len - back - block * kTile - 16 * KT * kg - 4 * g;
 #pragma unroll
           for (int e = 0; e < 4 * KT; ++e)
@@ -288,6 +291,18 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
           ref = next;
           probabilities();
         }
+        if (!tail) __syncthreads();
+      }
+      if (tail) {
+        // values of keys that not all rows see: 0 in place of what is not finite, whose probability of 0 would not take it away
+        for (int i = (unseen > 0 ? unseen : 0) * (R / 8) + threadIdx.x; i < kTile * (R / 8); i += kWaves * 64) {
+          const int r = i / (R / 8), at_col = i % (R / 8);
+          const uint32_t place = base + buf * S::kTileB + at_col / 8 * S::kBlockB + r * 128 + at_col % 8 * 16;      // (in any order of the granules)
+          u32x4 bits = *reinterpret_cast<MC_LDS const u32x4*>(place);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) bits[k] = finite_pair(bits[k]);
+          *reinterpret_cast<MC_LDS u32x4*>(place) = bits;
+        }
         __syncthreads();
       }
       l += sum;
@@ -312,15 +327,8 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
 #pragma unroll
             for (int m = 0; m < MT; ++m) pf[m] = *reinterpret_cast<MC_LDS const bf16x8*>(p_read + 16 * m * S::kPRowB + u / S::kColTiles * 64);
           }
-          bf16x8 vf = ring[u % kAhead];
-          if constexpr (tail) {
-            u32x4 bits = __builtin_bit_cast(u32x4, vf);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) bits[i] = finite_pair(bits[i]);
-            vf = __builtin_bit_cast(bf16x8, bits);
-          }
-#pragma unroll
-          for (int m = 0; m < MT; ++m) o[t][m] = mma(vf, pf[m], o[t][m]);
+          for (int m = 0; m < MT; ++m) o[t][m] = mma(ring[u % kAhead], pf[m], o[t][m]);
           if (u + kAhead < kUses) ring[u % kAhead] = value(u + kAhead);
           __builtin_amdgcn_sched_barrier(0);
         }
@@ -334,19 +342,16 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
     }
     fetched_one();
     for (;;) {
-      // the tiles of one row that lie in the stretch: those whose keys all its rows see, then the others
+      // the tiles of one row that lie in the stretch
       start();
       const bool whole = at.block == 0;                      // the row began in this stretch
       const int stop = at.blocks - at.block <= left ? at.blocks : at.block + left;
-      const int clear = (at.len - (a.tokens - 1)) / kTile;
       left -= stop - at.block;
       At behind = at;                                        // the next row
       behind.block = at.blocks - 1;
       if (left > 0) line.next(behind);
       const int then = left > 0 ? behind.row : -1;
-      int block = at.block;
-      for (; block < stop && block < clear; ++block) one_tile(at, block, block + 1 == stop, then, Int<0>{});
-      for (; block < stop; ++block) one_tile(at, block, block + 1 == stop, then, Int<1>{});
+      for (int block = at.block; block < stop; ++block) one_tile(at, block, block + 1 == stop, then);
 
       // the row's sums over the waves' keys, then its result or its part of one
       const bool done = stop == at.blocks;
