@@ -47,13 +47,16 @@ struct Line {
   }
   struct Sums {
     int per, upto, mine, all;                // rows a lane looks over; their tiles, running and its own
+    int rows;                                // that are not empty
   };
   __device__ __forceinline__ Sums sums() const {
     const int lane = threadIdx.x & 63;
-    Sums s = {(batch + 63) / 64, 0, 0, 0};
+    Sums s = {(batch + 63) / 64, 0, 0, 0, 0};
     for (int i = 0; i < s.per; ++i) {
       const int r = lane * s.per + i;
-      s.mine += r < batch ? tiles(valid(lens[r])) : 0;
+      const int n = r < batch ? tiles(valid(lens[r])) : 0;
+      s.mine += n;
+      s.rows += __popcll(__builtin_amdgcn_ballot_w64(n > 0));
     }
     s.upto = scan(s.mine);
     s.all = __builtin_amdgcn_readlane(s.upto, 63);
@@ -121,7 +124,7 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
   const int tile = (int)(blockIdx.x / (uint32_t)a.stretches), stretch = (int)blockIdx.x - tile * a.stretches;
   const Line line(a);
   const typename Line::Sums sums = line.sums();
-  const int used = latent_used(sums.all, a.stretches);
+  const int used = latent_used(sums.all, sums.rows, a.stretches);
   const int begin = stretch < used ? (int)decode_begin(sums.all, stretch, used) : 0;
   const int end = stretch < used ? (int)decode_begin(sums.all, stretch + 1, used) : 0;
   const bool notes = tile == 0 && threadIdx.x == 0, by_row = a.batch <= a.stretches;
@@ -426,35 +429,39 @@ __global__ __launch_bounds__(WAVES * 64) void latent_join_kernel(const LatentDec
   const int cols = SHARED ? (int)blockIdx.z : (int)blockIdx.z * WAVES + wave;      // which 16 of them
   const int row0 = blockIdx.y * 16, tile = row0 / tile_rows, in_tile = row0 - tile * tile_rows;
   const int n = chain.more + 1;
-  constexpr int kStep = SHARED ? WAVES : 1, kAtOnce = 8;
+  constexpr int kStep = SHARED ? WAVES : 1, kAtOnce = 4;
   float top = -INFINITY, l = 0.f;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
   auto reference = [](float m) __attribute__((always_inline)) { return m == -INFINITY ? 0.f : m; };      // (every score is -inf or NaN)
-  for (int i0 = SHARED ? wave : 0; i0 < n; i0 += kStep * kAtOnce) {
-    f32x4 v[kAtOnce];
-    float2 ml[kAtOnce];
+  auto take = [&](int i0, auto many) __attribute__((always_inline)) {      // so many parts, all asked for at once
+    constexpr int N = decltype(many)::value;
+    f32x4 v[N];
+    float2 ml[N];
     float next = top;
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      const int i = i0 + kStep * k < n ? i0 + kStep * k : i0;          // (behind the last: one again, for nothing)
+    for (int k = 0; k < N; ++k) {
+      const int i = i0 + kStep * k;
       const int64_t at = (((int64_t)tile * a.stretches + chain.first + i) * 2 + (i == 0 ? 1 : 0)) * tile_rows + in_tile;
       v[k] = *reinterpret_cast<const f32x4*>(a.o_parts + at * R + cols * 256 + lane * 4);
       ml[k] = a.ml_parts[at + j];
     }
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) next = fmaxf(next, ml[k].x);
+    for (int k = 0; k < N; ++k) next = fmaxf(next, ml[k].x);
     const float from = reference(next), before = __builtin_amdgcn_exp2f(top - from);
     l *= before;
     x *= before;
     top = next;
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k)
-      if (i0 + kStep * k < n) {
-        const float weight = __builtin_amdgcn_exp2f(ml[k].x - from);
-        l += weight * ml[k].y;
-        x += weight * v[k];
-      }
-  }
+    for (int k = 0; k < N; ++k) {
+      const float weight = __builtin_amdgcn_exp2f(ml[k].x - from);
+      l += weight * ml[k].y;
+      x += weight * v[k];
+    }
+  };
+  int i0 = SHARED ? wave : 0;
+  for (; i0 + kStep * (kAtOnce - 1) < n; i0 += kStep * kAtOnce) take(i0, Int<kAtOnce>{});
+  for (; i0 + kStep < n; i0 += kStep * 2) take(i0, Int<2>{});
+  if (i0 < n) take(i0, Int<1>{});
   if constexpr (SHARED) {
     outs[wave][lane] = x;
     if (g == 0) sums[wave][j] = float2{top, l};
