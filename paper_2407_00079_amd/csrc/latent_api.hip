@@ -169,9 +169,7 @@ mc_status mc_latent_expand_paged(const mc_latent_params* p, const void* weight, 
   args.weight = weight, args.pool = pool, args.block_tables = block_tables, args.kv = kv;
   args.tokens = all.total_new;
   args.outs = p->num_heads * 2 * p->head_dim, args.latent_dim = p->latent_dim, args.batch = batch, args.max_pages = max_pages_per_req;
-  args.token_tiles = (int32_t)((all.total_new + mc::kExpandTokens - 1) / mc::kExpandTokens);
-  args.out_tiles = (args.outs + mc::kExpandOuts - 1) / mc::kExpandOuts;
-  if ((int64_t)batch * max_pages_per_req > INT32_MAX || ((int64_t)args.token_tiles + mc::kXcds) * args.out_tiles > INT32_MAX) return MC_ERR_RANGE;
+  if ((int64_t)batch * max_pages_per_req > INT32_MAX) return MC_ERR_RANGE;
   if (workspace == nullptr || workspace_bytes < mc_latent_workspace_bytes(batch)) return MC_ERR_WORKSPACE;
 
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);

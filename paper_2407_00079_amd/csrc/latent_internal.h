@@ -45,7 +45,7 @@ struct LatentExpandArgs {
   void* kv;
   int64_t tokens;
   int32_t outs, latent_dim, batch, max_pages;
-  int32_t token_tiles, out_tiles;
+  int32_t token_tiles, out_tiles, by_xcd, past_caches;         // (the launch's own)
 };
 hipError_t launch_latent_expand(const LatentExpandArgs& args, const LatentReq* reqs, const LatentReqTable* arg, hipStream_t stream);
 

@@ -65,7 +65,5 @@ constexpr int latent_row_tiles(int chunk) { return (int)(((int64_t)chunk + kLate
 constexpr int latent_tile_height(int chunk, int row_tile) {
   return chunk - row_tile * kLatentRows < kLatentRows ? chunk - row_tile * kLatentRows : kLatentRows;
 }
-// Expansion: tokens and outputs of a workgroup's tile
-constexpr int kExpandTokens = 256, kExpandOuts = 256;
 
 }  // namespace mc
