@@ -76,7 +76,7 @@ _lib = None
 
 def lib():
     """The loaded library; raises if it was never built (run ``__graft_entry__.build()``)."""
-    global _lib, _call, _misfit, _row_stride
+    global _lib, _call, _misfit, _row_stride, _head_strides
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2407_00079_amd.build` "
@@ -188,7 +188,7 @@ def lib():
             _call = _call_by_ctypes
         else:
             _function.update((name, ctypes.cast(getattr(l, name), ctypes.c_void_p).value) for name in EXPORTS)
-            _call, _misfit, _row_stride = _mccall.call, _mccall.misfit, _mccall.row_stride
+            _call, _misfit, _row_stride, _head_strides = _mccall.call, _mccall.misfit, _mccall.row_stride, _mccall.head_strides
         _lib = l
     return _lib
 
@@ -696,7 +696,14 @@ def _row_stride_by_python(device: int, dtype, t, tokens: int, heads: int, dim: i
     return stride[0] if tokens > 1 else heads * dim
 
 
-_misfit, _row_stride = _misfit_by_python, _row_stride_by_python
+def _head_strides_by_python(device: int, dtype, t, tokens: int, heads: int, dim: int):
+    shape, stride = tuple(t.shape), t.stride()
+    if shape != (tokens, heads, dim) or stride[2] != 1 or t.dtype is not dtype or t.get_device() != device:
+        return None
+    return stride[0] if tokens > 1 else heads * dim, stride[1] if heads > 1 else dim
+
+
+_misfit, _row_stride, _head_strides = _misfit_by_python, _row_stride_by_python, _head_strides_by_python
 
 
 def _is(t) -> str:
@@ -913,35 +920,31 @@ def _latent(params):
     return (_DTYPES or _dtypes())[params.dtype]
 
 
-def _rows_of_heads(name: str, device: int, dtype, t, tokens: int, heads: int, dim: int):
-    """Elements from token to token and from head to head of [tokens, heads, dim] whose rows are dense."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or shape[0] != tokens or shape[1] != heads or shape[2] != dim or stride[2] != 1 or t.dtype is not dtype or \
-            t.get_device() != device:
-        raise ValueError(f"{name}: {dtype} [{tokens}, {heads}, {dim}] with dense rows on device {device} wanted, not {_is(t)}")
-    return stride[0] if tokens > 1 else heads * dim, stride[1] if heads > 1 else dim
+def _no_rows(name: str, device: int, dtype, t, *shape) -> None:
+    raise ValueError(f"{name}: {dtype} {list(shape)} with dense rows on device {device} wanted, not {_is(t)}")
 
 
-def _latent_pool(params, device: int, dtype, pool, block_tables, rows: int, workspace) -> int:
-    _dense("pool", device, dtype, pool, params.num_pages * params.page_size * (params.latent_dim + params.rope_dim))
+def _pool_table(params, device: int, dtype, pool, block_tables, rows: int, workspace, names: str = "", *more) -> int:
+    """Looks the pool, ``more`` tensors of its type, the block table and the workspace over: the table's columns."""
+    _dense("pool " + names, device, dtype, pool, params.num_pages * params.page_size * (params.latent_dim + params.rope_dim), *more)
     wide = _table(block_tables, rows)
-    _dense("block_tables", device, _torch.int32, block_tables, 0)
     _here(device, workspace)
     return wide
 
 
-def _latent_new(params, q, kv, norm, q_out, tokens: int):
+def _latent_new(params, q, kv, q_out, tokens: int):
     """Looks the tensors of an append over: (device, type, strides)."""
     dtype = _latent(params)
     device, H, P, row = q.get_device(), params.num_heads, params.rope_dim, params.latent_dim + params.rope_dim
-    a = _rows_of_heads("q", device, dtype, q, tokens, H, P)
-    b = _row_stride(device, dtype, kv, tokens, 1, row)
-    c = _rows_of_heads("q_out", device, dtype, q_out, tokens, H, P)
+    a, b, c = _head_strides(device, dtype, q, tokens, H, P), _row_stride(device, dtype, kv, tokens, 1, row), _head_strides(device, dtype, q_out, tokens, H, P)
+    if a is None or c is None:
+        _no_rows("q" if a is None else "q_out", device, dtype, q if a is None else q_out, tokens, H, P)
     if b < 0:
-        raise ValueError(f"kv: {dtype} [{tokens}, {row}] with dense rows on device {device} wanted, not {_is(kv)}")
-    if norm is not None:
-        _dense("norm", device, dtype, norm, params.latent_dim)
-    return device, dtype, (ctypes.c_int64 * 5)(*a, b, *c)
+        _no_rows("kv", device, dtype, kv, tokens, row)
+    return device, dtype, _Strides5(*a, b, *c)
+
+
+_Strides4, _Strides5 = ctypes.c_int64 * 4, ctypes.c_int64 * 5
 
 
 def mc_latent_workspace_bytes(batch: int) -> int:
@@ -956,8 +959,9 @@ def mc_latent_append_paged(params: McLatentParams, rope: McRopeParams, q, kv, no
     n = len(prefix_lens)
     if len(new_lens) != n:
         raise ValueError(f"{n} prefix lengths and {len(new_lens)} new lengths")
-    device, dtype, strides = _latent_new(params, q, kv, norm, q_out, sum(new_lens))
-    wide = _latent_pool(params, device, dtype, pool, block_tables, n, workspace)
+    device, dtype, strides = _latent_new(params, q, kv, q_out, sum(new_lens))
+    wide = _pool_table(params, device, dtype, pool, block_tables, n, workspace, "norm", *(() if norm is None else (norm, params.latent_dim)))
+    _dense("block_tables", device, _torch.int32, block_tables, 0)
     _enqueue("mc_latent_append_paged", params, _rope(rope), q, kv, strides, norm, q_out, pool, block_tables, wide, _ints("i", prefix_lens, n),
              _ints("i", new_lens, n), n, workspace, _nbytes(workspace), _on(stream))
 
@@ -966,9 +970,9 @@ def mc_latent_append_decode(params: McLatentParams, rope: McRopeParams, q, kv, n
                             stream=None) -> None:
     """The same for ``tokens`` new tokens a row, the last at position ``seq_lens[r] - 1``; ``seq_lens``: int32 device tensor."""
     n = seq_lens.numel()
-    device, dtype, strides = _latent_new(params, q, kv, norm, q_out, n * tokens)
-    wide = _latent_pool(params, device, dtype, pool, block_tables, n, None)
-    _dense("seq_lens", device, _torch.int32, seq_lens, n)
+    device, dtype, strides = _latent_new(params, q, kv, q_out, n * tokens)
+    wide = _pool_table(params, device, dtype, pool, block_tables, n, None, "norm", *(() if norm is None else (norm, params.latent_dim)))
+    _dense("block_tables seq_lens", device, _torch.int32, block_tables, 0, seq_lens, n)
     _enqueue("mc_latent_append_decode", params, _rope(rope), q, kv, strides, norm, q_out, pool, block_tables, wide, seq_lens, n, tokens,
              _on(stream))
 
@@ -982,9 +986,9 @@ def mc_latent_decode_attn_paged(params: McLatentParams, q, pool, block_tables, s
     dtype = _latent(params)
     n, device = seq_lens.numel(), q.get_device()
     rows = n * tokens * params.num_heads
-    _dense("q out", device, dtype, q, rows * (params.latent_dim + params.rope_dim), out, rows * params.latent_dim)
-    wide = _latent_pool(params, device, dtype, pool, block_tables, n, workspace)
-    _dense("seq_lens", device, _torch.int32, seq_lens, n)
+    wide = _pool_table(params, device, dtype, pool, block_tables, n, workspace, "q out", q, rows * (params.latent_dim + params.rope_dim), out,
+                       rows * params.latent_dim)
+    _dense("block_tables seq_lens", device, _torch.int32, block_tables, 0, seq_lens, n)
     if lse is not None:
         _dense("lse", device, _torch.float32, lse, rows)
     _enqueue("mc_latent_decode_attn_paged", params, q, pool, block_tables, wide, seq_lens, n, tokens, out, lse, workspace, _nbytes(workspace),
@@ -995,8 +999,8 @@ def mc_latent_expand_paged(params: McLatentParams, weight, pool, block_tables, l
     """Enqueue the keys and values of whole requests: weight [heads * 2 * head_dim, latent_dim], kv [sum of lens, heads, 2 * head_dim]."""
     dtype = _latent(params)
     n, device, outs = len(lens), pool.get_device(), params.num_heads * 2 * params.head_dim
-    _dense("weight kv", device, dtype, weight, outs * params.latent_dim, kv, sum(lens) * outs)
-    wide = _latent_pool(params, device, dtype, pool, block_tables, n, workspace)
+    wide = _pool_table(params, device, dtype, pool, block_tables, n, workspace, "weight kv", weight, outs * params.latent_dim, kv, sum(lens) * outs)
+    _dense("block_tables", device, _torch.int32, block_tables, 0)
     _enqueue("mc_latent_expand_paged", params, weight, pool, block_tables, wide, _ints("i", lens, n), n, kv, workspace, _nbytes(workspace), _on(stream))
 
 
@@ -1017,10 +1021,12 @@ def mc_latent_prefill_attn_paged(params: McLatentParams, q, k, v, pool, block_ta
         raise ValueError(f"{n} prefix lengths and {len(new_lens)} new lengths")
     device, H, D, T = q.get_device(), params.num_heads, params.head_dim, sum(new_lens)
     N = T + sum(prefix_lens)
-    _dense("q out", device, dtype, q, T * H * (D + params.rope_dim), out, T * H * D)
-    strides = (ctypes.c_int64 * 4)(*_rows_of_heads("k", device, dtype, k, N, H, D), *_rows_of_heads("v", device, dtype, v, N, H, D))
+    wide = _pool_table(params, device, dtype, pool, block_tables, n, workspace, "q out", q, T * H * (D + params.rope_dim), out, T * H * D)
+    a, b = _head_strides(device, dtype, k, N, H, D), _head_strides(device, dtype, v, N, H, D)
+    if a is None or b is None:
+        _no_rows("k" if a is None else "v", device, dtype, k if a is None else v, N, H, D)
+    _dense("block_tables", device, _torch.int32, block_tables, 0)
     if lse is not None:
         _dense("lse", device, _torch.float32, lse, T * H)
-    wide = _latent_pool(params, device, dtype, pool, block_tables, n, workspace)
-    _enqueue("mc_latent_prefill_attn_paged", params, q, k, v, strides, pool, block_tables, wide, _ints("i", prefix_lens, n), _ints("i", new_lens, n), n,
+    _enqueue("mc_latent_prefill_attn_paged", params, q, k, v, _Strides4(*a, *b), pool, block_tables, wide, _ints("i", prefix_lens, n), _ints("i", new_lens, n), n,
              out, lse, workspace, _nbytes(workspace), _on(stream))

@@ -227,7 +227,7 @@ mc_status mc_latent_prefill_attn_paged(const mc_latent_params* p, const void* q,
   args.ml_parts = reinterpret_cast<float2*>(ws + lay.ml_off);
   args.k_token = 2 * s.k_token, args.k_head = 2 * s.k_head, args.v_token = 2 * s.v_token, args.v_head = 2 * s.v_head;
   args.heads = p->num_heads, args.head_dim = p->head_dim, args.latent_dim = p->latent_dim, args.batch = batch, args.max_pages = max_pages_per_req;
-  args.most_tiles = lay.most_tiles, args.items = (int32_t)lay.items;
+  args.most_tiles = lay.most_tiles, args.items = (int32_t)lay.items, args.cut_tiles = (int32_t)lay.cut_tiles;
   args.scale_log2e = latent_scale_log2e(p);
   return mc::launch_latent_prefill(args, reinterpret_cast<const mc::LatentReq*>(workspace), batch <= mc::kMaxArgEntries ? &arg : nullptr, stream) == hipSuccess
              ? MC_OK

@@ -24,7 +24,7 @@ struct FromTable {
   Table t;
   __device__ __forceinline__ Place place(int32_t tok, int32_t) const {
     const int r = find_request<0>(t.ints(), t.batch, tok);
-    const const_i32_ptr at = (const_i32_ptr)t.ints() + 7 * (int64_t)r;
+    const const_i32_ptr at = (const_i32_ptr)t.ints() + 8 * (int64_t)r;
     return {r, at[2] + (tok - at[0])};
   }
 };

@@ -7,7 +7,7 @@ namespace mc {
 namespace {
 
 typedef const __attribute__((address_space(4))) int32_t* const_i32_ptr;
-static_assert(sizeof(LatentReq) == 28, "seven integers");
+static_assert(sizeof(LatentReq) == 32, "eight integers");
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
@@ -25,7 +25,7 @@ __device__ __forceinline__ int find_request(const int32_t* table, int batch, int
   int lo = 0, n = batch;
   while (n > 1) {
     const int stride = (n + 63) / 64, at = lane * stride;
-    const int32_t v = table[7 * (int64_t)(lo + (at < n ? at : 0)) + FIELD];
+    const int32_t v = table[8 * (int64_t)(lo + (at < n ? at : 0)) + FIELD];
     const int k = __popcll(__builtin_amdgcn_ballot_w64(at < n && v <= x)) - 1;
     lo += k * stride;
     n = n - k * stride < stride ? n - k * stride : stride;
@@ -46,8 +46,8 @@ struct LatentListTable {
 };
 template <typename Table>
 __device__ __forceinline__ LatentReq request(const Table& table, int r) {
-  const const_i32_ptr at = (const_i32_ptr)table.ints() + 7 * (int64_t)r;
-  return {at[0], at[1], at[2], at[3], at[4], at[5], at[6]};
+  const const_i32_ptr at = (const_i32_ptr)table.ints() + 8 * (int64_t)r;
+  return {at[0], at[1], at[2], at[3], at[4], at[5], at[6], at[7]};
 }
 
 }  // namespace

@@ -42,7 +42,7 @@ __global__ __launch_bounds__(T::kWavesOf * 64) void latent_expand_kernel(const L
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave_outs = wave % WO, wave_tokens = wave / WO;
   const int64_t last = a.tokens - 1;
   const int32_t* const ints = table.ints();
-  const int32_t starts = ints[7 * (int64_t)(lane < table.batch ? lane : table.batch - 1) + 1];         // (of up to 64 requests)
+  const int32_t starts = ints[8 * (int64_t)(lane < table.batch ? lane : table.batch - 1) + 1];         // (of up to 64 requests)
 
   // The workgroup's tiles: all outputs of one tile of tokens after another; or an XCD keeps to its own token tiles, a group of outputs at a time.
   const int of_xcd = (a.token_tiles + kXcds - 1) / kXcds;
@@ -87,9 +87,9 @@ __global__ __launch_bounds__(T::kWavesOf * 64) void latent_expand_kernel(const L
       int l = lo, h = hi;
       while (l < h) {
         const int mid = (l + h + 1) >> 1;
-        if (ints[7 * (int64_t)mid + 1] <= tok) l = mid; else h = mid - 1;
+        if (ints[8 * (int64_t)mid + 1] <= tok) l = mid; else h = mid - 1;
       }
-      pos[i] = tok - ints[7 * (int64_t)l + 1];
+      pos[i] = tok - ints[8 * (int64_t)l + 1];
       page[i] = a.block_tables[(int64_t)l * a.max_pages + pos[i] / kPageTokens];
     }
   };

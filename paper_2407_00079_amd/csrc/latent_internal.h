@@ -57,7 +57,7 @@ struct LatentPrefillArgs {
   float* o_parts;                            // most_tiles > 0: rows of partial results, [rows][heads][head_dim]
   float2* ml_parts;                          // their references and sums
   int64_t k_token, k_head, v_token, v_head;  // bytes
-  int32_t heads, head_dim, latent_dim, batch, max_pages, items;
+  int32_t heads, head_dim, latent_dim, batch, max_pages, items, cut_tiles;
   int32_t most_tiles;                        // key tiles of a piece at most; 0: row tiles are whole
   float scale_log2e;
 };

@@ -101,7 +101,7 @@ void fill_latent_table(const int32_t* prefix_lens, const int32_t* new_lens, int3
   int64_t q_off = 0, k_off = 0;
   for (int32_t r = 0; r < batch; ++r) {
     const int32_t before = prefix_lens != nullptr ? prefix_lens[r] : 0;
-    to[r] = {(int32_t)q_off, (int32_t)k_off, before, new_lens[r], 0, 0, r};
+    to[r] = {(int32_t)q_off, (int32_t)k_off, before, new_lens[r], 0, 0, r, 0};
     q_off += new_lens[r];
     k_off += (int64_t)before + new_lens[r];
   }
@@ -109,16 +109,18 @@ void fill_latent_table(const int32_t* prefix_lens, const int32_t* new_lens, int3
 
 void fill_latent_items(int32_t batch, int32_t most_tiles, LatentReq* reqs) {
   std::stable_sort(reqs, reqs + batch, [](const LatentReq& a, const LatentReq& b) { return (int64_t)a.prefix + a.chunk > (int64_t)b.prefix + b.chunk; });
-  int64_t items = 0, parts = 0;
+  int64_t items = 0, parts = 0, cut = 0;
   for (int32_t r = 0; r < batch; ++r) {
     const int32_t tiles = latent_row_tiles(reqs[r].chunk);
     reqs[r].item_off = (int32_t)items;
     reqs[r].part_off = (int32_t)parts;
+    reqs[r].cut_off = (int32_t)cut;
     if (most_tiles == 0) items += tiles;
     else
       for (int32_t t = 0; t < tiles; ++t) {
         const int pieces = latent_pieces(latent_key_tiles(reqs[r].prefix, reqs[r].chunk, t), most_tiles);
         items += pieces;
+        cut += pieces > 1;
         parts += pieces > 1 ? (int64_t)pieces * latent_tile_height(reqs[r].chunk, t) : 0;
       }
   }
@@ -148,14 +150,14 @@ PrefillTimes times_of(const mc_latent_params* p) {
   return p->head_dim == 128 ? PrefillTimes{1.15, 0.9 / kLatentRows, 5.0, 4.0, 0.5e-6} : PrefillTimes{0.75, 0.75 / kLatentRows, 4.0, 4.0, 0.5e-6};
 }
 struct PrefillCut {
-  int64_t items, part_rows;
+  int64_t items, cut_tiles, part_rows;
   int32_t longest;                           // key tiles of a row tile
   double us;                                 // negative: more work items than are worth looking at
 };
 // The launch as the compute units that each head has take the work items, in their order, one by one.
 PrefillCut cut_into(const mc_latent_params* p, const std::vector<LatentReq>& reqs, int32_t most_tiles) {
   const PrefillTimes t = times_of(p);
-  PrefillCut cut = {0, 0, 0, 0};
+  PrefillCut cut = {0, 0, 0, 0, 0};
   const size_t units = (size_t)std::max(1, kLatentWgs / p->num_heads);
   std::priority_queue<double, std::vector<double>, std::greater<double>> ends;
   double last = 0;
@@ -163,9 +165,10 @@ PrefillCut cut_into(const mc_latent_params* p, const std::vector<LatentReq>& req
     for (int32_t i = latent_row_tiles(r.chunk) - 1; i >= 0; --i) {
       const int keys = latent_key_tiles(r.prefix, r.chunk, i), pieces = latent_pieces(keys, most_tiles), rows = latent_tile_height(r.chunk, i);
       cut.items += pieces;
+      cut.cut_tiles += pieces > 1;
       cut.part_rows += pieces > 1 ? (int64_t)pieces * rows : 0;
       cut.longest = std::max(cut.longest, keys);
-      if (cut.items > 4 * (int64_t)units) return {0, 0, cut.longest, -1.0};
+      if (cut.items > 4 * (int64_t)units) return {0, 0, 0, cut.longest, -1.0};
       for (int piece = 0; piece < pieces; ++piece) {
         double from = 0;
         if (ends.size() == units) {
@@ -204,6 +207,7 @@ LatentPrefillLayout latent_prefill_layout(const mc_latent_params* p, const int32
     }
     if (l.most_tiles > 0) {
       l.items = best.items;
+      l.cut_tiles = best.cut_tiles;
       l.part_rows = best.part_rows;
     }
   }

@@ -46,7 +46,7 @@ LatentDecodeLayout latent_decode_layout(const mc_latent_params* p, int32_t batch
 // Expanded attention: how row tiles are cut along the keys, and where partial results lie.
 struct LatentPrefillLayout {
   int32_t most_tiles;                        // key tiles of a piece at most; 0: nothing is cut
-  int64_t items, part_rows;                  // pieces of row tiles; rows of partial results of each head
+  int64_t items, cut_tiles, part_rows;       // pieces of row tiles; row tiles of more than one; rows of partial results of each head
   size_t o_off, ml_off, total;
 };
 LatentPrefillLayout latent_prefill_layout(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch);

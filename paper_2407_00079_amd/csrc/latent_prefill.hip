@@ -501,49 +501,75 @@ __global__ __launch_bounds__(512) void latent_prefill_kernel(const LatentPrefill
   }
 }
 
-// Row tiles that were cut: a workgroup joins 32 rows of one head, 8 lanes a row.
-constexpr int kJoinRows = 32;
+// Row tiles that were cut (of a request those of most keys, its last ones): a workgroup joins 8 rows of one head, 32 lanes a row: 8 share out the
+// columns, times four that take every fourth part.
+constexpr int kJoinRows = 8;
 template <int D, typename Table>
-__global__ __launch_bounds__(kJoinRows * 8) void latent_prefill_join_kernel(const LatentPrefillArgs a, const Table table) {
-  constexpr int kPer = D / 8, kVecs = kPer / 4, kAtOnce = 4;
-  const int head = blockIdx.x % a.heads;
-  const Item it = item_of<true>(a, table, blockIdx.x / a.heads);
-  const int rows = latent_tile_height(it.rq.chunk, it.row_tile), row = blockIdx.y * kJoinRows + threadIdx.x / 8, col = threadIdx.x % 8 * 4;
-  if (it.pieces == 1 || it.piece != 0 || row >= rows) return;
-  auto part = [&](int i) __attribute__((always_inline)) { return (it.part_row + (int64_t)i * rows + row) * a.heads + head; };
-  float top = -INFINITY;
-  for (int i = 0; i < it.pieces; ++i) top = fmaxf(top, a.ml_parts[part(i)].x);
-  const float from = top == -INFINITY ? 0.f : top;           // (every score is -inf or NaN)
-  float l = 0.f;
+__global__ __launch_bounds__(kJoinRows * 32) void latent_prefill_join_kernel(const LatentPrefillArgs a, const Table table) {
+  constexpr int kVecs = D / 32, kShares = 4;
+  const int head = blockIdx.x % a.heads, at_cut = blockIdx.x / a.heads;
+  const LatentReq rq = request(table, find_request<7>(table.ints(), table.batch, at_cut));
+  int64_t part_row = rq.part_off;
+  int row_tile = latent_row_tiles(rq.chunk) - 1;
+  auto pieces_of = [&](int t) __attribute__((always_inline)) { return latent_pieces(latent_key_tiles(rq.prefix, rq.chunk, t), a.most_tiles); };
+  for (int k = at_cut - rq.cut_off; k > 0; --k, --row_tile) part_row += (int64_t)pieces_of(row_tile) * latent_tile_height(rq.chunk, row_tile);
+  const int pieces = pieces_of(row_tile), rows = latent_tile_height(rq.chunk, row_tile);
+  const int row = blockIdx.y * kJoinRows + threadIdx.x / 32, share = threadIdx.x / 8 % kShares, col = threadIdx.x % 8 * 4;
+  if (row >= rows) return;
+  float top = -INFINITY, l = 0.f;
   f32x4 x[kVecs];
 #pragma unroll
   for (int v = 0; v < kVecs; ++v) x[v] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int i0 = 0; i0 < it.pieces; i0 += kAtOnce) {
-    f32x4 o[kAtOnce][kVecs];
-    float2 ml[kAtOnce];
+  auto reference = [](float m) __attribute__((always_inline)) { return m == -INFINITY ? 0.f : m; };      // (every score so far is -inf or NaN)
+  auto take = [&](int first, auto many) __attribute__((always_inline)) {         // so many parts, all asked for at once
+    constexpr int N = decltype(many)::value;
+    f32x4 o[N][kVecs];
+    float2 ml[N];
+    float next = top;
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      const int64_t at = part(i0 + k < it.pieces ? i0 + k : i0);
+    for (int k = 0; k < N; ++k) {
+      const int64_t at = (part_row + (int64_t)(first + kShares * k) * rows + row) * a.heads + head;
       ml[k] = a.ml_parts[at];
 #pragma unroll
       for (int v = 0; v < kVecs; ++v) o[k][v] = *reinterpret_cast<const f32x4*>(a.o_parts + at * D + col + 32 * v);
     }
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k)
-      if (i0 + k < it.pieces) {
-        const float weight = __builtin_amdgcn_exp2f(ml[k].x - from);
-        l += weight * ml[k].y;
+    for (int k = 0; k < N; ++k) next = fmaxf(next, ml[k].x);
+    const float from = reference(next), before = __builtin_amdgcn_exp2f(top - from);
+    l *= before;
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v) x[v] += weight * o[k][v];
-      }
+    for (int v = 0; v < kVecs; ++v) x[v] *= before;
+    top = next;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float weight = __builtin_amdgcn_exp2f(ml[k].x - from);
+      l += weight * ml[k].y;
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v) x[v] += weight * o[k][v];
+    }
+  };
+  int i = share;
+  for (; i + 3 * kShares < pieces; i += 4 * kShares) take(i, Int<4>{});
+  for (; i < pieces; i += kShares) take(i, Int<1>{});
+#pragma unroll
+  for (int step = 8; step < 8 * kShares; step *= 2) {        // (always in the same order: the two sides add the same two numbers)
+    const float there = __shfl_xor(top, step, 64), both = fmaxf(top, there), from = reference(both);
+    const float mine = __builtin_amdgcn_exp2f(top - from), other = __builtin_amdgcn_exp2f(there - from);
+    l = l * mine + __shfl_xor(l, step, 64) * other;
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[v][e] = x[v][e] * mine + __shfl_xor(x[v][e], step, 64) * other;
+    top = both;
   }
-  const int64_t to = (int64_t)(it.rq.q_off + it.row_tile * kLatentRows + row) * a.heads + head;
+  if (share != 0) return;
+  const int64_t to = (int64_t)(rq.q_off + row_tile * kLatentRows + row) * a.heads + head;
   const float inv = 1.0f / l;
 #pragma unroll
   for (int v = 0; v < kVecs; ++v) {
     bf16x4 y;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = (__bf16)(x[v][i] * inv);
+    for (int e = 0; e < 4; ++e) y[e] = (__bf16)(x[v][e] * inv);
     *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(a.out) + to * D + col + 32 * v) = y;
   }
   if (a.lse != nullptr && col == 0) a.lse[to] = (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
@@ -556,7 +582,7 @@ hipError_t enqueue(const LatentPrefillArgs& args, const Table& table, hipStream_
     latent_prefill_kernel<D, false><<<wgs, 512, 0, stream>>>(args, table);
   } else {
     latent_prefill_kernel<D, true><<<wgs, 512, 0, stream>>>(args, table);
-    latent_prefill_join_kernel<D><<<dim3(wgs, kLatentRows / kJoinRows), kJoinRows * 8, 0, stream>>>(args, table);
+    latent_prefill_join_kernel<D><<<dim3(args.cut_tiles * args.heads, kLatentRows / kJoinRows), kJoinRows * 32, 0, stream>>>(args, table);
   }
   return hipGetLastError();
 }

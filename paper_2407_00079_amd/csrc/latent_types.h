@@ -18,6 +18,7 @@ struct LatentReq {
   int32_t item_off;                          // its first work item
   int32_t part_off;                          // its first row of partial results
   int32_t row;                               // of the block table
+  int32_t cut_off;                           // its first row tile of more than one piece
 };
 // at most kMaxArgEntries requests travel with the launch, behind them entries that no search ends at
 struct LatentReqTable {

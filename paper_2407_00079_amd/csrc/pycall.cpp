@@ -9,13 +9,15 @@
 //     I  a list of n integers as int32[n], or an integer address
 //     Q  a list of n integers as int64[n], or an integer address
 //
-// and two looks at tensors before a call, made here because a dozen of them through Python are a sixth of a small call (one new
+// and three looks at tensors before a call, made here because a dozen of them through Python are a sixth of a small call (one new
 // token a row, rotation and append, launch included: 8.9 us of the host, so 7.6):
 //
 //   misfit(device, dtype, tensor, least, tensor, least, ...) -> the first that is not a dense tensor of dtype on the device with
 //                                                              at least so many elements, or -1
 //   row_stride(device, dtype, tensor, tokens, heads, dim) -> elements from token to token of [tokens, heads, dim] or
 //                                                              [tokens, heads * dim] whose heads are dense, -1 if it is none
+//   head_strides(device, dtype, tensor, tokens, heads, dim) -> elements from token to token and from head to head of [tokens, heads, dim]
+//                                                              whose rows are dense, None if it is none
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <stdint.h>
@@ -201,9 +203,32 @@ PyObject* row_stride(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return PyLong_FromLongLong(!fits ? -1 : tokens > 1 ? step[0] : heads * dim);
 }
 
+PyObject* head_strides(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  long long device, tokens, heads, dim;
+  if (n != 6) {
+    PyErr_SetString(PyExc_TypeError, "head_strides(device, dtype, tensor, tokens, heads, dim)");
+    return nullptr;
+  }
+  device = PyLong_AsLongLong(args[0]), tokens = PyLong_AsLongLong(args[3]), heads = PyLong_AsLongLong(args[4]), dim = PyLong_AsLongLong(args[5]);
+  if (PyErr_Occurred()) return nullptr;
+  const int there = lies(args[2], device, args[1]);
+  if (there < 0) return nullptr;
+  if (there == 0) Py_RETURN_NONE;
+  PyObject* shape = PyObject_GetAttr(args[2], g_shape);
+  PyObject* stride = shape == nullptr ? nullptr : PyObject_CallMethodNoArgs(args[2], g_stride);
+  long long size[3] = {0, 0, 0}, step[3] = {0, 0, 0};
+  const int dims = integers(shape, size), steps = integers(stride, step);
+  Py_XDECREF(shape);
+  Py_XDECREF(stride);
+  if (PyErr_Occurred()) return nullptr;
+  if (dims != 3 || steps != 3 || size[0] != tokens || size[1] != heads || size[2] != dim || step[2] != 1) Py_RETURN_NONE;
+  return Py_BuildValue("LL", tokens > 1 ? step[0] : heads * dim, heads > 1 ? step[1] : dim);
+}
+
 PyMethodDef g_methods[] = {{"call", (PyCFunction)(void (*)(void))call, METH_FASTCALL, "call(address, kinds, *arguments) -> status"},
                            {"misfit", (PyCFunction)(void (*)(void))misfit, METH_FASTCALL, "misfit(device, dtype, tensor, least, ...) -> index or -1"},
                            {"row_stride", (PyCFunction)(void (*)(void))row_stride, METH_FASTCALL, "row_stride(device, dtype, tensor, tokens, heads, dim) -> stride or -1"},
+                           {"head_strides", (PyCFunction)(void (*)(void))head_strides, METH_FASTCALL, "head_strides(device, dtype, tensor, tokens, heads, dim) -> strides or None"},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_mccall", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
