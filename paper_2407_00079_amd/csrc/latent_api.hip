@@ -31,7 +31,7 @@ mc_status place_latent(const int32_t* prefix_lens, const int32_t* new_lens, int3
 }
 
 // false: no memory for it
-bool lay_prefill_out(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, LatentPrefillLayout* lay) {
+bool plan_prefill(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, LatentPrefillLayout* lay) {
   try {
     *lay = latent_prefill_layout(p, prefix_lens, new_lens, batch);
     return true;
@@ -184,9 +184,9 @@ mc_status mc_latent_expand_paged(const mc_latent_params* p, const void* weight, 
 size_t mc_latent_prefill_attn_workspace_bytes(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch) {
   LatentLens lens;
   if (check_latent(p) != MC_OK || batch < 0 || (batch > 0 && (prefix_lens == nullptr || new_lens == nullptr))) return 0;
-  if (check_latent_lens(prefix_lens, new_lens, batch, &lens) != MC_OK) return 0;
+  if (check_latent_lens(prefix_lens, new_lens, batch, &lens) != MC_OK || lens.total_keys > kMostLatentTokens) return 0;
   LatentPrefillLayout lay;
-  return lay_prefill_out(p, prefix_lens, new_lens, batch, &lay) ? lay.total : 0;
+  return plan_prefill(p, prefix_lens, new_lens, batch, &lay) ? lay.total : 0;
 }
 
 mc_status mc_latent_prefill_attn_paged(const mc_latent_params* p, const void* q, const void* k, const void* v, const int64_t* strides,
@@ -205,6 +205,7 @@ mc_status mc_latent_prefill_attn_paged(const mc_latent_params* p, const void* q,
   st = check_latent_lens(prefix_lens, new_lens, batch, &lens);
   if (st != MC_OK) return st;
   if (lens.total_new == 0) return MC_OK;
+  if (lens.total_keys > kMostLatentTokens) return MC_ERR_RANGE;
   if (max_pages_per_req < lens.need_pages) return MC_ERR_SHAPE;
   for (const void* at : {q, k, v, pool, (const void*)out, (const void*)block_tables})
     if (at == nullptr) return MC_ERR_NULL;
@@ -212,7 +213,7 @@ mc_status mc_latent_prefill_attn_paged(const mc_latent_params* p, const void* q,
     if (!aligned16(at)) return MC_ERR_ALIGN;
   if (!aligned4(block_tables) || !aligned4(lse)) return MC_ERR_ALIGN;
   LatentPrefillLayout lay;
-  if (!lay_prefill_out(p, prefix_lens, new_lens, batch, &lay)) return MC_ERR_HIP;
+  if (!plan_prefill(p, prefix_lens, new_lens, batch, &lay)) return MC_ERR_HIP;
   if ((int64_t)batch * max_pages_per_req > INT32_MAX || lay.items * p->num_heads > INT32_MAX) return MC_ERR_RANGE;
   if (workspace == nullptr || workspace_bytes < lay.total) return MC_ERR_WORKSPACE;
 

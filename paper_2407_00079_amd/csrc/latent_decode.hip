@@ -72,8 +72,9 @@ struct Line {
     for (;;) {                               // (x lies in one of the lane's rows)
       const int r = at.row + lane, mine = r < batch ? tiles(valid(lens[r])) : 0, upto = before + scan(mine);
       k = __popcll(__builtin_amdgcn_ballot_w64(upto <= x));
-      if (k < 64) {
-        at.row += k;
+      if (k < 64 || r - lane + 64 >= batch) {                // (the second: lengths that changed under the call; it ends all the same)
+        k = k < 64 ? k : 63;
+        at.row += at.row + k < batch ? k : batch - 1 - at.row;
         before = __builtin_amdgcn_readlane(upto - mine, k);
         break;
       }

@@ -83,7 +83,7 @@ mc_status check_latent_lens(const int32_t* prefix_lens, const int32_t* new_lens,
     const int32_t before = prefix_lens != nullptr ? prefix_lens[r] : 0;
     if (before < 0 || new_lens[r] < 0) return MC_ERR_SHAPE;
     const int64_t len = (int64_t)before + new_lens[r];
-    if (len > INT32_MAX - 1024) return MC_ERR_RANGE;
+    if (len > kMostLatentTokens) return MC_ERR_RANGE;
     if (new_lens[r] > 0) {
       out->need_pages = std::max(out->need_pages, (int32_t)((len + 15) / 16));
       out->most_keys = std::max(out->most_keys, (int32_t)len);
@@ -91,8 +91,7 @@ mc_status check_latent_lens(const int32_t* prefix_lens, const int32_t* new_lens,
     out->total_new += new_lens[r];
     out->total_keys += len;
   }
-  // (tokens are counted with 32 bits)
-  return out->total_keys > INT32_MAX - 1024 ? MC_ERR_RANGE : MC_OK;
+  return out->total_new > kMostLatentTokens ? MC_ERR_RANGE : MC_OK;
 }
 
 size_t latent_table_bytes(int32_t batch) { return ((size_t)batch * sizeof(LatentReq) + 15) & ~(size_t)15; }

@@ -23,9 +23,11 @@ mc_status latent_append_strides(const mc_latent_params* p, const int64_t* stride
 mc_status check_latent_append(const mc_latent_params* p, const void* q, const void* kv, const AppendStrides& s, const void* norm,
                               const void* q_out, const void* pool, const int32_t* block_tables, int64_t tokens);
 
+// What a call may count with 32 bits: tiles of up to 256 tokens end behind the last one.
+constexpr int64_t kMostLatentTokens = INT32_MAX - 1024;
 // Lengths of a batch with `prefix_lens` null for none before: sign and range checks, sums, most pages of a request that has any new tokens.
 struct LatentLens {
-  int64_t total_new, total_keys;
+  int64_t total_new, total_keys;             // total_keys: to be checked by who counts keys
   int32_t need_pages, most_keys;             // most_keys: of a request with new tokens
 };
 mc_status check_latent_lens(const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, LatentLens* out);
