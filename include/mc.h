@@ -775,7 +775,7 @@ mc_status mc_latent_append_decode(const mc_latent_params* p, const mc_rope_param
  *
  * Slots at or past what a token sees are never used as values (they may hold NaN).  Products on the matrix cores, fp32 accumulation and softmax;
  * probabilities are rounded to bf16 before they meet c, as in the bf16 prefill attention.  A key that a token sees and whose score is NaN or +inf
- * makes the token's row NaN; one whose score is -inf, with c finite, counts for nothing.  The same lengths and inputs give the same bits.  Nothing is allocated, uploaded or waited for; the call can be captured.
+ * makes the token's row NaN; one whose score is -inf, with c finite, counts for nothing (no others: 0, lse -inf).  The same lengths and inputs give the same bits.  Nothing is allocated, uploaded or waited for; the call can be captured.
  * batch * tokens * H > 2^26 or batch * max_pages_per_req > 2^31 - 1 is MC_ERR_RANGE; batch == 0 enqueues nothing.
  */
 size_t mc_latent_decode_attn_workspace_bytes(const mc_latent_params* p, int32_t batch, int32_t tokens);
@@ -819,7 +819,7 @@ mc_status mc_latent_expand_paged(const mc_latent_params* p, const void* weight, 
  *
  * A key that a row does not see is never used as a value for it (its k, v and r may hold NaN).  Products on the matrix cores, fp32
  * accumulation and softmax; probabilities rounded to bf16 before they meet v.  More than 64 requests are uploaded (no stream capture then).
- * No new tokens: nothing is enqueued.  A key whose score is -inf, with v finite, counts for nothing.
+ * No new tokens: nothing is enqueued.  A key whose score is -inf, with v finite, counts for nothing (no others: 0, lse -inf).
  */
 size_t mc_latent_prefill_attn_workspace_bytes(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch);
 mc_status mc_latent_prefill_attn_paged(const mc_latent_params* p, const void* q, const void* k, const void* v, const int64_t* strides,

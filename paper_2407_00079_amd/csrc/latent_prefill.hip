@@ -10,7 +10,7 @@
 //     and V^T fragments come by two transposing LDS reads in the same order.  Each fragment read feeds two instructions.
 //   * Softmax in one pass in fp32, its reference lagging behind the largest score by at most 2^8.
 //   * On the diagonal, keys that a row does not see get probability 0, and elements of V that are not finite are taken out of the products there;
-//     where a block has any, the rows that see them get them by a loop of their own (a product of 0 and an infinity would be NaN).
+//     where a block has any, a second product counts those that a row sees, and puts their sum in (0 times an infinity would be NaN).
 #include "attn_narrow_device.h"
 #include "latent_device.h"
 
@@ -489,7 +489,7 @@ __global__ __launch_bounds__(512) void latent_prefill_kernel(const LatentPrefill
       if (g == 0) a.ml_parts[to] = float2{m[rt], all};
       continue;
     }
-    const float inv = 1.0f / all;                            // (a row sees its own key at least)
+    const float inv = all == 0.f ? 0.f : 1.0f / all;         // (every score is -inf: 0)
 #pragma unroll
     for (int dt = 0; dt < kDTiles; ++dt) {
       bf16x4 v;
@@ -564,7 +564,7 @@ __global__ __launch_bounds__(kJoinRows * 32) void latent_prefill_join_kernel(con
   }
   if (share != 0) return;
   const int64_t to = (int64_t)(rq.q_off + row_tile * kLatentRows + row) * a.heads + head;
-  const float inv = 1.0f / l;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
   for (int v = 0; v < kVecs; ++v) {
     bf16x4 y;

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from latent_util import (BF16, DEV, P, PAGE, absorbed_reference, assert_near, gen, lens_tensor, params, randn, tables, workspace)
+from latent_util import (BF16, DEV, P, PAGE, absorbed_reference, assert_near, attended, gen, lens_tensor, params, randn, rows_of, tables, workspace)
 from paper_2407_00079_amd import binding as B
 
 pytestmark = pytest.mark.gpu
@@ -119,3 +119,26 @@ def test_same_bits_whatever_stands_around():
         ws.fill_(fill)
         again = attend(p, q, pool, table, lens, 1, ws=ws)
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_scores_of_minus_infinity():
+    """A key whose score is -inf counts for nothing; a row that has no others is 0, whether stretches cut it or not."""
+    g = gen(15)
+    lens, heads = [1, 70, 3000], 16
+    table, pages = tables(g, lens)
+    pool, q = randn(g, pages, PAGE, 512 + P), randn(g, 3, heads, 512 + P)
+    q[:, :, 515] = q[:, :, 515].abs() + 0.5
+    whole = pool.clone()
+    for lost in (2, 1):                                        # every second key, every key
+        for r, n in enumerate(lens):
+            at = torch.arange(0, n, lost, device=DEV)
+            pool[table[r, at // PAGE].long(), at % PAGE, 515] = -float("inf")
+        out, lse = attend(params(heads, 512, 128, pages), q, pool, table, lens, 1)
+        for r, n in enumerate(lens):
+            if lost == 1 or n == 1:
+                assert bool((out[r] == 0).all()) and bool((lse[r] == -float("inf")).all())
+                continue
+            rows = rows_of(whole, table, r, n)[1::2]
+            want, want_lse, out_off, lse_off = attended(q[r].double(), rows, rows[:, :512], 192 ** -0.5)
+            assert_near(lse[r], want_lse, lse_off, "lse")
+            assert_near(out[r], want, out_off, "out")

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from latent_util import (BF16, DEV, F32, HALF, P, PAGE, assert_near, gen, params, prefill_reference, randn, rows_of, tables, workspace)
+from latent_util import (BF16, DEV, F32, HALF, P, PAGE, assert_near, attended, gen, params, prefill_reference, randn, rows_of, tables, workspace)
 from paper_2407_00079_amd import binding as B
 
 pytestmark = pytest.mark.gpu
@@ -102,3 +102,29 @@ def test_growing_scores():
     p, q, k, v, pool, table = inputs(9, 2, 512, 128, [1200], [40])
     k *= (0.1 + 20.0 * torch.arange(1240, device=DEV) / 1240)[:, None, None].to(BF16)
     check(p, q, k, v, pool, table, [1200], [40])
+
+
+@pytest.mark.parametrize("prefix,new", [([0], [130]), ([2500], [40])])
+def test_scores_of_minus_infinity(prefix, new):
+    """A key whose score is -inf counts for nothing; a row that has no others is 0, whether its tile was cut along the keys or not."""
+    p, q, k, v, pool, table = inputs(12, 2, 512, 128, prefix, new)
+    n = prefix[0] + new[0]
+    q[:, :, 7] = q[:, :, 7].abs() + 0.5
+    few = torch.arange(0, n, 3, device=DEV)
+    lost = torch.ones(n, dtype=torch.bool, device=DEV)
+    k[few, :, 7] = -float("inf")
+    lost[few] = False
+    out, lse = attend(p, q, k, v, pool, table, prefix, new)
+    shared = rows_of(pool, table, 0, n)[:, 512:]
+    for i in range(new[0]):
+        seen = torch.nonzero(lost[: prefix[0] + i + 1])[:, 0]
+        if len(seen) == 0:
+            assert bool((out[i] == 0).all()) and bool((lse[i] == -float("inf")).all())
+            continue
+        keys = torch.cat((k[seen].double().transpose(0, 1), shared[seen].expand(2, -1, -1)), 2)
+        want, want_lse, out_off, lse_off = attended(q[i].double(), keys, v[seen].double().transpose(0, 1), 192 ** -0.5)
+        assert_near(lse[i], want_lse, lse_off, "lse")
+        assert_near(out[i], want, out_off, "out")
+    k[:, :, 7] = -float("inf")
+    out, lse = attend(p, q, k, v, pool, table, prefix, new)
+    assert bool((out == 0).all()) and bool((lse == -float("inf")).all())
