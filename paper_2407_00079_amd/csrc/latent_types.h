@@ -35,18 +35,17 @@ constexpr int latent_tiles(int64_t stacked) { return (int)((stacked + latent_til
 // workgroups a tile has
 constexpr int latent_stretches(int tiles) { return tiles >= kLatentWgs ? 1 : kLatentWgs / tiles; }
 // How many stretches have work (decode_begin says where each begins, decode_wave_of which has a place).  A tile takes its workgroup 2.4 to 2.7 us, and what
-// is joined behind takes 0.05 to 0.08 us a part of a row, so t tiles of r rows are done soonest by about sqrt(30 t r) stretches; from 64 tiles on
-// two tiles each at least, since every stretch begins and ends.  us, stretches of 1 / 2 / 4 / 8 tiles at least, 16 query rows: one row of 1000 keys
-// 10.1 / 11.1 / 13.1 / 17.4, 8192 13.5 / 12.4 / 13.5 / 17.3, 32768 19.9 / 20.1 / 17.6 / 19.5; 4 rows of 4096 14.8 / 13.1 / 13.9 / 17.7, 16 of 1000
-// 14.2 / 13.0 / 14.2 / 18.6, 64 of 500 15.9 / 16.0 / 15.3 / 17.4.
+// is joined behind takes 0.05 to 0.08 us a part of a row, so t tiles of r rows are done soonest by about sqrt(30 t r) stretches.  Short rows are
+// cut least by stretches of one tile, although each begins and ends: us, one tile at least / two, 16 and 64 query rows, 50 lengths of 1 to 256 tokens
+// 12.4 / 15.2, 24.3 / 29.1; 20 to 640 12.7 / 15.4, 22.4 / 26.5; 10 to 2048 13.2 / 14.3, 24.1 / 26.3; two tiles of 64 rows, 135 tiles of keys for 128
+// workgroups 26.0 / 31.7, 160 30.5 / 30.0.  (Lengths that are all the same meet the ends of two: 64 rows of 128 11.6 / 10.1, 23.9 / 17.9.)
 inline
 #ifdef __HIP__
 __host__ __device__
 #endif
 int latent_used(int total, int rows, int stretches) {
   const float best = __builtin_sqrtf(30.0f * (float)total * (float)rows);
-  int used = total <= 64 ? total : total <= 128 ? 64 : total / 2;
-  used = used < stretches ? used : stretches;
+  const int used = total < stretches ? total : stretches;
   return best < (float)used ? (int)best : used;
 }
 // A row that several stretches have parts of: the first of them, and how many follow.  more == 0: nothing is to be joined.

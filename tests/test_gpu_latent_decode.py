@@ -41,7 +41,7 @@ def test_heads(heads, latent):
     check(heads, latent, 128, [1, 15, 16, 17, 63, 64, 65, 300], seed=heads)
 
 
-@pytest.mark.parametrize("lens", [[1], [64], [65], [1000], [5000, 1, 4999], [0, 3, 0, 0, 130, 0], [0, 0], [20000], [129] * 300, [1] * 70, [-5, 20, 10 ** 9, 7]])
+@pytest.mark.parametrize("lens", [[1], [64], [65], [1000], [5000, 1, 4999], [0, 3, 0, 0, 130, 0], [0, 0], [20000], [129] * 300, [1] * 70, [64, 65] * 50, [30] * 300, [-5, 20, 10 ** 9, 7]])
 @pytest.mark.parametrize("heads", [16, 64])
 def test_lengths(heads, lens):
     g = len(lens) + heads
