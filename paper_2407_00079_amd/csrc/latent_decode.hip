@@ -424,10 +424,10 @@ template <int R, int WAVES, bool SHARED>
 __global__ __launch_bounds__(WAVES * 64) void latent_join_kernel(const LatentDecodeArgs a, int tile_rows) {
   __shared__ f32x4 outs[SHARED ? WAVES : 1][64];
   __shared__ float2 sums[SHARED ? WAVES : 1][16];
-  const LatentChain chain = a.chains[blockIdx.x];
+  const LatentChain chain = a.chains[blockIdx.z];
   if (chain.more == 0) return;
   const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, wave = threadIdx.x >> 6;
-  const int cols = SHARED ? (int)blockIdx.z : (int)blockIdx.z * WAVES + wave;      // which 16 of them
+  const int cols = SHARED ? (int)blockIdx.x : (int)blockIdx.x * WAVES + wave;      // which 16 of them
   const int row0 = blockIdx.y * 16, tile = row0 / tile_rows, in_tile = row0 - tile * tile_rows;
   const int n = chain.more + 1;
   constexpr int kStep = SHARED ? WAVES : 1, kAtOnce = 4;
@@ -499,9 +499,9 @@ hipError_t enqueue(int rows, const LatentDecodeArgs& args, hipStream_t stream) {
   else if (rows == 32) latent_decode_kernel<R, 2><<<wgs, kWaves * 64, 0, stream>>>(args);
   else if (rows == 64) latent_decode_kernel<R, 4><<<wgs, kWaves * 64, 0, stream>>>(args);
   else return hipErrorInvalidValue;
-  const int pieces = (args.stacked + 15) / 16;
-  if (args.n_chains * pieces < 32) latent_join_kernel<R, 16, true><<<dim3(args.n_chains, pieces, R / 16), 16 * 64, 0, stream>>>(args, rows);
-  else latent_join_kernel<R, 4, false><<<dim3(args.n_chains, pieces, R / 16 / 4), 4 * 64, 0, stream>>>(args, rows);
+  const int pieces = (args.stacked + 15) / 16;               // (columns fastest, so that each XCD has its share of every row, long ones too)
+  if (args.n_chains * pieces < 32) latent_join_kernel<R, 16, true><<<dim3(R / 16, pieces, args.n_chains), 16 * 64, 0, stream>>>(args, rows);
+  else latent_join_kernel<R, 4, false><<<dim3(R / 16 / 4, pieces, args.n_chains), 4 * 64, 0, stream>>>(args, rows);
   return hipGetLastError();
 }
 
