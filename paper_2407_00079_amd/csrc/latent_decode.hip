@@ -101,11 +101,12 @@ struct Shape {
   static constexpr int kRows = 16 * MT;
   static constexpr int kKeyGroups = MT == 4 ? 2 : 4, kKeyTiles = kTile / 16 / kKeyGroups, kScoring = MT * kKeyGroups;      // waves that make scores
   static constexpr int kColTiles = R / 16 / kWaves;   // 16-column tiles of the output a wave has
-  static constexpr int kPRowB = kTile * 2 + 16;              // 16 rows of a column spread over the banks
-  // A tile in LDS: block by block of 64 columns, in each 64 rows of 128 bytes, the 16-byte granules of row r at their place ^ swizzle(r).  The
-  // 256 bytes of all banks are two rows: reads of one granule of 16 rows, and transposing reads of 32 bytes of rows 0-3 and 8-11
-  // (4-7 and 12-15), meet every bank once.
-  static __device__ __forceinline__ int swizzle(int r) { return (r & 2) | ((r >> 1) & 4) | ((r >> 2) & 1); }
+  static constexpr int kPRowB = kTile * 2;                   // (granules as in a tile)
+  // A tile in LDS: block by block of 64 columns, in each 64 rows of 128 bytes, the 16-byte granules of row r at their place ^ swizzle(r).  The 256
+  // bytes of all banks are two rows.  LDS serves lanes 0-3, 12-15, 20-23 and 24-27 of a 16-byte read at once (4-11, 16-19, 28-31 ..), and 32 lanes of
+  // a transposing one: one granule of rows 0-3 and 12-15 with the next one of rows 4-11, and 32 bytes of rows 0-3 and 8-11 (4-7 and 12-15), meet every
+  // bank once.  (With reads of keys two by two instead: 64 query rows, 1427 tiles of keys twice 55.3 us for 51.7.)
+  static __device__ __forceinline__ int swizzle(int r) { return (r & 2) | (((r >> 1) ^ r) & 4) | ((r >> 2) & 1); }
   struct Shared {
     char tile[2][kTileB];
     char p[kRows][kPRowB];
@@ -161,7 +162,8 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
     const int r0 = 8 * g + (j >> 2);
     const uint32_t v_lane = base + (R / 8 * w / 64) * S::kBlockB + r0 * 128 + (((((j & 3) >> 1) ^ S::swizzle(r0)) ^ (R / 8 * w % 64 / 8)) << 4) + ((j & 1) << 3);
     const uint32_t p_base = base + (uint32_t)__builtin_offsetof(typename S::Shared, p);
-    const uint32_t p_read = p_base + j * S::kPRowB + g * 16, p_write = p_base + (16 * mine + j) * S::kPRowB + (16 * KT * kg + 4 * g) * 2;
+    const uint32_t p_read = p_base + j * S::kPRowB + ((g ^ S::swizzle(j)) << 4);
+    const uint32_t p_write = p_base + (16 * mine + j) * S::kPRowB + (((2 * KT * kg + (g >> 1)) ^ S::swizzle(j)) << 4) + (g & 1) * 8;
 
     bf16x8 qf[S::kSteps];                                    // of the wave's rows of scores
     f32x4 o[S::kColTiles][MT];                               // of all rows: the wave's columns
@@ -225,7 +227,7 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
           }
           const uint32_t low = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[0], p[1]}, bf16x2));
           const uint32_t high = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[2], p[3]}, bf16x2));
-          *reinterpret_cast<MC_LDS u32x2*>(p_write + kt * 32) = u32x2{low, high};
+          *reinterpret_cast<MC_LDS u32x2*>(p_write ^ (kt << 5)) = u32x2{low, high};
         }
       };
       if (scoring) {
@@ -317,7 +319,7 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
         auto value = [&](int u) __attribute__((always_inline)) {
           const int half = u / S::kColTiles, t = u % S::kColTiles;
           const uint32_t at0 = (v_lane ^ ((t & 3) << 5)) + buf * S::kTileB + (t >> 2) * S::kBlockB + half * (32 * 128);
-          const uint32_t at1 = (v_lane ^ ((t & 3) << 5) ^ 16) + buf * S::kTileB + (t >> 2) * S::kBlockB + half * (32 * 128) + 4 * 128;
+          const uint32_t at1 = (v_lane ^ ((t & 3) << 5) ^ 80) + buf * S::kTileB + (t >> 2) * S::kBlockB + half * (32 * 128) + 4 * 128;
           const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((MC_LDS bf16x4*)(uintptr_t)at0);
           const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((MC_LDS bf16x4*)(uintptr_t)at1);
           return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -329,7 +331,7 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
           const int t = u % S::kColTiles;
           if (t == 0) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m) pf[m] = *reinterpret_cast<MC_LDS const bf16x8*>(p_read + 16 * m * S::kPRowB + u / S::kColTiles * 64);
+            for (int m = 0; m < MT; ++m) pf[m] = *reinterpret_cast<MC_LDS const bf16x8*>((p_read ^ (u / S::kColTiles << 6)) + 16 * m * S::kPRowB);
           }
 #pragma unroll
           for (int m = 0; m < MT; ++m) o[t][m] = mma(ring[u % kAhead], pf[m], o[t][m]);

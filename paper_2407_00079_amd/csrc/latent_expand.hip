@@ -16,11 +16,6 @@ namespace {
 constexpr int kStepB = 64, kBufs = 4, kAhead = kBufs - 1;    // bytes of a row that a step takes: 32 columns
 constexpr int kCopyRows = 1024 / kStepB;                     // of a copy instruction
 
-// The four 16-byte granules of a row are stored at their place ^ swizzle, four rows make the 256 bytes of all banks, and the 16 rows of a fragment
-// meet every bank once: consecutive tokens, and outputs 8 (j / 4) + j % 4
-__device__ __forceinline__ int token_swizzle(int row) { return (row >> 2) & 3; }
-__device__ __forceinline__ int out_swizzle(int row) { return (row >> 3) & 3; }
-
 // WO x WT waves, each of 64 outputs and TT tiles of 16 tokens
 template <int WO, int WT, int TT>
 struct Tile {
@@ -28,6 +23,13 @@ struct Tile {
   static constexpr int kTokensB = kTokens * kStepB, kBufB = kTokensB + kOuts * kStepB;
   static constexpr int kTokenCopies = kTokens / kCopyRows / kWavesOf, kOutCopies = kOuts / kCopyRows / kWavesOf;       // of a wave
   static_assert(kTokenCopies * kCopyRows * kWavesOf == kTokens && kOutCopies * kCopyRows * kWavesOf == kOuts, "whole copies");
+  // The four 16-byte granules of a row are stored at their place ^ swizzle; four rows make the 256 bytes of all banks, and a fragment reads 16 rows:
+  // consecutive tokens, and outputs 8 (j / 4) + j % 4.  LDS serves lanes 0-3, 12-15, 20-23 and 24-27 (4-11, 16-19, 28-31 ..) at once, which meet every bank
+  // once by -quad.  Large tiles read two by two, 4 cycles more a read, and are no slower for it, the other way round: 131072 tokens, 4096 outputs, R 512
+  // 650 us against 685, R 256 435 and 435; 1425 tokens, 1280 outputs, R 256 (small tiles) 6.0 against 5.75.
+  static __device__ __forceinline__ int swizzle(int quad) { return (kWavesOf == 8 ? quad : -quad) & 3; }
+  static __device__ __forceinline__ int token_swizzle(int row) { return swizzle(row >> 2); }
+  static __device__ __forceinline__ int out_swizzle(int row) { return swizzle(row >> 3); }
 };
 // tiles of outputs that an XCD goes over with its token tiles before the next ones: their weights stay in its cache
 constexpr int kOutGroup = 4;
@@ -98,12 +100,12 @@ __global__ __launch_bounds__(T::kWavesOf * 64) void latent_expand_kernel(const L
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
       const int row = (wave * NT + i) * kCopyRows + lane / 4;
-      from[i] = reinterpret_cast<const char*>(a.pool) + ((int64_t)page[i] * kPageTokens + pos[i] % kPageTokens) * kRowB + ((lane % 4 ^ token_swizzle(row)) << 4);
+      from[i] = reinterpret_cast<const char*>(a.pool) + ((int64_t)page[i] * kPageTokens + pos[i] % kPageTokens) * kRowB + ((lane % 4 ^ T::token_swizzle(row)) << 4);
     }
 #pragma unroll
     for (int i = 0; i < NO; ++i) {
       const int row = (wave * NO + i) * kCopyRows + lane / 4, out = out0 + row < a.outs ? row : a.outs - 1 - out0;
-      weight_at[i] = (uint32_t)(out * (R * 2) + ((lane % 4 ^ out_swizzle(row)) << 4));
+      weight_at[i] = (uint32_t)(out * (R * 2) + ((lane % 4 ^ T::out_swizzle(row)) << 4));
     }
     weights = reinterpret_cast<const char*>(a.weight) + (int64_t)out0 * (R * 2);
   };
@@ -120,11 +122,11 @@ __global__ __launch_bounds__(T::kWavesOf * 64) void latent_expand_kernel(const L
     static_assert(n < 64, "vmcnt");
     __builtin_amdgcn_s_waitcnt(0x0F70 | (n & 15) | (n >> 4 << 14));
   };
-  const uint32_t token_lane = base + (wave_tokens * TT * 16 + j) * kStepB + ((g ^ token_swizzle(j)) << 4);
+  const uint32_t token_lane = base + (wave_tokens * TT * 16 + j) * kStepB + ((g ^ T::token_swizzle(j)) << 4);
   // row m of output tile o is output 32 (o / 2) + 8 (m / 4) + 4 (o % 2) + m % 4: a lane ends up with 8 consecutive ones of each pair of tiles, four
   // lanes with 64 bytes
   const int out_row = 8 * (j >> 2) + (j & 3);
-  const uint32_t out_lane = base + T::kTokensB + (wave_outs * 64 + out_row) * kStepB + ((g ^ out_swizzle(out_row)) << 4);
+  const uint32_t out_lane = base + T::kTokensB + (wave_outs * 64 + out_row) * kStepB + ((g ^ T::out_swizzle(out_row)) << 4);
 
   int token_tile = 0, out_tile = 0;
   int64_t seq = next_of(blockIdx.x, &token_tile, &out_tile);
