@@ -7,6 +7,12 @@
 // in between three steps ahead; each lane keeps the addresses of its token rows, found from the request table and the block table, so that
 // a tile may hold any number of requests.  The outputs are the rows of the instruction.  Workgroups stay and take one tile after another: the next tile's rows are looked up during a tile, its
 // first steps are copied under the last ones, and the stores of a tile are not waited for before the next begins.
+//
+// What bounds it: 131072 tokens, 16 heads of 128, R 512 597 us, 920 TFLOP/s; the library's product of that shape, from a dense left side, 684 to 696.  398 us
+// of it are what its largest product makes, the rest mostly the 1074 MB of outputs, which the products do not hide.  Workgroups that stay 714 -> 700; three
+// steps ahead and outputs by groups 670; whole 128-byte lines to a store instead of halves, which had written 1296 MB, 616; every bank once and groups of
+// eight 597.  Tried, no faster: two workgroups of four waves a compute unit.  Below 192 large tiles small ones: 1425 tokens, 10 heads of 64, R 256 5.7 us
+// where large ones took 13.5.
 #include "attn_narrow_device.h"
 #include "latent_device.h"
 
@@ -24,15 +30,15 @@ struct Tile {
   static constexpr int kTokenCopies = kTokens / kCopyRows / kWavesOf, kOutCopies = kOuts / kCopyRows / kWavesOf;       // of a wave
   static_assert(kTokenCopies * kCopyRows * kWavesOf == kTokens && kOutCopies * kCopyRows * kWavesOf == kOuts, "whole copies");
   // The four 16-byte granules of a row are stored at their place ^ swizzle; four rows make the 256 bytes of all banks, and a fragment reads 16 rows:
-  // consecutive tokens, and outputs 8 (j / 4) + j % 4.  LDS serves lanes 0-3, 12-15, 20-23 and 24-27 (4-11, 16-19, 28-31 ..) at once, which meet every bank
-  // once by -quad.  Large tiles read two by two, 4 cycles more a read, and are no slower for it, the other way round: 131072 tokens, 4096 outputs, R 512
-  // 650 us against 685, R 256 435 and 435; 1425 tokens, 1280 outputs, R 256 (small tiles) 6.0 against 5.75.
-  static __device__ __forceinline__ int swizzle(int quad) { return (kWavesOf == 8 ? quad : -quad) & 3; }
+  // consecutive tokens, and outputs 8 (j / 4) + j % 4.  LDS serves lanes 0-3, 12-15, 20-23 and 24-27 (4-11, 16-19, 28-31 ..) at once: granule g of quads 0
+  // and 3 of the rows with g ^ 1 of 1 and 2, which by -quad meet every bank once (two by two by quad: 131072 tokens 616 us against 607).
+  static __device__ __forceinline__ int swizzle(int quad) { return -quad & 3; }
   static __device__ __forceinline__ int token_swizzle(int row) { return swizzle(row >> 2); }
   static __device__ __forceinline__ int out_swizzle(int row) { return swizzle(row >> 3); }
 };
-// tiles of outputs that an XCD goes over with its token tiles before the next ones: their weights stay in its cache
-constexpr int kOutGroup = 4;
+// Tiles of outputs that an XCD goes over with its token tiles before the next ones: their weights, 1 or 2 MiB, stay in its cache.  Of 4 / 8 / 16, 131072
+// tokens, R 512 607 / 600 / 627 us, R 256 427 / 412 / 426.
+constexpr int kOutGroup = 8;
 
 template <int R, typename T, int WO, int WT, int TT, typename Table>
 __global__ __launch_bounds__(T::kWavesOf * 64) void latent_expand_kernel(const LatentExpandArgs a, const Table table) {
@@ -194,27 +200,45 @@ __global__ __launch_bounds__(T::kWavesOf * 64) void latent_expand_kernel(const L
     const int64_t t0 = (int64_t)token_tile * T::kTokens;
     const int out = out_tile * T::kOuts + wave_outs * 64;
     const bool whole = t0 + T::kTokens - 1 <= last && out < a.outs;
+    // lanes 2 i and 2 i + 1 exchange a half, so that a store has all 128 bytes of a token: the even one's first, then the odd one's
+    const bool odd = (j & 1) != 0;
     auto put = [&](auto past) __attribute__((always_inline)) {
+      const int64_t tok0 = t0 + wave_tokens * (TT * 16) + (j & ~1);
+      const int left = last - tok0 < TT * 16 ? (int)(last - tok0) : TT * 16;
+      __bf16* to0 = reinterpret_cast<__bf16*>(a.kv) + tok0 * a.outs + out + (odd ? 32 : 0) + 8 * g;
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
-        const int64_t tok = t0 + wave_tokens * (TT * 16) + 16 * t + j;
-        if (!whole && tok > last) continue;
-        __bf16* const to = reinterpret_cast<__bf16*>(a.kv) + tok * a.outs + out + 8 * g;
+        u32x4 v[2];
 #pragma unroll
         for (int o = 0; o < 4; o += 2) {
-          bf16x8 v;
+          bf16x8 x;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            v[i] = (__bf16)acc[o][t][i];
-            v[4 + i] = (__bf16)acc[o + 1][t][i];
+            x[i] = (__bf16)acc[o][t][i];
+            x[4 + i] = (__bf16)acc[o + 1][t][i];
           }
-          if constexpr (decltype(past)::value != 0) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4*>(to + 16 * o));
-          else *reinterpret_cast<bf16x8*>(to + 16 * o) = v;
+          v[o / 2] = __builtin_bit_cast(u32x4, x);
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t got = (uint32_t)__builtin_amdgcn_mov_dpp((int)(odd ? v[0][i] : v[1][i]), 0xB1, 0xF, 0xF, true);
+          v[0][i] = odd ? got : v[0][i];
+          v[1][i] = odd ? v[1][i] : got;
+        }
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const bool some = whole || 16 * t + p <= left;
+          u32x4* const to = reinterpret_cast<u32x4*>(to0);
+          to0 += (int64_t)(p == 0 ? 1 : 15) * a.outs;
+          if (!some) continue;
+          if constexpr (decltype(past)::value != 0) __builtin_nontemporal_store(v[p], to);
+          else *to = v[p];
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
     };
-    // An output that the last-level cache does not hold passes it by: 1074 MB 790 -> 670 us, but 134 MB 82 -> 100.  (The empty statements keep the
-    // compiler from making one of the two, which costs the hint.)
+    // An output that the last-level cache does not hold passes it by: 1074 MB 760 -> 616 us, 537 MB 348 -> 331, 134 MB 84 either way.  (The empty statements
+    // keep the compiler from making one of the two, which costs the hint.)
     if (out < a.outs) {
       if (a.past_caches) {
         asm volatile("; past the caches");
