@@ -9,6 +9,9 @@
 // What is rotated are rows of 64 numbers, H of a token's queries and one of its cache row: 8 lanes of 16 bytes each, 32 rows a workgroup (or
 // 64), their angles computed once a token and pair into LDS.  A latent row is a wave's (R = 512) or half a wave's; those workgroups
 // stand behind the others in the same launch.
+//
+// What bounds it: HBM.  8192 tokens of 16 heads 52 MB, 11.5 us = 4.6 TB/s with the launch's ends (a copy of this size 8.7 + 3); 4085 tokens of 128 heads 143 MB,
+// 28.0 us, 5.1 TB/s; 64 single tokens 3.4 us, a launch and dependent loads.
 #include "latent_device.h"
 
 namespace mc {

@@ -2,19 +2,31 @@
 //
 //   x(j) = scale q . [c(j), r(j)],      out = sum_j softmax_j(x) c(j),      lse = log sum_j exp(x(j))
 //
-// One cache row serves all heads, as key and as value.  A workgroup has 16, 32 or 64 stacked query rows (row = token * H + head) and walks
-// tiles of 64 keys through LDS, read from memory once a workgroup and from LDS once as keys and once as values by each 16 or 32 rows:
+// One cache row serves all heads, as key and as value.  A workgroup of 8 waves has 16, 32 or 64 stacked query rows (row = token * H + head) and walks
+// tiles of 64 keys through LDS, two buffers, copied without registers in between:
 //
-//   * Four waves a group of rows.  Wave w makes the scores S^T = K Q^T of keys 16 w .. 16 w + 15 of the tile for all rows of its group
-//     (queries stay in registers), the probabilities meet in LDS, and it then adds the tile's share of columns R/4 w .. of the output,
-//     O^T += C^T P^T: every element of the tile is read once for each product, whatever the number of waves.
-//   * A softmax runs in one pass in fp32.  Its reference is one for all four waves and lags behind the largest score by at most 2^8: probabilities
+//   * A wave makes the scores S^T = K Q^T of 16 rows and a group of the tile's keys (16, or 32 of 64 rows; queries stay in registers), the
+//     probabilities meet in LDS, and each wave then adds the tile's share of R/8 columns of the output, for all rows, O^T += C^T P^T: values are read once a
+//     workgroup, keys once each 16 rows.
+//   * A softmax runs in one pass in fp32.  Its reference is one for all waves and lags behind the largest score by at most 2^8: probabilities
 //     are formed against it before the waves have met, and only where a score outgrew it the waves exchange maxima, scale what they
 //     have and form the tile's probabilities again (flags that all waves of the workgroup read behind the same barrier).
 //   * Keys behind what a row sees get probability 0, and what is not finite in a row's last tiles is cleared, once it has been used as keys, before
 //     it is used as values: 0 times whatever an unwritten slot holds stays 0.  (A key that counts and is not finite has made its score so.)
 //   * The tiles of all rows stand in one line, of which each workgroup takes an equal stretch; it finds its place from the lengths.  Rows that a stretch's
-//     end cuts leave partial results in the workspace, and a second kernel joins them in the order of the line.
+//     end cuts leave partial results in the workspace, in the order of the registers, and a second kernel joins them in the order of the line.
+//
+// What bounds it: with 16 rows a workgroup the cache's bytes (one row of 131071 keys, 16 heads: 151 MB in 27.9 us, 5.4 TB/s; 128 rows of 704 to 1408 keys
+// 2.75 us a tile, 6.9 TB/s), behind it a join of 7.4 us.  With 64 rows (128 heads, or 4 tokens of 16) what a tile takes from end to end of a wave: 2.5 us
+// at R 512 (1.55 at R 256), of which matrix products 0.9 and LDS reads 1.4, one after the other for the most part, since two buffers of 72 KiB leave no
+// room for a second workgroup: 51 rows of 120 to 8000 keys, 128 heads, 50.5 us and 9.6 in the join; 64 rows of 4
+// tokens of 16 heads 38.1 and 9.0.
+//
+// Rows of a workgroup: a tile of R 512 takes 2.5 to 2.75 us whether it has 16, 32 or 64 rows, so as few workgroups as 64 rows make; 16 or 32 where that is
+// all there is, for fewer rows of queries and partial results (two tiles a row, nothing cut: 13.9 / 19.5 / 22.0 us a call).  Tried, slower: groups of four waves
+// for each 16 rows; scores of two row tiles a wave (R 512 does not fit the registers, R 256 the same 1.55 us); halves of 32 keys in four buffers, the
+// values of one while the next one's scores are made (3.0 us a tile of R 256, 4.6 of R 512: a half takes as long from end to end); no maxima unless a
+// probability reaches 2 (the same).
 #include "attn_narrow_device.h"
 #include "latent_device.h"
 
@@ -105,7 +117,7 @@ struct Shape {
   // A tile in LDS: block by block of 64 columns, in each 64 rows of 128 bytes, the 16-byte granules of row r at their place ^ swizzle(r).  The 256
   // bytes of all banks are two rows.  LDS serves lanes 0-3, 12-15, 20-23 and 24-27 of a 16-byte read at once (4-11, 16-19, 28-31 ..), and 32 lanes of
   // a transposing one: one granule of rows 0-3 and 12-15 with the next one of rows 4-11, and 32 bytes of rows 0-3 and 8-11 (4-7 and 12-15), meet every
-  // bank once.  (With reads of keys two by two instead: 64 query rows, 1427 tiles of keys twice 55.3 us for 51.7.)
+  // bank once.  (With reads two by two: 64 query rows, 51 rows of 128 heads, 55.3 us for 51.7.)
   static __device__ __forceinline__ int swizzle(int r) { return (r & 2) | (((r >> 1) ^ r) & 4) | ((r >> 2) & 1); }
   struct Shared {
     char tile[2][kTileB];

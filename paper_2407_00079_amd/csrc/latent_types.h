@@ -29,7 +29,7 @@ struct LatentReqTable {
 // query rows (row = token * H + head) take equal stretches of it.
 constexpr int kLatentTileKeys = 64;
 constexpr int kLatentWgs = 256;              // one a compute unit
-// stacked query rows of a tile, by how many there are: 16, 32 or 64 (latent_decode.hip says what each measured)
+// stacked query rows of a tile, by how many there are: 16, 32 or 64 (latent_decode.hip says what a tile takes)
 constexpr int latent_tile_rows(int64_t stacked) { return stacked <= 16 ? 16 : stacked <= 32 ? 32 : 64; }
 constexpr int latent_tiles(int64_t stacked) { return (int)((stacked + latent_tile_rows(stacked) - 1) / latent_tile_rows(stacked)); }
 // workgroups a tile has
