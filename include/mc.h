@@ -815,7 +815,8 @@ mc_status mc_latent_expand_paged(const mc_latent_params* p, const void* weight, 
  *   prefix_lens, new_lens  host [batch], as in mc_prefill_attn_paged
  *   out      dev   [total_new_tokens, H, D] dense, every row written
  *   lse      dev   [total_new_tokens, H] fp32, or NULL
- *   workspace  dev  >= mc_latent_prefill_attn_workspace_bytes(...) for the same lengths, 16-byte aligned
+ *   workspace  dev  >= mc_latent_prefill_attn_workspace_bytes(...) for the same lengths, 16-byte aligned; calls that may overlap, and captured graphs that
+ *                   may, need one each
  *
  * A key that a row does not see is never used as a value for it (its k, v and r may hold NaN).  Products on the matrix cores, fp32
  * accumulation and softmax; probabilities rounded to bf16 before they meet v.  More than 64 requests are uploaded (no stream capture then).

@@ -19,8 +19,7 @@
 // What bounds it: with 16 rows a workgroup the cache's bytes (one row of 131071 keys, 16 heads: 151 MB in 27.9 us, 5.4 TB/s; 128 rows of 704 to 1408 keys
 // 2.75 us a tile, 6.9 TB/s), behind it a join of 7.4 us.  With 64 rows (128 heads, or 4 tokens of 16) what a tile takes from end to end of a wave: 2.5 us
 // at R 512 (1.55 at R 256), of which matrix products 0.9 and LDS reads 1.4, one after the other for the most part, since two buffers of 72 KiB leave no
-// room for a second workgroup: 51 rows of 120 to 8000 keys, 128 heads, 50.5 us and 9.6 in the join; 64 rows of 4
-// tokens of 16 heads 38.1 and 9.0.
+// room for a second workgroup: 51 rows of 120 to 8000 keys, 128 heads, 50.5 us and 9.6 in the join; 64 rows of 4 tokens of 16 heads 38.1 and 9.0.
 //
 // Rows of a workgroup: a tile of R 512 takes 2.5 to 2.75 us whether it has 16, 32 or 64 rows, so as few workgroups as 64 rows make; 16 or 32 where that is
 // all there is, for fewer rows of queries and partial results (two tiles a row, nothing cut: 13.9 / 19.5 / 22.0 us a call).  Tried, slower: groups of four waves

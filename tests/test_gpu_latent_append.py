@@ -90,3 +90,18 @@ def test_in_place_and_by_head():
     B.mc_latent_append_paged(p, rope, q.transpose(0, 1).contiguous().transpose(0, 1), kv, None, out.transpose(0, 1), pool, table, [0], [50], ws)
     B.mc_latent_append_paged(p, rope, q, kv, None, q, pool, table, [0], [50], ws)
     assert torch.equal(q, out.transpose(0, 1))
+
+
+@pytest.mark.parametrize("tokens", [1, 5])
+def test_most_heads(tokens):
+    g = gen(tokens)
+    lens, heads = [1, 20, 0, 33], 1024
+    table, pages = tables(g, lens)
+    T = len(lens) * tokens
+    q, kv = randn(g, T, heads, P), randn(g, T, 256 + P)
+    q_out = torch.full((T, heads, P), 7.0, dtype=BF16, device=DEV)
+    pool = randn(g, pages, PAGE, 256 + P)
+    before, rope = pool.clone(), rope_of(B.MC_ROPE_HALF)
+    B.mc_latent_append_decode(params(heads, 256, 64, pages), rope, q, kv, None, q_out, pool, table, lens_tensor(lens), tokens)
+    pos = np.concatenate([n - tokens + np.arange(tokens) if n > 0 else np.full(tokens, -1) for n in lens])
+    check_results(rope, 256, q, kv, None, q_out, pool, before, table, pos, np.repeat(np.arange(len(lens)), tokens))

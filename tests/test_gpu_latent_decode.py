@@ -142,3 +142,18 @@ def test_scores_of_minus_infinity():
             want, want_lse, out_off, lse_off = attended(q[r].double(), rows, rows[:, :512], 192 ** -0.5)
             assert_near(lse[r], want_lse, lse_off, "lse")
             assert_near(out[r], want, out_off, "out")
+
+
+@pytest.mark.parametrize("heads,tokens", [(1024, 1), (1000, 3), (1024, 16)])
+def test_most_heads(heads, tokens):
+    check(heads, 256, 64, [70, 3, 0], tokens=tokens, seed=heads)
+
+
+def test_thousands_of_rows():
+    """More rows than 64 a lane, of which few have keys: first, last, in between, and many beside each other."""
+    lens = [0] * 4300
+    for r in (0, 1, 63, 64, 70, 2047, 4299):
+        lens[r] = 1 + 17 * (r % 11)
+    lens[900: 1200] = [5] * 300
+    lens[3000] = 700
+    check(16, 256, 64, lens, seed=33)

@@ -129,3 +129,8 @@ def test_scores_of_minus_infinity(prefix, new):
     k[:, :, 7] = -float("inf")
     out, lse = attend(p, q, k, v, pool, table, prefix, new)
     assert bool((out == 0).all()) and bool((lse == -float("inf")).all())
+
+
+def test_most_heads():
+    prefix, new = [40, 0], [3, 20]
+    check(*inputs(14, 1024, 256, 64, prefix, new), prefix, new)
