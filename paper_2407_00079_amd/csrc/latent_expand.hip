@@ -2,17 +2,17 @@
 //
 //   kv[t, o] = sum_i c(t)_i W[o, i],      t over the tokens of whole requests back to back, o over 2 head_dim outputs of each head
 //
-// A matrix product whose left side lies in pages, on 16x16x32 matrix instructions: a wave makes 64 outputs of 128 tokens, a workgroup of 8 waves 256 x
-// 256 (few tokens: 4 waves of 64 x 32, 128 x 64).  Tokens and weights come through LDS in steps of 32 columns, four buffers, copied without registers
-// in between three steps ahead; each lane keeps the addresses of its token rows, found from the request table and the block table, so that
-// a tile may hold any number of requests.  The outputs are the rows of the instruction.  Workgroups stay and take one tile after another: the next tile's rows are looked up during a tile, its
-// first steps are copied under the last ones, and the stores of a tile are not waited for before the next begins.
+// A matrix product whose left side lies in pages, on 16x16x32 matrix instructions: a wave makes 64 outputs of 128 tokens, a workgroup of 8 waves
+// 256 x 256 (fewer tokens: 64 x 64, 256 x 128; few: 4 waves of 64 x 32, 128 x 64).  Tokens and weights come through LDS in steps of 32 columns, four
+// buffers, copied without registers in between three steps ahead; each lane keeps the addresses of its token rows, found from the request table and the
+// block table, so that a tile may hold any number of requests.  The outputs are the rows of the instruction.  Workgroups stay and take one tile after
+// another: the next tile's rows are looked up during a tile, its first steps are copied under the last ones, and the stores of a tile are not waited
+// for before the next begins.
 //
 // What bounds it: 131072 tokens, 16 heads of 128, R 512 597 us, 920 TFLOP/s; the library's product of that shape, from a dense left side, 684 to 696.  398 us
 // of it are what its largest product makes, the rest mostly the 1074 MB of outputs, which the products do not hide.  Workgroups that stay 714 -> 700; three
 // steps ahead and outputs by groups 670; whole 128-byte lines to a store instead of halves, which had written 1296 MB, 616; every bank once and groups of
-// eight 597.  Tried, no faster: two workgroups of four waves a compute unit.  Below 192 large tiles small ones: 1425 tokens, 10 heads of 64, R 256 5.7 us
-// where large ones took 13.5.
+// eight 597.  Tried, no faster: two workgroups of four waves a compute unit.  Which tiles when: see enqueue.
 #include "attn_narrow_device.h"
 #include "latent_device.h"
 
@@ -271,8 +271,13 @@ void enqueue_tiles(LatentExpandArgs args, const Table& table, hipStream_t stream
 }
 template <int R, typename Table>
 void enqueue(const LatentExpandArgs& args, const Table& table, hipStream_t stream) {
-  const int64_t tiles = ((args.tokens + 255) / 256) * ((args.outs + 255) / 256);
-  if (tiles < 192) enqueue_tiles<R, 2, 2, 2>(args, table, stream);
+  // 64 tokens of 128 outputs, or 128 or 256 of 256, by how many of the second there would be: the first while there are too few, the last, which reads
+  // least, once rounds of workgroups are many.  us, first / second / third, 16 heads of 128 and R 512: 1000 tokens 11.0 / 11.1 / 17.0, 2000 18.3 / 14.8 / 19.7,
+  // 5000 36 / 30 / 34, 7000 - / 42.5 / 40.3, 16384 112 / 86 / 79; 10 heads of 64, R 256: 2600 7.0 / 8.0 / 11.4, 8192 13.4 / 13.6 / 15, 16384 22.3 / 19.2 / 22.9,
+  // 60000 - / 57.5 / 60; 16 of 128, 65536 - / 190 / 178.
+  const int64_t tiles = ((args.tokens + 127) / 128) * ((args.outs + 255) / 256);
+  if (tiles < kLatentWgs / 2) enqueue_tiles<R, 2, 2, 2>(args, table, stream);
+  else if (tiles < (R == 256 ? 10 : 3) * kLatentWgs) enqueue_tiles<R, 4, 2, 4>(args, table, stream);
   else enqueue_tiles<R, 4, 2, 8>(args, table, stream);
 }
 template <typename Table>

@@ -10,7 +10,8 @@ pytestmark = pytest.mark.gpu
 
 @pytest.mark.parametrize("latent,head_dim,heads,lens", [
     *((*x, lens) for x in ((512, 128, 16), (256, 64, 10), (512, 64, 1), (256, 128, 3), (512, 128, 2)) for lens in ([1], [256], [257], [15, 0, 33, 500, 1], [1] * 100, [0, 7] * 40)),
-    (512, 128, 64, [700, 0, 33, 1, 290]), (256, 64, 130, [513, 2, 254]), (256, 128, 64, [3] * 341), (512, 64, 1, [50000, 1, 3])])
+    (512, 128, 64, [700, 0, 33, 1, 290]), (256, 64, 130, [513, 2, 254]), (256, 128, 64, [3] * 341), (512, 64, 1, [50000, 1, 3]),
+    (512, 128, 128, [513, 2, 254, 0, 30]), (256, 128, 512, [300, 0, 299]), (512, 64, 256, [1] * 770)])
 def test_expand(latent, head_dim, heads, lens):
     g = gen(heads + len(lens))
     table, pages = tables(g, lens)
