@@ -17,7 +17,7 @@
 //     end cuts leave partial results in the workspace, in the order of the registers, and a second kernel joins them in the order of the line.
 //
 // What bounds it: with 16 rows a workgroup the cache's bytes (one row of 131071 keys, 16 heads: 151 MB in 27.9 us, 5.4 TB/s; 128 rows of 704 to 1408 keys
-// 2.75 us a tile, 6.9 TB/s), behind it a join of 7.4 us.  With 64 rows (128 heads, or 4 tokens of 16) what a tile takes from end to end of a wave: 2.5 us
+// 2.75 us a tile, 6.9 TB/s), behind it a join of 5.6 us.  With 64 rows (128 heads, or 4 tokens of 16) what a tile takes from end to end of a wave: 2.5 us
 // at R 512 (1.55 at R 256), of which matrix products 0.9 and LDS reads 1.4, one after the other for the most part, since two buffers of 72 KiB leave no
 // room for a second workgroup: 51 rows of 120 to 8000 keys, 128 heads, 50.5 us and 9.6 in the join; 64 rows of 4 tokens of 16 heads 38.1 and 9.0.
 //
@@ -505,6 +505,85 @@ __global__ __launch_bounds__(WAVES * 64) void latent_join_kernel(const LatentDec
   if (a.lse != nullptr && cols == 0 && g == 0) a.lse[to] = (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
+// One row of the batch, of at most 16 stacked rows: 128 bytes of each part (8 rows by 4 columns) a workgroup, so that all compute units read.  A wave
+// takes 8 parts at once, 8 lanes each.  us a call, this way / by 16 waves: 131072 keys, 16 heads 33.4 / 35.4, 16384 13.8 / 14.7, 1024 10.0 / 10.0; of two
+// pieces 26.7 / 27.5 for 65536 keys, but 12.6 / 12.3 for 256.
+constexpr int kOneWaves = 4;
+template <int R>
+__global__ __launch_bounds__(kOneWaves * 64) void latent_join_one_kernel(const LatentDecodeArgs a) {
+  constexpr int kParts = kOneWaves * 8, kAtOnce = 4;
+  __shared__ f32x4 outs[kOneWaves][8];
+  __shared__ float2 sums[kOneWaves][8];
+  const LatentChain chain = a.chains[0];
+  if (chain.more == 0) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 7;
+  const int cols = blockIdx.x >> 3, g = (blockIdx.x & 7) >> 1, j = 8 * (blockIdx.x & 1) + i;       // which 16 columns, which 4 of them; the row
+  const int n = chain.more + 1;
+  auto reference = [](float m) __attribute__((always_inline)) { return m == -INFINITY ? 0.f : m; };      // (every score is -inf or NaN)
+  float top = -INFINITY, l = 0.f;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int part = wave * 8 + lane / 8; part < n; part += kParts * kAtOnce) {
+    f32x4 v[kAtOnce];
+    float2 ml[kAtOnce];
+    float next = top;
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {                      // (past the last part: the first of them again, with no weight)
+      const int p = part + k * kParts < n ? part + k * kParts : part;
+      const int64_t at = ((int64_t)(chain.first + p) * 2 + (p == 0 ? 1 : 0)) * 16;
+      v[k] = *reinterpret_cast<const f32x4*>(a.o_parts + at * R + cols * 256 + (g * 16 + j) * 4);
+      ml[k] = a.ml_parts[at + j];
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) next = fmaxf(next, ml[k].x);
+    const float from = reference(next), before = __builtin_amdgcn_exp2f(top - from);
+    l *= before;
+    x *= before;
+    top = next;
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      if (part + k * kParts >= n) break;
+      const float weight = __builtin_amdgcn_exp2f(ml[k].x - from);
+      l += weight * ml[k].y;
+      x += weight * v[k];
+    }
+  }
+#pragma unroll
+  for (int step = 8; step < 64; step *= 2) {                 // (the two sides add the same two numbers)
+    const float there = __shfl_xor(top, step, 64), both = fmaxf(top, there), from = reference(both);
+    const float mine = __builtin_amdgcn_exp2f(top - from), other = __builtin_amdgcn_exp2f(there - from);
+    l = l * mine + __shfl_xor(l, step, 64) * other;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = x[e] * mine + __shfl_xor(x[e], step, 64) * other;
+    top = both;
+  }
+  if (lane < 8) {
+    outs[wave][i] = x;
+    sums[wave][i] = float2{top, l};
+  }
+  __syncthreads();
+  if (threadIdx.x >= 8) return;
+#pragma unroll
+  for (int w = 1; w < kOneWaves; ++w) top = fmaxf(top, sums[w][i].x);
+  const float from = reference(top);
+  l = 0.f;
+  x = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < kOneWaves; ++w) {
+    const float2 ml = sums[w][i];
+    const float weight = __builtin_amdgcn_exp2f(ml.x - from);
+    l += weight * ml.y;
+    x += weight * outs[w][i];
+  }
+  if (j >= a.stacked) return;
+  const int64_t to = (int64_t)chain.row * a.stacked + j;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  bf16x4 y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = (__bf16)(x[e] * inv);
+  *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(a.out) + to * R + cols * 16 + 4 * g) = y;
+  if (a.lse != nullptr && cols == 0 && g == 0) a.lse[to] = (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
 template <int R>
 hipError_t enqueue(int rows, const LatentDecodeArgs& args, hipStream_t stream) {
   const int wgs = args.tiles * args.stretches;
@@ -513,7 +592,8 @@ hipError_t enqueue(int rows, const LatentDecodeArgs& args, hipStream_t stream) {
   else if (rows == 64) latent_decode_kernel<R, 4><<<wgs, kWaves * 64, 0, stream>>>(args);
   else return hipErrorInvalidValue;
   const int pieces = (args.stacked + 15) / 16;               // (columns fastest, so that each XCD has its share of every row, long ones too)
-  if (args.n_chains * pieces < 32) latent_join_kernel<R, 16, true><<<dim3(R / 16, pieces, args.n_chains), 16 * 64, 0, stream>>>(args, rows);
+  if (args.n_chains * pieces == 1) latent_join_one_kernel<R><<<R / 16 * 8, kOneWaves * 64, 0, stream>>>(args);      // (rows is 16)
+  else if (args.n_chains * pieces < 32) latent_join_kernel<R, 16, true><<<dim3(R / 16, pieces, args.n_chains), 16 * 64, 0, stream>>>(args, rows);
   else latent_join_kernel<R, 4, false><<<dim3(R / 16 / 4, pieces, args.n_chains), 4 * 64, 0, stream>>>(args, rows);
   return hipGetLastError();
 }

@@ -121,12 +121,13 @@ def test_same_bits_whatever_stands_around():
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
 
 
-def test_scores_of_minus_infinity():
+@pytest.mark.parametrize("lens", [[1, 70, 3000], [5000]])
+def test_scores_of_minus_infinity(lens):
     """A key whose score is -inf counts for nothing; a row that has no others is 0, whether stretches cut it or not."""
     g = gen(15)
-    lens, heads = [1, 70, 3000], 16
+    heads = 16
     table, pages = tables(g, lens)
-    pool, q = randn(g, pages, PAGE, 512 + P), randn(g, 3, heads, 512 + P)
+    pool, q = randn(g, pages, PAGE, 512 + P), randn(g, len(lens), heads, 512 + P)
     q[:, :, 515] = q[:, :, 515].abs() + 0.5
     whole = pool.clone()
     for lost in (2, 1):                                        # every second key, every key
