@@ -10,19 +10,15 @@ namespace {
 
 using namespace mc::host;
 
-// The request table of a call: in `arg` if it fits, else uploaded to the workspace.  most_tiles: -1, or how attention's work items are cut.
-mc_status place_latent(const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, int32_t most_tiles, void* workspace, hipStream_t stream,
-                       mc::LatentReqTable* arg) {
-  auto fill = [&](mc::LatentReq* to) {
-    fill_latent_table(prefix_lens, new_lens, batch, to);
-    if (most_tiles >= 0) fill_latent_items(batch, most_tiles, to);
-  };
-  if (batch <= mc::kMaxArgEntries) {
+// The request table of a call: in `arg` if it fits, else uploaded to the workspace.  fill: writes at most `entries` of them.
+template <typename Fill>
+mc_status place_latent(int32_t entries, const Fill& fill, void* workspace, hipStream_t stream, mc::LatentReqTable* arg) {
+  if (entries <= mc::kMaxArgEntries) {
     fill(arg->r);
     return MC_OK;
   }
   try {
-    std::vector<mc::LatentReq> reqs((size_t)batch);
+    std::vector<mc::LatentReq> reqs((size_t)entries);
     fill(reqs.data());
     return mc::upload_table(workspace, reqs.data(), sizeof(mc::LatentReq) * reqs.size(), stream);
   } catch (const std::bad_alloc&) {
@@ -88,7 +84,7 @@ mc_status mc_latent_append_paged(const mc_latent_params* p, const mc_rope_params
 
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   mc::LatentReqTable arg = {};
-  st = place_latent(prefix_lens, new_lens, batch, -1, workspace, stream, &arg);
+  st = place_latent(batch, [&](mc::LatentReq* to) { fill_latent_table(prefix_lens, new_lens, batch, to); }, workspace, stream, &arg);
   if (st != MC_OK) return st;
   const mc::LatentAppendArgs args = append_args(p, rope, q, kv, s, norm, q_out, pool, block_tables, max_pages_per_req, lens.total_new);
   return mc::launch_latent_append(args, reinterpret_cast<const mc::LatentReq*>(workspace), batch <= mc::kMaxArgEntries ? &arg : nullptr, batch,
@@ -174,7 +170,7 @@ mc_status mc_latent_expand_paged(const mc_latent_params* p, const void* weight, 
 
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   mc::LatentReqTable arg = {};
-  st = place_latent(nullptr, lens, batch, -1, workspace, stream, &arg);
+  st = place_latent(batch, [&](mc::LatentReq* to) { fill_latent_table(nullptr, lens, batch, to); }, workspace, stream, &arg);
   if (st != MC_OK) return st;
   return mc::launch_latent_expand(args, reinterpret_cast<const mc::LatentReq*>(workspace), batch <= mc::kMaxArgEntries ? &arg : nullptr, stream) == hipSuccess
              ? MC_OK
@@ -219,7 +215,12 @@ mc_status mc_latent_prefill_attn_paged(const mc_latent_params* p, const void* q,
 
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   mc::LatentReqTable arg = {};
-  st = place_latent(prefix_lens, new_lens, batch, lay.most_tiles, workspace, stream, &arg);
+  const int32_t entries = latent_entries(new_lens, batch);
+  auto fill = [&](mc::LatentReq* to) {
+    fill_latent_entries(p, prefix_lens, new_lens, batch, to);
+    fill_latent_items(entries, lay.most_tiles, to);
+  };
+  st = place_latent(entries, fill, workspace, stream, &arg);
   if (st != MC_OK) return st;
   char* const ws = reinterpret_cast<char*>(workspace);
   mc::LatentPrefillArgs args = {};
@@ -227,10 +228,10 @@ mc_status mc_latent_prefill_attn_paged(const mc_latent_params* p, const void* q,
   args.o_parts = reinterpret_cast<float*>(ws + lay.o_off);
   args.ml_parts = reinterpret_cast<float2*>(ws + lay.ml_off);
   args.k_token = 2 * s.k_token, args.k_head = 2 * s.k_head, args.v_token = 2 * s.v_token, args.v_head = 2 * s.v_head;
-  args.heads = p->num_heads, args.head_dim = p->head_dim, args.latent_dim = p->latent_dim, args.batch = batch, args.max_pages = max_pages_per_req;
+  args.heads = p->num_heads, args.head_dim = p->head_dim, args.latent_dim = p->latent_dim, args.batch = entries, args.max_pages = max_pages_per_req;
   args.most_tiles = lay.most_tiles, args.items = (int32_t)lay.items, args.cut_tiles = (int32_t)lay.cut_tiles;
   args.scale_log2e = latent_scale_log2e(p);
-  return mc::launch_latent_prefill(args, reinterpret_cast<const mc::LatentReq*>(workspace), batch <= mc::kMaxArgEntries ? &arg : nullptr, stream) == hipSuccess
+  return mc::launch_latent_prefill(args, reinterpret_cast<const mc::LatentReq*>(workspace), entries <= mc::kMaxArgEntries ? &arg : nullptr, stream) == hipSuccess
              ? MC_OK
              : MC_ERR_HIP;
 }

@@ -106,10 +106,58 @@ void fill_latent_table(const int32_t* prefix_lens, const int32_t* new_lens, int3
   }
 }
 
-void fill_latent_items(int32_t batch, int32_t most_tiles, LatentReq* reqs) {
-  std::stable_sort(reqs, reqs + batch, [](const LatentReq& a, const LatentReq& b) { return (int64_t)a.prefix + a.chunk > (int64_t)b.prefix + b.chunk; });
-  int64_t items = 0, parts = 0, cut = 0;
+namespace {
+// us of a tile of keys (and of each of a row tile's rows in it), of a workgroup's beginning and end, of joining and of a byte of partial results,
+// as measured: head_dim 128 2.0 and 64 1.5 with 256 rows, 1.4 and 0.9 with 64
+struct PrefillTimes {
+  double tile, row, ends, join, part_byte;
+};
+PrefillTimes times_of(const mc_latent_params* p) {
+  return p->head_dim == 128 ? PrefillTimes{1.15, 0.9 / kLatentRows, 5.0, 4.0, 0.5e-6} : PrefillTimes{0.75, 0.75 / kLatentRows, 4.0, 4.0, 0.5e-6};
+}
+// row tiles, where each is an entry; else -1
+int32_t tile_entries(const int32_t* new_lens, int32_t batch) {
+  int64_t tiles = 0;
+  for (int32_t r = 0; r < batch; ++r) tiles += latent_row_tiles(new_lens[r]);
+  return batch <= kMaxArgEntries && tiles <= kMaxArgEntries ? (int32_t)tiles : -1;
+}
+}  // namespace
+
+int32_t latent_entries(const int32_t* new_lens, int32_t batch) {
+  const int32_t tiles = tile_entries(new_lens, batch);
+  return tiles >= 0 ? tiles : batch;
+}
+
+void fill_latent_entries(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, LatentReq* to) {
+  if (tile_entries(new_lens, batch) < 0) {
+    fill_latent_table(prefix_lens, new_lens, batch, to);
+    std::stable_sort(to, to + batch, [](const LatentReq& a, const LatentReq& b) { return (int64_t)a.prefix + a.chunk > (int64_t)b.prefix + b.chunk; });
+    return;
+  }
+  struct Entry {
+    double us;
+    LatentReq req;
+  };
+  Entry tiles[kMaxArgEntries];
+  const PrefillTimes t = times_of(p);
+  int64_t q_off = 0, k_off = 0;
+  int32_t n = 0;
   for (int32_t r = 0; r < batch; ++r) {
+    for (int32_t i = 0; i < latent_row_tiles(new_lens[r]); ++i) {
+      const int32_t done = i * kLatentRows, height = latent_tile_height(new_lens[r], i);
+      tiles[n++] = {latent_key_tiles(prefix_lens[r], new_lens[r], i) * (t.tile + t.row * height),
+                    {(int32_t)(q_off + done), (int32_t)k_off, prefix_lens[r] + done, height, 0, 0, r, 0}};
+    }
+    q_off += new_lens[r];
+    k_off += (int64_t)prefix_lens[r] + new_lens[r];
+  }
+  std::stable_sort(tiles, tiles + n, [](const Entry& a, const Entry& b) { return a.us > b.us; });
+  for (int32_t i = 0; i < n; ++i) to[i] = tiles[i].req;
+}
+
+void fill_latent_items(int32_t entries, int32_t most_tiles, LatentReq* reqs) {
+  int64_t items = 0, parts = 0, cut = 0;
+  for (int32_t r = 0; r < entries; ++r) {
     const int32_t tiles = latent_row_tiles(reqs[r].chunk);
     reqs[r].item_off = (int32_t)items;
     reqs[r].part_off = (int32_t)parts;
@@ -140,14 +188,6 @@ LatentDecodeLayout latent_decode_layout(const mc_latent_params* p, int32_t batch
 }
 
 namespace {
-// us of a tile of keys (and of each of a row tile's rows in it), of a workgroup's beginning and end, of joining and of a byte of partial results,
-// as measured: head_dim 128 2.0 and 64 1.5 with 256 rows, 1.4 and 0.9 with 64
-struct PrefillTimes {
-  double tile, row, ends, join, part_byte;
-};
-PrefillTimes times_of(const mc_latent_params* p) {
-  return p->head_dim == 128 ? PrefillTimes{1.15, 0.9 / kLatentRows, 5.0, 4.0, 0.5e-6} : PrefillTimes{0.75, 0.75 / kLatentRows, 4.0, 4.0, 0.5e-6};
-}
 struct PrefillCut {
   int64_t items, cut_tiles, part_rows;
   int32_t longest;                           // key tiles of a row tile
@@ -189,9 +229,8 @@ LatentPrefillLayout latent_prefill_layout(const mc_latent_params* p, const int32
   for (int32_t r = 0; r < batch; ++r) l.items += latent_row_tiles(new_lens[r]);
   // From four rounds of workgroups on, whole row tiles keep the compute units busy to the end.
   if (l.items > 0 && l.items * p->num_heads <= 4 * kLatentWgs) {
-    std::vector<LatentReq> reqs((size_t)batch);
-    fill_latent_table(prefix_lens, new_lens, batch, reqs.data());
-    fill_latent_items(batch, 0, reqs.data());
+    std::vector<LatentReq> reqs((size_t)latent_entries(new_lens, batch));
+    fill_latent_entries(p, prefix_lens, new_lens, batch, reqs.data());
     PrefillCut best = cut_into(p, reqs, 0);
     const int32_t longest = best.longest;
     for (const int parts : {2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64}) {
@@ -210,7 +249,7 @@ LatentPrefillLayout latent_prefill_layout(const mc_latent_params* p, const int32
       l.part_rows = best.part_rows;
     }
   }
-  l.o_off = round_up(latent_table_bytes(batch));
+  l.o_off = round_up(latent_table_bytes(batch));             // (of what is uploaded: more than 64 requests)
   const size_t rows = (size_t)l.part_rows * (size_t)p->num_heads;
   l.ml_off = l.o_off + round_up(rows * p->head_dim * sizeof(float));
   l.total = l.ml_off + round_up(rows * 2 * sizeof(float)) + 256;

@@ -33,10 +33,15 @@ struct LatentLens {
 mc_status check_latent_lens(const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, LatentLens* out);
 
 size_t latent_table_bytes(int32_t batch);
-// The request table; and with the work items of expanded attention whose pieces have at most most_tiles key tiles (0: whole), the requests of most
-// keys first, so that what starts last is short.
+// The request table of the other calls.
 void fill_latent_table(const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, LatentReq* to);
-void fill_latent_items(int32_t batch, int32_t most_tiles, LatentReq* reqs);
+// That of expanded attention: of up to 64 requests and row tiles an entry each row tile (as a request whose prefix ends where it begins), those that take
+// longest first, so that what starts last is short; else the requests, those of most keys first.  (Entries of row tiles / of requests: 8 requests of 111 to
+// 2031 new tokens, 16 heads of 128 129.8 / 135.7 us, of 64 85.0 / 88.8; eight random batches 1 % sooner in the mean, from 2.4 % to -2.3.)  Work items are
+// pieces of at most most_tiles key tiles (0: whole).
+int32_t latent_entries(const int32_t* new_lens, int32_t batch);
+void fill_latent_entries(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, LatentReq* to);
+void fill_latent_items(int32_t entries, int32_t most_tiles, LatentReq* reqs);
 
 // Where the parts of an absorbed attention call lie in its workspace.
 struct LatentDecodeLayout {

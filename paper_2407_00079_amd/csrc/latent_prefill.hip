@@ -13,7 +13,7 @@
 //     where a block has any, a second product counts those that a row sees, and puts their sum in (0 times an infinity would be NaN).
 //
 // What bounds it: the power that matrix products may draw (8192 new tokens behind 8192, 16 heads of 128: 813 to 850 us by board, 1.21 to 1.27 PFLOP/s, where
-// the library's largest product makes 1.38); in ragged batches how row tiles share out over the compute units (8 requests of 111 to 2031 new tokens, 16 heads, 118 us where 87 would do
+// the library's largest product makes 1.38); in ragged batches how row tiles share out over the compute units (8 requests of 111 to 2031 new tokens, 16 heads, 113 us where 87 would do
 // if all units ended together); for one short chunk the time a key tile takes the few waves that have rows, 1 us, whatever their number.
 //
 // A row tile of many keys is cut into pieces, each a work item, where whole ones would leave compute units idle (latent_plan.cpp weighs how often: 45 new

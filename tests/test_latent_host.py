@@ -172,19 +172,24 @@ static int items(int heads, int head_dim, const std::vector<int32_t>& prefix, co
   const mc_latent_params p = {heads, 512, 64, head_dim, 16, MC_DTYPE_BF16, 1 << 20, 0.f};
   const int32_t batch = (int32_t)prefix.size();
   const LatentPrefillLayout l = latent_prefill_layout(&p, prefix.data(), fresh.data(), batch);
-  std::vector<LatentReq> reqs((size_t)batch);
-  fill_latent_table(prefix.data(), fresh.data(), batch, reqs.data());
-  fill_latent_items(batch, l.most_tiles, reqs.data());
-  std::vector<int> named((size_t)batch, 0);
+  const int32_t entries = latent_entries(fresh.data(), batch);
+  std::vector<LatentReq> reqs((size_t)entries);
+  fill_latent_entries(&p, prefix.data(), fresh.data(), batch, reqs.data());
+  fill_latent_items(entries, l.most_tiles, reqs.data());
+  std::vector<int64_t> rows((size_t)batch, 0);               // of each request that some entry has
   int64_t item = 0, part = 0, cut = 0, tiles = 0, new_tiles = 0;
-  for (int32_t r = 0; r < batch; ++r) {
+  for (int32_t r = 0; r < batch; ++r) tiles += latent_row_tiles(fresh[r]);
+  NEED(entries <= batch || (entries <= 64 && batch <= 64));
+  for (int32_t r = 0; r < entries; ++r) {
     const LatentReq& q = reqs[r];
-    NEED(q.row >= 0 && q.row < batch && !named[q.row]++ && q.prefix == prefix[q.row] && q.chunk == fresh[q.row]);
+    NEED(q.row >= 0 && q.row < batch);
     int64_t q_off = 0, k_off = 0;
     for (int i = 0; i < q.row; ++i) q_off += fresh[i], k_off += (int64_t)prefix[i] + fresh[i];
-    NEED(q.q_off == q_off && q.k_off == k_off && q.item_off == item && q.part_off == part && q.cut_off == cut);
-    NEED(r == 0 || reqs[r - 1].prefix + reqs[r - 1].chunk >= q.prefix + q.chunk);
-    tiles += latent_row_tiles(q.chunk);
+    const int64_t done = q.prefix - prefix[q.row];           // of its request, before the entry: whole row tiles
+    NEED(done >= 0 && done % 256 == 0 && done + q.chunk <= fresh[q.row] && (done + q.chunk == fresh[q.row] || q.chunk % 256 == 0));
+    NEED(q.q_off == q_off + done && q.k_off == k_off && q.item_off == item && q.part_off == part && q.cut_off == cut);
+    rows[q.row] += q.chunk;
+    NEED(entries == tiles || r == 0 || reqs[r - 1].prefix + reqs[r - 1].chunk >= q.prefix + q.chunk);
     for (int t = latent_row_tiles(q.chunk) - 1; t >= 0; --t) {
       const int keys = latent_key_tiles(q.prefix, q.chunk, t), pieces = latent_pieces(keys, l.most_tiles), height = latent_tile_height(q.chunk, t);
       NEED(height >= 1 && height <= 256 && keys >= 1 && pieces >= 1 && pieces <= keys);
@@ -194,6 +199,7 @@ static int items(int heads, int head_dim, const std::vector<int32_t>& prefix, co
       if (pieces > 1) cut += 1, part += (int64_t)pieces * height;
     }
   }
+  for (int32_t r = 0; r < batch; ++r) NEED(rows[r] == fresh[r]);
   NEED(tiles == new_tiles && item == l.items && part == l.part_rows && cut == l.cut_tiles);
   NEED(l.o_off >= latent_table_bytes(batch) && l.ml_off - l.o_off >= (size_t)part * heads * head_dim * 4 && l.total - l.ml_off >= (size_t)part * heads * 8);
   NEED(item * heads <= 4 * 1024 || l.most_tiles == 0);
