@@ -739,7 +739,7 @@ size_t mc_latent_workspace_bytes(int32_t batch);
  *   workspace  dev  >= mc_latent_workspace_bytes(batch), 16-byte aligned
  *
  * More than 64 requests are uploaded (no stream capture then).  Two requests whose block tables name the same page for positions both write:
- * undefined which wins.
+ * undefined which wins.  More than one launch holds, here and in the form below, is MC_ERR_RANGE: total_new_tokens * (H + 9) past about 2^30.
  */
 mc_status mc_latent_append_paged(const mc_latent_params* p, const mc_rope_params* rope, const void* q, const void* kv,
                                  const int64_t* strides, const void* norm, void* q_out, void* pool, const int32_t* block_tables,
@@ -821,6 +821,7 @@ mc_status mc_latent_expand_paged(const mc_latent_params* p, const void* weight, 
  * A key that a row does not see is never used as a value for it (its k, v and r may hold NaN).  Products on the matrix cores, fp32
  * accumulation and softmax; probabilities rounded to bf16 before they meet v.  More than 64 requests are uploaded (no stream capture then).
  * No new tokens: nothing is enqueued.  A key whose score is -inf, with v finite, counts for nothing (no others: 0, lse -inf).
+ * From 2^23 on, the sum of ceil(C_r / 256) times H is MC_ERR_RANGE.
  */
 size_t mc_latent_prefill_attn_workspace_bytes(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch);
 mc_status mc_latent_prefill_attn_paged(const mc_latent_params* p, const void* q, const void* k, const void* v, const int64_t* strides,

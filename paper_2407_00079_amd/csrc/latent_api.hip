@@ -210,7 +210,7 @@ mc_status mc_latent_prefill_attn_paged(const mc_latent_params* p, const void* q,
   if (!aligned4(block_tables) || !aligned4(lse)) return MC_ERR_ALIGN;
   LatentPrefillLayout lay;
   if (!plan_prefill(p, prefix_lens, new_lens, batch, &lay)) return MC_ERR_HIP;
-  if ((int64_t)batch * max_pages_per_req > INT32_MAX || lay.items * p->num_heads > INT32_MAX) return MC_ERR_RANGE;
+  if ((int64_t)batch * max_pages_per_req > INT32_MAX || lay.items * p->num_heads * mc::kLatentPrefillThreads > mc::kLatentMostThreads) return MC_ERR_RANGE;
   if (workspace == nullptr || workspace_bytes < lay.total) return MC_ERR_WORKSPACE;
 
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);

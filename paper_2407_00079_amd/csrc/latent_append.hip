@@ -17,7 +17,7 @@
 namespace mc {
 namespace {
 
-constexpr int kThreads = 256, kPairs = kLatentRope / 2, kRowB = kLatentRope * 2, kRowLanes = kRowB / 16;
+constexpr int kThreads = kLatentAppendThreads, kPairs = kLatentRope / 2, kRowB = kLatentRope * 2, kRowLanes = kRowB / 16;
 
 struct Place {
   int32_t row, pos;                          // block-table row; position, negative: the token is left out
@@ -178,9 +178,9 @@ __global__ __launch_bounds__(kThreads) void latent_append_kernel(const LatentApp
 
 template <int R, typename Source>
 void enqueue(const LatentAppendArgs& args, const Source& source, hipStream_t stream) {
-  constexpr int kInWave = 64 / (R / 8), kSlots = kThreads / kRowLanes;
-  auto rotating = [&](int u) { return (int)(((int64_t)args.total_tokens * (args.heads + 1) + kSlots * u - 1) / (kSlots * u)); };
-  auto latents = [&](int u) { return (int)(((int64_t)args.total_tokens + 4 * kInWave * u - 1) / (4 * kInWave * u)); };
+  static_assert(kRowLanes == 8, "the host counts workgroups by it");
+  auto rotating = [&](int u) { return (int)latent_rotating_wgs(args.total_tokens, args.heads, u); };
+  auto latents = [&](int u) { return (int)latent_row_wgs(args.total_tokens, R, u); };
   if (rotating(2) < 2 * 256) latent_append_kernel<R, 1><<<rotating(1) + latents(1), kThreads, 0, stream>>>(args, source, rotating(1));
   else latent_append_kernel<R, 2><<<rotating(2) + latents(2), kThreads, 0, stream>>>(args, source, rotating(2));
 }

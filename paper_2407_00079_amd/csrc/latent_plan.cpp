@@ -73,8 +73,9 @@ mc_status check_latent_append(const mc_latent_params* p, const void* q, const vo
   if (!aligned4(block_tables)) return MC_ERR_ALIGN;
   // in place only where a row is read and written at one place
   if (q == q_out && ((tokens > 1 && s.q_token != s.out_token) || (p->num_heads > 1 && s.q_head != s.out_head))) return MC_ERR_SHAPE;
-  // (workgroups of 32 rows of 64 columns, and of 4 latent rows)
-  return tokens > INT32_MAX || tokens * (p->num_heads + 1) / 32 + tokens / 4 + 2 > INT32_MAX ? MC_ERR_RANGE : MC_OK;
+  // (calls of this size have two rows of each kind a lane group)
+  const int64_t wgs = latent_rotating_wgs(tokens, p->num_heads, 2) + latent_row_wgs(tokens, p->latent_dim, 2);
+  return wgs * kLatentAppendThreads > kLatentMostThreads ? MC_ERR_RANGE : MC_OK;
 }
 
 mc_status check_latent_lens(const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, LatentLens* out) {

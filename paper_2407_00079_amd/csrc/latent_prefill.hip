@@ -87,7 +87,7 @@ __device__ __forceinline__ Item item_of(const LatentPrefillArgs& a, const Table&
 }
 
 template <int D, bool CUT, typename Table>
-__global__ __launch_bounds__(512) void latent_prefill_kernel(const LatentPrefillArgs a, const Table table) {
+__global__ __launch_bounds__(kLatentPrefillThreads) void latent_prefill_kernel(const LatentPrefillArgs a, const Table table) {
   constexpr int kRowB = D * 2, kSteps = D / 32, kRopeSteps = kLatentRope / 32, kDTiles = D / 16, kQRowB = (D + kLatentRope) * 2;
   constexpr int kKeyB = kTile * kRowB, kRopeB = kTile * 128;
   constexpr int kRopeBase = kBufs * kKeyB, kValueBase = kRopeBase + kBufs * kRopeB;       // keys of all buffers, their shared parts, values
@@ -586,9 +586,9 @@ template <int D, typename Table>
 hipError_t enqueue(const LatentPrefillArgs& args, const Table& table, hipStream_t stream) {
   const int wgs = args.items * args.heads;
   if (args.most_tiles == 0) {
-    latent_prefill_kernel<D, false><<<wgs, 512, 0, stream>>>(args, table);
+    latent_prefill_kernel<D, false><<<wgs, kLatentPrefillThreads, 0, stream>>>(args, table);
   } else {
-    latent_prefill_kernel<D, true><<<wgs, 512, 0, stream>>>(args, table);
+    latent_prefill_kernel<D, true><<<wgs, kLatentPrefillThreads, 0, stream>>>(args, table);
     latent_prefill_join_kernel<D><<<dim3(args.cut_tiles * args.heads, kLatentRows / kJoinRows), kJoinRows * 32, 0, stream>>>(args, table);
   }
   return hipGetLastError();

@@ -9,6 +9,18 @@ namespace mc {
 constexpr int kLatentRope = 64;              // columns of the shared key part, P
 constexpr int kLatentMostHeads = 1024;
 constexpr int kLatentMostTokens = 16;
+constexpr int64_t kLatentMostThreads = UINT32_MAX;           // of a launch
+
+// Append: rotated rows (H + 1 of a token), and latent rows, that a workgroup takes; per_group: of each kind and lane group
+constexpr int kLatentAppendThreads = 256, kLatentPrefillThreads = 512;
+constexpr int64_t latent_rotating_wgs(int64_t tokens, int heads, int per_group) {
+  const int64_t rows = kLatentAppendThreads / 8 * per_group;
+  return (tokens * (heads + 1) + rows - 1) / rows;
+}
+constexpr int64_t latent_row_wgs(int64_t tokens, int latent_dim, int per_group) {
+  const int64_t rows = kLatentAppendThreads / (latent_dim / 8) * per_group;
+  return (tokens + rows - 1) / rows;
+}
 
 // A request of a call with host lengths.
 struct LatentReq {

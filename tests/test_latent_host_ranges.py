@@ -1,0 +1,35 @@
+"""Calls on a cache of latent vectors that one launch does not hold are refused as such, before anything is uploaded or launched."""
+import pytest
+
+from paper_2407_00079_amd import binding as B
+from test_latent_host import call, par
+
+MOST = 2 ** 32 - 1           # threads of a launch
+APPEND, PREFILL = 256, 512   # of a workgroup
+
+
+@pytest.mark.parametrize("heads", [48, 64, 1024])
+def test_prefills_that_one_launch_does_not_hold(heads):
+    """One workgroup a row tile and head, here of one row."""
+    most = MOST // PREFILL // heads
+    for n, status in ((most, B.MC_ERR_WORKSPACE), (most + 1, B.MC_ERR_RANGE)):       # (the workspace is looked at behind)
+        assert call("prefill", p=par(heads=heads), prefix=(0,) * n, new=(1,) * n, max_pages=1, ws=None) == status
+
+
+@pytest.mark.parametrize("heads,latent", [(1, 512), (1, 256), (16, 512), (128, 256), (1024, 512)])
+def test_appends_that_one_launch_does_not_hold(heads, latent):
+    """64 rotated rows a workgroup, H + 1 of a token; behind them the latent rows, 8 or 16 a workgroup."""
+    def workgroups(tokens):
+        return -(-tokens * (heads + 1) // 64) + -(-tokens // (8 if latent == 512 else 16))
+
+    low, high = 1, 2 ** 31 - 1025
+    while low < high:                                          # the most tokens that fit
+        mid = (low + high + 1) // 2
+        low, high = (mid, high) if workgroups(mid) * APPEND <= MOST else (low, mid - 1)
+    p = par(heads=heads, latent=latent)
+    for tokens, status in ((low, B.MC_ERR_WORKSPACE), (low + 1, B.MC_ERR_RANGE)):
+        assert call("append", p=p, prefix=(0,), new=(tokens,), max_pages=2 ** 27, ws=None) == status
+    assert call("append_decode", p=p, batch=low + 1, tokens=1, max_pages=1) == B.MC_ERR_RANGE
+    assert call("append_decode", p=p, batch=-(-(low + 1) // 16), tokens=16, max_pages=1) == B.MC_ERR_RANGE
+    # ... and every call with so few rows does fit
+    assert workgroups((2 ** 30 - 192) // (heads + 9)) * APPEND <= MOST
