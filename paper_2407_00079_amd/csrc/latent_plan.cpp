@@ -79,16 +79,13 @@ mc_status check_latent_append(const mc_latent_params* p, const void* q, const vo
 }
 
 mc_status check_latent_lens(const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, LatentLens* out) {
-  *out = {0, 0, 0, 0};
+  *out = {0, 0, 0};
   for (int32_t r = 0; r < batch; ++r) {
     const int32_t before = prefix_lens != nullptr ? prefix_lens[r] : 0;
     if (before < 0 || new_lens[r] < 0) return MC_ERR_SHAPE;
     const int64_t len = (int64_t)before + new_lens[r];
     if (len > kMostLatentTokens) return MC_ERR_RANGE;
-    if (new_lens[r] > 0) {
-      out->need_pages = std::max(out->need_pages, (int32_t)((len + 15) / 16));
-      out->most_keys = std::max(out->most_keys, (int32_t)len);
-    }
+    if (new_lens[r] > 0) out->need_pages = std::max(out->need_pages, (int32_t)((len + 15) / 16));
     out->total_new += new_lens[r];
     out->total_keys += len;
   }

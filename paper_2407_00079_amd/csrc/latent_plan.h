@@ -28,7 +28,7 @@ constexpr int64_t kMostLatentTokens = INT32_MAX - 1024;
 // Lengths of a batch with `prefix_lens` null for none before: sign and range checks, sums, most pages of a request that has any new tokens.
 struct LatentLens {
   int64_t total_new, total_keys;             // total_keys: to be checked by who counts keys
-  int32_t need_pages, most_keys;             // most_keys: of a request with new tokens
+  int32_t need_pages;
 };
 mc_status check_latent_lens(const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch, LatentLens* out);
 
