@@ -820,7 +820,8 @@ mc_status mc_latent_expand_paged(const mc_latent_params* p, const void* weight, 
  *
  * A key that a row does not see is never used as a value for it (its k, v and r may hold NaN).  Products on the matrix cores, fp32
  * accumulation and softmax; probabilities rounded to bf16 before they meet v.  More than 64 requests are uploaded (no stream capture then).
- * No new tokens: nothing is enqueued.  A key whose score is -inf, with v finite, counts for nothing (no others: 0, lse -inf).
+ * No new tokens: nothing is enqueued.  A key that a row sees and whose score is NaN or +inf makes the row NaN; one whose score is -inf, with v
+ * finite, counts for nothing (no others: 0, lse -inf).
  * From 2^23 on, the sum of ceil(C_r / 256) times H is MC_ERR_RANGE.
  */
 size_t mc_latent_prefill_attn_workspace_bytes(const mc_latent_params* p, const int32_t* prefix_lens, const int32_t* new_lens, int32_t batch);
