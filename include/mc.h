@@ -486,6 +486,12 @@ mc_status mc_kv_pages_fork(int32_t* ref_counts, int64_t num_pages, int32_t* bloc
  * each row's last token over, in a page that other rows may share.  Look at the report first, or give the step a copy of the
  * lengths that is 0 wherever report[1] is not.  (A row of length 0 grows like any other: add is 0 for rows that are to stay empty.)
  *
+ * The lengths of this state say which pages a row has, so they only grow, but for mc_kv_pages_free: a length that was lowered over a page's end and
+ * grows again gets a new page in place of the one the table has there, whose count then never falls.  A program that takes tokens back (drafts
+ * that were refused) keeps the lengths that count in a tensor of its own, len <= seq_lens, lets rows hold add = len + n - seq_lens more
+ * before a step of n tokens, and gives the step len + n.  mc_kv_pages_fork copies the page in which seq_lens ends and shares those before,
+ * so it takes such a row only while len ends there, too: len / page_size == seq_lens / page_size.
+ *
  *   add     dev  int32 [rows]
  *   report  { pages given, flags, free pages left, pages wanted }
  *   rows == 0 enqueues nothing.
