@@ -706,7 +706,8 @@ mc_status mc_prefix_match(const uint64_t* keys, const int64_t* key_offsets, int3
  *   pool  dev  [num_pages, page_size, R + P]   a layer's cache: row j of a request is pool[block_tables[r][j / 16]][j % 16][:] = [c(j), r(j)]
  *
  * Block tables, lengths and the care of pages (mc_kv_pages_*) are those of the other cache; the calls that move pages take two pools at a time
- * (mc_kv_copy_pages, mc_kv_pack_layer and their relatives): give them two layers' pools.
+ * (mc_kv_copy_pages, mc_kv_pack_layer and their relatives): give them two layers' pools, with page_bytes = 32 (R + P).  A last layer without a partner
+ * may be given as both, with one buffer as both of the other side: its bytes are then written twice, the same ones.
  */
 typedef struct {
   int32_t num_heads;    /* H: 1 .. 1024 */
