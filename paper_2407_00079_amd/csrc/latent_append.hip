@@ -11,7 +11,7 @@
 // stand behind the others in the same launch.
 //
 // What bounds it: HBM.  8192 tokens of 16 heads 52 MB, 11.5 us = 4.6 TB/s with the launch's ends (a copy of this size 8.7 + 3); 4085 tokens of 128 heads 143 MB,
-// 28.0 us, 5.1 TB/s; 64 single tokens 3.4 us, a launch and dependent loads.
+// 28.7 us, 5.0 TB/s; 64 single tokens 3.4 us, a launch and dependent loads.
 #include "latent_device.h"
 
 namespace mc {

@@ -16,13 +16,19 @@
 //   * The tiles of all rows stand in one line, of which each workgroup takes an equal stretch; it finds its place from the lengths.  Rows that a stretch's
 //     end cuts leave partial results in the workspace, in the order of the registers, and a second kernel joins them in the order of the line.
 //
-// What bounds it: with 16 rows a workgroup the cache's bytes (one row of 131071 keys, 16 heads: 151 MB in 27.9 us, 5.4 TB/s; 128 rows of 704 to 1408 keys
-// 2.75 us a tile, 6.9 TB/s), behind it a join of 5.6 us.  With 64 rows (128 heads, or 4 tokens of 16) what a tile takes from end to end of a wave: 2.5 us
-// at R 512 (1.55 at R 256), of which matrix products 0.9 and LDS reads 1.4, one after the other for the most part, since two buffers of 72 KiB leave no
-// room for a second workgroup: 51 rows of 120 to 8000 keys, 128 heads, 50.5 us and 9.6 in the join; 64 rows of 4 tokens of 16 heads 38.1 and 9.0.
+//   * A probability is rounded to bf16 before it meets a value, for one matrix product a tile: with what the rounding leaves out as a second operand the
+//     products with values, half of a tile's, and what goes through LDS for them would double.  Sums take it as it was.
 //
-// Rows of a workgroup: a tile of R 512 takes 2.5 to 2.75 us whether it has 16, 32 or 64 rows, so as few workgroups as 64 rows make; 16 or 32 where that is
-// all there is, for fewer rows of queries and partial results (two tiles a row, nothing cut: 13.9 / 19.5 / 22.0 us a call).  Tried, slower: groups of four waves
+// What bounds it, with inputs that no cache holds.  A tile takes a workgroup, 256 of them at once, us at R 512 / 256: 3.2 / 1.9 with 16 rows (the cache's bytes, 6.0 and
+// 5.5 TB/s), 3.4 / 2.2 with 64, 2.7 where two workgroups share a row's keys (128 heads); alone a tile of 64 rows is 2.5 / 1.55 from end to end of a wave,
+// matrix products 0.9 and LDS reads 1.4 of it, mostly one after the other, since two buffers of 72 KiB leave no room for a second workgroup.  Before and behind
+// the tiles, whatever their number (1 to 16 tiles a workgroup, no row cut): 7 to 9 / 5 us with 16 rows, 14 to 18 / 10 with 64: launch, lengths, tables, queries, the
+// first tile's way, results (128 rows of 128 heads: 36 MB of queries and results, 6 us).  So one row of 131071 keys, 16 heads: 8 or 9 tiles, 33.3 us, 4.5 TB/s, and 5.8
+// in the join; 51 rows of 120 to 8000 keys, 128 heads: 12 tiles, 32 us, with 14 to 16 and 37 MB of partial results 53.8, and 9.5 in the join that reads them; 64 rows of
+// 4 tokens of 16 heads: 5 tiles, 17 us, with 14 to 18 and 34 MB 43.4, and 9.4.
+//
+// Rows of a workgroup: a tile of R 512 takes about as long with 16, 32 or 64 rows, so as few workgroups as 64 rows make; 16 or 32 where that is all there
+// is, for fewer rows of queries and partial results (two tiles a row, nothing cut: 13.9 / 19.5 / 22.0 us a call).  Tried, slower: groups of four waves
 // for each 16 rows; scores of two row tiles a wave (R 512 does not fit the registers, R 256 the same 1.55 us); halves of 32 keys in four buffers, the
 // values of one while the next one's scores are made (3.0 us a tile of R 256, 4.6 of R 512: a half takes as long from end to end); no maxima unless a
 // probability reaches 2 (the same).
@@ -234,7 +240,7 @@ __global__ __launch_bounds__(kWaves * 64) void latent_decode_kernel(const Latent
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i], c, -from));
-            sum += p[i];                                     // (before its rounding: lse keeps 32 bits)
+            sum += p[i];                                     // (before its rounding: sums keep 32 bits)
           }
           const uint32_t low = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[0], p[1]}, bf16x2));
           const uint32_t high = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{p[2], p[3]}, bf16x2));

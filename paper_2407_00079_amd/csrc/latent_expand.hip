@@ -9,8 +9,10 @@
 // another: the next tile's rows are looked up during a tile, its first steps are copied under the last ones, and the stores of a tile are not waited
 // for before the next begins.
 //
-// What bounds it: 131072 tokens, 16 heads of 128, R 512 597 us, 920 TFLOP/s; the library's product of that shape, from a dense left side, 684 to 696.  398 us
-// of it are what its largest product makes, the rest mostly the 1074 MB of outputs, which the products do not hide.  Workgroups that stay 714 -> 700; three
+// What bounds it: 131072 tokens, 16 heads of 128, R 512 611 us, 900 TFLOP/s (over the same inputs again and again 597); the library's product of that shape, from
+// a dense left side, 684 to 696.  398 us of it are what its largest product makes, the rest mostly the 1074 MB of outputs, which the products do not hide, and
+// 500 MB read for 155, as groups of outputs read the tokens again.  Tiles of 256 by 256 spill 8 to 12 registers, none of them in the loop over steps: a tile reads
+// 5 to 7 values back from scratch memory.  Workgroups that stay 714 -> 700; three
 // steps ahead and outputs by groups 670; whole 128-byte lines to a store instead of halves, which had written 1296 MB, 616; every bank once and groups of
 // eight 597.  Tried, no faster: two workgroups of four waves a compute unit.  Which tiles when: see enqueue.
 #include "attn_narrow_device.h"

@@ -8,16 +8,20 @@
 //   * Scores as S^T = K Q^T on 16x16x32 matrix instructions, head_dim / 32 + 2 steps: lane l holds, for rows l % 16 of both tiles, the 8 keys
 //     4 (l / 16) + {0..3} and 16 + 4 (l / 16) + {0..3} of a block of 32.  Its probabilities are then the B operand of O^T += V^T P^T as they are,
 //     and V^T fragments come by two transposing LDS reads in the same order.  Each fragment read feeds two instructions.
-//   * Softmax in one pass in fp32, its reference lagging behind the largest score by at most 2^8.
+//   * Softmax in one pass in fp32, its reference lagging behind the largest score by at most 2^8.  A probability is rounded to bf16 before it meets
+//     a value, for one matrix product: with what the rounding leaves out as a second operand the kernel, bound by them, would have 40 % more of them
+//     (33 with heads of 64).  Sums take it as it was.
 //   * On the diagonal, keys that a row does not see get probability 0, and elements of V that are not finite are taken out of the products there;
 //     where a block has any, a second product counts those that a row sees, and puts their sum in (0 times an infinity would be NaN).
 //
-// What bounds it: the power that matrix products may draw (8192 new tokens behind 8192, 16 heads of 128: 813 to 850 us by board, 1.21 to 1.27 PFLOP/s, where
-// the library's largest product makes 1.38); in ragged batches how row tiles share out over the compute units (8 requests of 111 to 2031 new tokens, 16 heads, 113 us where 87 would do
-// if all units ended together); for one short chunk the time a key tile takes the few waves that have rows, 1 us, whatever their number.
+// What bounds it: the power that matrix products may draw (8192 new tokens behind 8192, 16 heads of 128: 804 to 850 us by board and by what ran before, 1.21 to 1.28
+// PFLOP/s, where the library's largest product makes 1.38); in ragged batches how row tiles share out over the compute units (8 requests of 111 to 2031 new tokens, 16
+// heads, 109 us and 5.9 in the join, where 87 would do if all units ended together); for one short chunk the time a key tile takes the few waves that have
+// rows, 1 us, whatever their number.  With heads of 128 20 registers are spilled (15 where row tiles are cut), all of them near the diagonal: the loop over
+// tiles that every row sees has none.
 //
 // A row tile of many keys is cut into pieces, each a work item, where whole ones would leave compute units idle (latent_plan.cpp weighs how often: 45 new
-// tokens behind 20011, 10 heads of 64, 44 -> 19.4 us and 4.4 in the join).  The join reads cut row tiles alone.
+// tokens behind 20011, 10 heads of 64, 44 -> 18.9 us and 4.4 in the join).  The join reads cut row tiles alone.
 #include "attn_narrow_device.h"
 #include "latent_device.h"
 

@@ -46,8 +46,9 @@ constexpr int latent_tile_rows(int64_t stacked) { return stacked <= 16 ? 16 : st
 constexpr int latent_tiles(int64_t stacked) { return (int)((stacked + latent_tile_rows(stacked) - 1) / latent_tile_rows(stacked)); }
 // workgroups a tile has
 constexpr int latent_stretches(int tiles) { return tiles >= kLatentWgs ? 1 : kLatentWgs / tiles; }
-// How many stretches have work (decode_begin says where each begins, decode_wave_of which has a place).  A tile takes its workgroup 2.4 to 2.7 us, and what
-// is joined behind takes 0.05 to 0.08 us a part of a row, so t tiles of r rows are done soonest by about sqrt(30 t r) stretches.  Short rows are
+// How many stretches have work (decode_begin says where each begins, decode_wave_of which has a place).  A tile takes its workgroup 2.4 to 2.7 us of what
+// caches hold (3.2 from memory), and what is joined behind takes 0.05 to 0.08 us a part of a row, so t tiles of r rows are done soonest by about
+// sqrt(30 t r) stretches (40 would be as right; whether they come out in equal tiles is not weighed).  Short rows are
 // cut least by stretches of one tile, although each begins and ends: us, one tile at least / two, 16 and 64 query rows, 50 lengths of 1 to 256 tokens
 // 12.4 / 15.2, 24.3 / 29.1; 20 to 640 12.7 / 15.4, 22.4 / 26.5; 10 to 2048 13.2 / 14.3, 24.1 / 26.3; two tiles of 64 rows, 135 tiles of keys for 128
 // workgroups 26.0 / 31.7, 160 30.5 / 30.0.  (Lengths that are all the same meet the ends of two: 64 rows of 128 11.6 / 10.1, 23.9 / 17.9.)
