@@ -709,6 +709,9 @@ mc_status mc_prefix_match(const uint64_t* keys, const int64_t* key_offsets, int3
  * tokens, 16 heads, R 512: 254 / 300 us expanded, 181 / 312 absorbed; 64 / 128, 10 heads of 64, R 256: 83 / 89 and 75 / 111.)  The chunk goes through
  * mc_latent_append_paged, and its attention as rows of up to 16 tokens: entry i of block_tables is the request's line again, of seq_lens P_r + 16 (i + 1).
  *
+ * Scores are held in 32 bits in both forms.  From a size of about 2^30 on these leave no differences that a softmax could use, and a row with such
+ * scores, though they are finite, may be 0 or NaN.
+ *
  *   pool  dev  [num_pages, page_size, R + P]   a layer's cache: row j of a request is pool[block_tables[r][j / 16]][j % 16][:] = [c(j), r(j)]
  *
  * Block tables, lengths and the care of pages (mc_kv_pages_*) are those of the other cache; the calls that move pages take two pools at a time
@@ -723,7 +726,7 @@ typedef struct {
   int32_t page_size;    /* 16 */
   int32_t dtype;        /* MC_DTYPE_BF16 */
   int64_t num_pages;    /* N pages in a pool */
-  float softmax_scale;  /* 0 selects 1 / sqrt(head_dim + rope_dim), in both forms */
+  float softmax_scale;  /* 0 selects 1 / sqrt(head_dim + rope_dim), in both forms; times log2(e) it has to be finite in 32 bits */
 } mc_latent_params;
 #define MC_LATENT_MAX_HEADS 1024
 #define MC_LATENT_MAX_TOKENS 16

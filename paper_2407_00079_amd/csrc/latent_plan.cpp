@@ -25,7 +25,7 @@ mc_status check_latent(const mc_latent_params* p) {
   if (p->dtype != MC_DTYPE_BF16 || p->page_size != 16 || p->rope_dim != kLatentRope) return MC_ERR_UNSUPPORTED;
   if (p->latent_dim != 512 && p->latent_dim != 256) return MC_ERR_UNSUPPORTED;
   if (p->head_dim != 128 && p->head_dim != 64) return MC_ERR_UNSUPPORTED;
-  if (!(p->softmax_scale >= 0.f) || std::isinf(p->softmax_scale)) return MC_ERR_SHAPE;
+  if (!(p->softmax_scale >= 0.f) || std::isinf(latent_scale_log2e(p))) return MC_ERR_SHAPE;
   if (p->num_heads > kLatentMostHeads) return MC_ERR_RANGE;
   return MC_OK;
 }

@@ -33,3 +33,12 @@ def test_appends_that_one_launch_does_not_hold(heads, latent):
     assert call("append_decode", p=p, batch=-(-(low + 1) // 16), tokens=16, max_pages=1) == B.MC_ERR_RANGE
     # ... and every call with so few rows does fit
     assert workgroups((2 ** 30 - 192) // (heads + 9)) * APPEND <= MOST
+
+
+@pytest.mark.parametrize("form", ["append", "append_decode", "decode", "expand", "prefill"])
+def test_scales_past_32_bits(form):
+    """The kernels take the scale times log2(e) in 32 bits: where that is infinite, 0 times it would be NaN."""
+    largest = 2.0 ** 128 * (1 - 2.0 ** -25)                    # (from here on a number rounds to infinity)
+    assert call(form, p=par(scale=3e38)) == B.MC_ERR_SHAPE
+    assert call(form, p=par(scale=1.0001 * largest / 1.4426950408889634)) == B.MC_ERR_SHAPE
+    assert call(form, p=par(scale=0.9999 * largest / 1.4426950408889634), pool=None) == B.MC_ERR_NULL     # (which is looked at behind)
